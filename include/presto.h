@@ -75,8 +75,13 @@ enum {
     PRESTO_FLAG_NGRAM_BAD = 4,   /* an n-gram entry was invalid and skipped    */
     PRESTO_FLAG_NGRAM_FULL = 8,  /* an n-gram entry found no free table slot   */
     PRESTO_FLAG_BAD_INDEX = 16,  /* presto_topk_rows: a row index outside the logits */
-    PRESTO_FLAG_KV_COMMIT = 32   /* round bookkeeping: a sequence's slot, length or
+    PRESTO_FLAG_KV_COMMIT = 32,  /* round bookkeeping: a sequence's slot, length or
                                     path was invalid; that sequence was skipped */
+    PRESTO_FLAG_BAD_PAGE = 64,   /* paged cache: a page-table entry that is needed lies
+                                    outside the pool, or names a page that is free */
+    PRESTO_FLAG_NO_PAGES = 128,  /* paged cache: the pool ran out of free pages */
+    PRESTO_FLAG_BAD_SEQ = 256    /* paged cache: a sequence index, length or offset
+                                    outside its range, or a fork that cannot be made */
 };
 
 /* ------------------------------------------------------------------------ */
@@ -416,6 +421,180 @@ presto_status presto_flatten_slots(int32_t batch, int32_t n_max, int32_t slots,
                                    const int32_t *n_nodes, const int32_t *root_pos,
                                    int32_t *pos_out, uint64_t *anc_out, int32_t *n_rows,
                                    hipStream_t stream);
+
+/* ------------------------------------------------------------------------ */
+/* Paged KV cache: prompts, plain decoding and shared prefixes, beside the
+ * packed and slot caches that presto_tree_attention reads.
+ *
+ * A cache is a pool of num_pages pages of page_size positions, K and V each,
+ * per layer:
+ *   k_pages, v_pages [layers, num_pages, page_size, hkv, head_dim]
+ *                    page p of layer l starts at l * layer_stride + p *
+ *                    page_stride elements, and is contiguous itself (so K and
+ *                    V may be the halves of one tensor of page pairs)
+ *   page_table [batch, max_pages] int32 device: position j of sequence b is
+ *                    row j % page_size of page page_table[b, j / page_size];
+ *                    -1: no page
+ *   refs [num_pages] int32 device: the table entries that hold a page; 0: free
+ *   ctx [batch] int32 device: cached positions of each sequence
+ * One table serves all layers.  Rows are laid out as in the other caches: a
+ * slot of presto_commit_kv that starts at a multiple of page_size is a run of
+ * consecutive pages, and the other way round.  A program starts with refs and
+ * ctx 0 and page_table -1.
+ *
+ * A step is presto_pages_reserve (pages for the new positions, the new
+ * lengths), presto_append_kv and an attention call per layer.
+ *
+ * Limits: page_size a power of two, 16 .. 1024; head_dim in {64, 128}; hkv
+ * 1 .. 4096; 1 <= num_pages; max_pages 1 .. 2^20, max_pages * page_size <
+ * 2^30; batch >= 0 (0: nothing to do); layers >= 1; page_stride >= page_size *
+ * hkv * head_dim (0: exactly that), layer_stride >= 0; pools 16-byte aligned
+ * with strides of a multiple of 16 bytes.  Layers of a pool must not overlap.
+ */
+typedef struct {
+    int32_t batch, max_pages;
+    int32_t num_pages, page_size, hkv, head_dim;
+    presto_dtype dt;
+    int32_t layers;       /* read by the calls that move pages only */
+    int64_t page_stride;  /* elements; 0: page_size * hkv * head_dim */
+    int64_t layer_stride; /* elements; 0: num_pages * page_stride */
+} presto_pages_desc;
+
+/* Attention over the paged cache of one layer, causal, with grouped query
+ * heads.  A query of sequence b at position p sees key j when
+ *     j <= p  and  (window == 0  or  j > p - window  or  j < sinks),
+ * and O = softmax_j(scale * q . k_j) v_j over the keys it sees (zeros if it
+ * sees none).  Only pages that hold a visible key are needed; the others may
+ * be -1.
+ *
+ * presto_paged_attention: one new token per sequence, at position ctx[b] - 1
+ *   (its K/V are in the cache already: ctx counts it).
+ *   q, out [batch, hq, head_dim]; max_q and total_q are ignored
+ * presto_window_attention: a ragged batch of new tokens.
+ *   q_offsets [batch + 1] int32 device, non-decreasing; rows q_offsets[b] ..
+ *   q_offsets[b + 1] - 1 of q are the last n_b positions of sequence b (row i
+ *   at ctx[b] - n_b + i), whose K/V are in the cache already; n_b = 0 is
+ *   allowed.  Rows at negative positions (n_b > ctx[b]) see nothing.  Rows of
+ *   q outside all sequences are not read, nor are those rows of out written.
+ *   q, out [total_q, hq, head_dim]; every n_b <= max_q
+ *
+ * q rows are q_stride elements apart (a slice of a wider projection), out is
+ * contiguous.  A page-table entry that a visible key needs and that lies
+ * outside the pool raises PRESTO_FLAG_BAD_PAGE; its keys count as not
+ * visible.  ctx[b] outside 0 .. max_ctx is cut to that range, n_b > max_q to
+ * the first max_q rows (the others are not written), and offsets out of
+ * order or past total_q skip the sequence; each raises PRESTO_FLAG_BAD_SEQ.
+ * A K or V that is not finite reaches the queries that see it only.
+ * Arithmetic: bf16 inputs use bf16 matrix cores with fp32 accumulation and
+ * fp32 softmax; fp32 inputs use fp32 throughout.
+ * Limits: hq % hkv == 0; max_ctx <= max_pages * page_size; window, sinks 0 ..
+ * 2^30 (sinks without a window change nothing); max_q * hq / hkv < 2^30,
+ * total_q < 2^30; bf16 and fp32; q and out 16-byte aligned, q_stride a
+ * multiple of 16 bytes.
+ */
+typedef struct {
+    presto_pages_desc pages;
+    int32_t hq;
+    int32_t max_q;   /* presto_window_attention: the most new tokens of a sequence */
+    int32_t max_ctx; /* the largest ctx[b] */
+    int32_t window, sinks;
+    float scale; /* usually 1/sqrt(head_dim) */
+    int64_t total_q;
+    int64_t q_stride; /* elements; 0: hq * head_dim */
+    int64_t total_ctx; /* sum of ctx over the batch, 0: unknown.  Scheduling only */
+} presto_paged_attn_desc;
+
+size_t presto_paged_attention_workspace(const presto_paged_attn_desc *desc);
+presto_status presto_paged_attention(const presto_paged_attn_desc *desc, const void *q,
+                                     const void *k_pages, const void *v_pages,
+                                     const int32_t *page_table, const int32_t *ctx, void *out,
+                                     int32_t *flags, void *ws, size_t ws_bytes,
+                                     hipStream_t stream);
+size_t presto_window_attention_workspace(const presto_paged_attn_desc *desc);
+presto_status presto_window_attention(const presto_paged_attn_desc *desc, const void *q,
+                                      const int32_t *q_offsets, const void *k_pages,
+                                      const void *v_pages, const int32_t *page_table,
+                                      const int32_t *ctx, void *out, int32_t *flags, void *ws,
+                                      size_t ws_bytes, hipStream_t stream);
+
+/* Pages for new positions: ctx_out[b] = ctx[b] + add[b] + extra (add may be
+ * NULL: extra alone, e.g. 1 for a decode step), and every table entry of those
+ * positions that holds no page gets the lowest free one, in order of sequence
+ * and position.  Entries that hold a page keep it; columns below ctx[b]'s last
+ * page are not looked at.  Sequences are served in order: where the free pages
+ * do not reach, that sequence and the later ones that need any keep their
+ * length and table, and PRESTO_FLAG_NO_PAGES is raised.  A negative ctx or add
+ * or a length past max_pages * page_size leaves the sequence alone and raises
+ * PRESTO_FLAG_BAD_SEQ.  ctx_out may be ctx.
+ */
+size_t presto_pages_workspace(const presto_pages_desc *desc); /* for every call below */
+presto_status presto_pages_reserve(const presto_pages_desc *desc, int32_t *refs,
+                                   int32_t *page_table, const int32_t *ctx, const int32_t *add,
+                                   int32_t extra, int32_t *ctx_out, int32_t *flags, void *ws,
+                                   size_t ws_bytes, hipStream_t stream);
+
+/* Writes new K/V rows of one layer into the cache: row offsets[b] + i of
+ * k_new, v_new [new_rows, hkv, head_dim] (rows new_stride elements apart, 0:
+ * contiguous) goes to position ctx[b] + i, i = 0 .. ctx_new[b] - ctx[b] - 1
+ * (ctx and ctx_new before and after presto_pages_reserve: a sequence that got
+ * no pages writes nothing).  offsets [batch + 1] int32 device; a sequence may
+ * write fewer rows than offsets gives it.  Positions without a page are
+ * skipped (PRESTO_FLAG_BAD_PAGE); a sequence whose lengths or offsets do not
+ * fit (more than max_new or than its rows, offsets out of order or past
+ * new_rows) is skipped (PRESTO_FLAG_BAD_SEQ).  No page is written that another
+ * sequence shares as long as pages come from the calls here.
+ * Limits: new_rows < 2^31; 16-byte aligned, new_stride a multiple of 16 bytes.
+ */
+presto_status presto_append_kv(const presto_pages_desc *desc, const void *k_new, const void *v_new,
+                               int64_t new_rows, int64_t new_stride, const int32_t *offsets,
+                               int32_t max_new, void *k_pages, void *v_pages,
+                               const int32_t *page_table, const int32_t *ctx,
+                               const int32_t *ctx_new, int32_t *flags, hipStream_t stream);
+
+/* Sequences that share pages.
+ *
+ * presto_pages_fork: sequence child[i] (empty: ctx 0 and no page) takes the
+ *   length and the prefix of parent[i], i < n: the parent's full pages are
+ *   shared, and the rows of its partly filled last page are copied, in all
+ *   layers, into the lowest free page (in order of i; the rest of that page is
+ *   left as it was).  Pages reserved past ctx are not shared.  A fork that
+ *   cannot be made (an index outside the batch, a child that is not empty, is
+ *   its own parent or was named before, a prefix with entries outside the pool
+ *   or free) is skipped with PRESTO_FLAG_BAD_SEQ; one without a free page left
+ *   with PRESTO_FLAG_NO_PAGES.  Parents are read as they were before the call.
+ * presto_pages_free: drops all references of the sequences rows[0 .. n - 1]
+ *   and sets their ctx to 0; a page whose last reference goes is free.  A
+ *   sequence named twice is dropped once.  An index outside the batch raises
+ *   PRESTO_FLAG_BAD_SEQ, an entry outside the pool or to a free page
+ *   PRESTO_FLAG_BAD_PAGE (the entry is cleared).
+ * presto_pages_trim: drops, of every sequence, the references to pages whose
+ *   positions no query at position ctx[b] - 1 or later sees under window and
+ *   sinks.  Flags as above.
+ * presto_pages_compact: moves the live pages to the front of the pool, in all
+ *   layers: of *n_live (int32 device) live pages, the i-th free page below
+ *   *n_live takes the i-th live one from there on.  refs_out [num_pages] and
+ *   table_out [batch, max_pages] are the books afterwards (refs_out may be
+ *   refs, table_out may be page_table), page_map [num_pages] (may be NULL)
+ *   the new number of every live page, -1 for a free one.  The old table
+ *   stays readable until a freed page is written.  An entry outside the pool
+ *   or to a free page becomes -1 (PRESTO_FLAG_BAD_PAGE).
+ * Limits: 0 <= n <= batch.
+ */
+presto_status presto_pages_fork(const presto_pages_desc *desc, int32_t *refs, int32_t *page_table,
+                                int32_t *ctx, const int32_t *parent, const int32_t *child,
+                                int32_t n, void *k_pages, void *v_pages, int32_t *flags, void *ws,
+                                size_t ws_bytes, hipStream_t stream);
+presto_status presto_pages_free(const presto_pages_desc *desc, int32_t *refs, int32_t *page_table,
+                                int32_t *ctx, const int32_t *rows, int32_t n, int32_t *flags,
+                                hipStream_t stream);
+presto_status presto_pages_trim(const presto_pages_desc *desc, int32_t *refs, int32_t *page_table,
+                                const int32_t *ctx, int32_t window, int32_t sinks, int32_t *flags,
+                                hipStream_t stream);
+presto_status presto_pages_compact(const presto_pages_desc *desc, const int32_t *refs,
+                                   int32_t *refs_out, const int32_t *page_table,
+                                   int32_t *table_out, int32_t *n_live, int32_t *page_map,
+                                   void *k_pages, void *v_pages, int32_t *flags, void *ws,
+                                   size_t ws_bytes, hipStream_t stream);
 
 /* ------------------------------------------------------------------------ */
 const char *presto_status_string(presto_status s);

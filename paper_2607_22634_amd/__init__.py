@@ -16,4 +16,10 @@ from ._lib import (  # noqa: F401
     presto_ngram_gather, presto_ngram_insert, presto_ngram_table_bytes, presto_topk,
     presto_topk_noalloc,
     presto_tree_attention, topk_fallback_chunks, topk_workspace, version,
+    PRESTO_FLAG_BAD_PAGE, PRESTO_FLAG_BAD_SEQ, PRESTO_FLAG_NO_PAGES, PagedAttnDesc, PagesDesc,
+)
+from ._paged import (  # noqa: F401
+    paged_attention_workspace, pages_workspace, presto_append_kv, presto_paged_attention,
+    presto_pages_compact, presto_pages_fork, presto_pages_free, presto_pages_reserve,
+    presto_pages_trim, presto_window_attention,
 )

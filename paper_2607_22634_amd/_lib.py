@@ -36,6 +36,9 @@ PRESTO_FLAG_NGRAM_BAD = 4
 PRESTO_FLAG_NGRAM_FULL = 8
 PRESTO_FLAG_BAD_INDEX = 16
 PRESTO_FLAG_KV_COMMIT = 32
+PRESTO_FLAG_BAD_PAGE = 64
+PRESTO_FLAG_NO_PAGES = 128
+PRESTO_FLAG_BAD_SEQ = 256
 PRESTO_CTX_PACKED = 0
 PRESTO_CTX_SLOTS = 1
 
@@ -46,7 +49,10 @@ EXPORTS = (
     "presto_build_tree",
     "presto_tree_attention_workspace", "presto_tree_attention", "presto_accept_workspace",
     "presto_accept", "presto_topk_rows", "presto_commit_kv", "presto_select_slots",
-    "presto_flatten_slots", "presto_status_string", "presto_last_error", "presto_version",
+    "presto_flatten_slots", "presto_paged_attention_workspace", "presto_paged_attention",
+    "presto_window_attention_workspace", "presto_window_attention", "presto_pages_workspace",
+    "presto_pages_reserve", "presto_append_kv", "presto_pages_fork", "presto_pages_free",
+    "presto_pages_trim", "presto_pages_compact", "presto_status_string", "presto_last_error", "presto_version",
 )
 
 
@@ -72,6 +78,20 @@ class AttnDesc(ctypes.Structure):
 class CommitDesc(ctypes.Structure):
     _fields_ = [("batch", ctypes.c_int32), ("n_max", ctypes.c_int32), ("hkv", ctypes.c_int32),
                 ("head_dim", ctypes.c_int32), ("depth", ctypes.c_int32), ("dt", ctypes.c_int32)]
+
+
+class PagesDesc(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("num_pages", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("hkv", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("dt", ctypes.c_int32), ("layers", ctypes.c_int32), ("page_stride", ctypes.c_int64),
+                ("layer_stride", ctypes.c_int64)]
+
+
+class PagedAttnDesc(ctypes.Structure):
+    _fields_ = [("pages", PagesDesc), ("hq", ctypes.c_int32), ("max_q", ctypes.c_int32),
+                ("max_ctx", ctypes.c_int32), ("window", ctypes.c_int32), ("sinks", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("total_q", ctypes.c_int64), ("q_stride", ctypes.c_int64),
+                ("total_ctx", ctypes.c_int64)]
 
 
 _VP, _I32, _I64, _SZ = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
@@ -124,6 +144,22 @@ def lib() -> ctypes.CDLL:
         L.presto_select_slots.restype = _I32
         L.presto_flatten_slots.argtypes = [_I32, _I32, _I32] + [_VP] * 8
         L.presto_flatten_slots.restype = _I32
+        pages, attn = ctypes.POINTER(PagesDesc), ctypes.POINTER(PagedAttnDesc)
+        for name, desc in (("presto_pages_workspace", pages), ("presto_paged_attention_workspace", attn),
+                           ("presto_window_attention_workspace", attn)):
+            getattr(L, name).argtypes = [desc]
+            getattr(L, name).restype = _SZ
+        for name, args in (
+                ("presto_paged_attention", [attn] + [_VP] * 8 + [_SZ, _VP]),
+                ("presto_window_attention", [attn] + [_VP] * 9 + [_SZ, _VP]),
+                ("presto_pages_reserve", [pages] + [_VP] * 4 + [_I32] + [_VP] * 3 + [_SZ, _VP]),
+                ("presto_append_kv", [pages, _VP, _VP, _I64, _I64, _VP, _I32] + [_VP] * 7),
+                ("presto_pages_fork", [pages] + [_VP] * 5 + [_I32] + [_VP] * 4 + [_SZ, _VP]),
+                ("presto_pages_free", [pages] + [_VP] * 4 + [_I32, _VP, _VP]),
+                ("presto_pages_trim", [pages] + [_VP] * 3 + [_I32, _I32, _VP, _VP]),
+                ("presto_pages_compact", [pages] + [_VP] * 10 + [_SZ, _VP])):
+            getattr(L, name).argtypes = args
+            getattr(L, name).restype = _I32
         L.presto_status_string.argtypes = [_I32]
         L.presto_status_string.restype = ctypes.c_char_p
         L.presto_last_error.restype = ctypes.c_char_p

@@ -1,0 +1,325 @@
+"""Binding of the paged KV cache (include/presto.h): the attention that reads
+it, the append that fills it and the bookkeeping of its pages.
+
+As in ``_lib``: argument marshalling and checks only.  The calls run on the
+device of their tensors, on that device's current stream unless one is given.
+"""
+from __future__ import annotations
+
+import contextlib
+import ctypes
+
+import torch
+
+from ._lib import PagedAttnDesc, PagesDesc, _check, _dt, _ptr, lib
+
+
+def _same(dev, **ts):
+    for name, t in ts.items():
+        if t is not None and (not t.is_cuda or t.device != dev):
+            raise ValueError(f"{name} must be a tensor on {dev}")
+
+
+def _book(dev, **ts):
+    """int32 bookkeeping tensors, contiguous, on one device."""
+    _same(dev, **ts)
+    for name, t in ts.items():
+        if t is not None and (t.dtype != torch.int32 or not t.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous int32 tensor")
+
+
+def _shape(name, t, *shape):
+    if t is not None and tuple(t.shape) != shape:
+        raise ValueError(f"{name} must be of shape {list(shape)}, not {list(t.shape)}")
+
+
+@contextlib.contextmanager
+def _switch(dev):
+    with torch.cuda.device(dev):
+        yield
+
+
+def _on(dev):
+    """Makes `dev` the current device (free when it is already)."""
+    if dev.index is None or dev.index == torch._C._cuda_getDevice():
+        return contextlib.nullcontext()
+    return _switch(dev)
+
+
+def _queue(dev, stream, *made):
+    """The stream's handle; tensors made here for a call on a stream that is
+    not the current one must not be handed out again before it is through."""
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(dev.index)
+    if stream.device != dev:
+        raise ValueError(f"the stream belongs to {stream.device}, the tensors to {dev}")
+    for t in made:
+        if t is not None:
+            t.record_stream(stream)
+    return stream.cuda_stream
+
+
+def _pool(k, v, page_table, batch, layers: bool) -> PagesDesc:
+    """Descriptor of the pools k, v: [pages, page, hkv, dim], or with a leading
+    layer dimension where `layers` allows it."""
+    if k.dim() not in ((4, 5) if layers else (4,)):
+        raise ValueError("the page pools must be [pages, page, hkv, dim]" + (" or with layers first" if layers else ""))
+    if v.shape != k.shape or v.stride() != k.stride() or v.dtype != k.dtype:
+        raise ValueError("k_pages and v_pages must have one shape, stride and type")
+    n, page, hkv, d = k.shape[-4:]
+    if k.stride()[-3:] != (hkv * d, d, 1) and k.numel() > 0:
+        raise ValueError("a page must be contiguous")
+    desc = PagesDesc()
+    desc.batch, desc.max_pages = batch, page_table.shape[1]
+    desc.num_pages, desc.page_size, desc.hkv, desc.head_dim = n, page, hkv, d
+    desc.dt = _dt(k)
+    desc.layers = k.shape[0] if k.dim() == 5 else 1
+    # (the stride of a single page or layer is free: the default)
+    desc.page_stride = k.stride(-4) if n > 1 else 0
+    desc.layer_stride = k.stride(0) if k.dim() == 5 and k.shape[0] > 1 else 0
+    if (n > 1 and desc.page_stride == 0) or (desc.layers > 1 and desc.layer_stride == 0):
+        raise ValueError("pages and layers must not overlap")
+    if k.dim() == 5 and desc.layers > 1:
+        # layers apart, or pages apart and the layers inside a page's stride
+        # would be interleaved: only the former is a layout of the pool
+        if desc.layer_stride < (n - 1) * k.stride(-4) + page * hkv * d:
+            raise ValueError("layers must not overlap")
+    return desc
+
+
+def _books(refs, page_table, page_size) -> PagesDesc:
+    """Descriptor for the calls that look at the books only."""
+    desc = PagesDesc()
+    desc.batch, desc.max_pages = page_table.shape
+    desc.num_pages, desc.page_size = refs.numel(), page_size
+    desc.hkv, desc.head_dim, desc.dt, desc.layers = 1, 64, 0, 1
+    return desc
+
+
+def _rows(name, t, hkv, d):
+    """Token rows [n, heads, dim], any stride between tokens; the stride."""
+    if t.dim() != 3 or tuple(t.shape[1:]) != (hkv, d):
+        raise ValueError(f"{name} must be [tokens, {hkv}, {d}]")
+    if t.numel() > 0 and t.stride()[1:] != (d, 1) and not (hkv == 1 and t.stride(2) == 1):
+        raise ValueError(f"the heads of a token of {name} must be contiguous")
+    return t.stride(0) if t.shape[0] > 1 else 0
+
+
+def _attn_desc(q, k_pages, v_pages, page_table, batch, max_q, max_ctx, scale, window, sinks, total_ctx):
+    if page_table.dim() != 2:
+        raise ValueError("page_table must be [sequences, columns]")
+    _shape("page_table", page_table, batch, page_table.shape[1])
+    desc = PagedAttnDesc()
+    desc.pages = _pool(k_pages, v_pages, page_table, batch, False)
+    if q.dtype != k_pages.dtype:
+        raise TypeError("q and the pages must be of one type")
+    hkv, d = k_pages.shape[2:]
+    desc.hq = q.shape[1]
+    desc.q_stride = _rows("q", q, q.shape[1], d)
+    desc.max_q, desc.total_q = max_q, q.shape[0]
+    desc.max_ctx = page_table.shape[1] * k_pages.shape[1] if max_ctx is None else max_ctx
+    desc.window, desc.sinks, desc.total_ctx = window, sinks, total_ctx
+    desc.scale = d ** -0.5 if scale is None else scale
+    return desc
+
+
+def _attend(who, q, q_offsets, k_pages, v_pages, page_table, ctx, desc, out, flags, workspace, stream):
+    dev = q.device
+    _same(dev, q=q, k_pages=k_pages, v_pages=v_pages, out=out, workspace=workspace)
+    _book(dev, page_table=page_table, ctx=ctx, q_offsets=q_offsets, flags=flags)
+    made = None
+    if out is None:
+        out = made = torch.empty(q.shape, dtype=q.dtype, device=dev)
+    elif out.shape != q.shape or out.dtype != q.dtype or not out.is_contiguous():
+        raise ValueError("out must be a contiguous tensor of q's shape and type")
+    need = getattr(lib(), who + "_workspace")(ctypes.byref(desc))
+    ws, made_ws = workspace, None
+    if need and ws is None:
+        ws = made_ws = torch.empty(need, dtype=torch.uint8, device=dev)
+    nb = 0 if ws is None else ws.numel() * ws.element_size()
+    with _on(dev):
+        st = _queue(dev, stream, made, made_ws)
+        offs = () if q_offsets is None else (_ptr(q_offsets),)
+        _check(getattr(lib(), who)(ctypes.byref(desc), _ptr(q), *offs, _ptr(k_pages), _ptr(v_pages),
+                                   _ptr(page_table), _ptr(ctx), _ptr(out), _ptr(flags), _ptr(ws), nb, st), who)
+    return out
+
+
+def presto_paged_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor,
+                           page_table: torch.Tensor, ctx: torch.Tensor, *, max_ctx: int | None = None,
+                           scale: float | None = None, window: int = 0, sinks: int = 0, total_ctx: int = 0,
+                           out=None, flags=None, workspace=None, stream=None) -> torch.Tensor:
+    """One new token per sequence: q [b, Hq, d] at position ctx[b] - 1 over the
+    cached positions it sees (all up to its own, or with a window the last
+    `window` of them and the first `sinks`)."""
+    b = q.shape[0]
+    desc = _attn_desc(q, k_pages, v_pages, page_table, b, 1, max_ctx, scale, window, sinks, total_ctx)
+    _shape("ctx", ctx, b)
+    return _attend("presto_paged_attention", q, None, k_pages, v_pages, page_table, ctx, desc, out, flags,
+                   workspace, stream)
+
+
+def presto_window_attention(q: torch.Tensor, q_offsets: torch.Tensor, max_q: int, k_pages: torch.Tensor,
+                            v_pages: torch.Tensor, page_table: torch.Tensor, ctx: torch.Tensor, *,
+                            max_ctx: int | None = None, scale: float | None = None, window: int = 0,
+                            sinks: int = 0, total_ctx: int = 0, out=None, flags=None, workspace=None,
+                            stream=None) -> torch.Tensor:
+    """A ragged batch of new tokens: rows q_offsets[b] .. q_offsets[b+1] - 1 of
+    q [total, Hq, d] are the last positions of sequence b, at most max_q."""
+    b = q_offsets.shape[0] - 1
+    desc = _attn_desc(q, k_pages, v_pages, page_table, b, max_q, max_ctx, scale, window, sinks, total_ctx)
+    _shape("ctx", ctx, b)
+    return _attend("presto_window_attention", q, q_offsets, k_pages, v_pages, page_table, ctx, desc, out, flags,
+                   workspace, stream)
+
+
+def paged_attention_workspace(q: torch.Tensor, k_pages: torch.Tensor, page_table: torch.Tensor, *, max_q: int = 1,
+                              max_ctx: int | None = None, window: int = 0, sinks: int = 0,
+                              total_ctx: int = 0) -> torch.Tensor:
+    """A workspace for presto_paged_attention, and for presto_window_attention
+    with up to max_q new tokens per sequence."""
+    desc = _attn_desc(q, k_pages, k_pages, page_table, page_table.shape[0], max_q, max_ctx, None, window, sinks,
+                      total_ctx)
+    need = max(lib().presto_window_attention_workspace(ctypes.byref(desc)),
+               lib().presto_paged_attention_workspace(ctypes.byref(desc)), 16)
+    return torch.empty(need, dtype=torch.uint8, device=q.device)
+
+
+def _pages_call(who, dev, desc, args, flags, workspace, stream, made=()):
+    """args: the call's pointers up to flags."""
+    need = lib().presto_pages_workspace(ctypes.byref(desc))
+    _same(dev, workspace=workspace)
+    ws, made_ws = workspace, None
+    if ws is None:
+        ws = made_ws = torch.empty(max(need, 16), dtype=torch.uint8, device=dev)
+    with _on(dev):
+        st = _queue(dev, stream, made_ws, *made)
+        _check(getattr(lib(), who)(ctypes.byref(desc), *args, _ptr(flags), _ptr(ws),
+                                   ws.numel() * ws.element_size(), st), who)
+
+
+def pages_workspace(refs: torch.Tensor, page_table: torch.Tensor) -> torch.Tensor:
+    """A workspace for every presto_pages_* call on these books."""
+    need = lib().presto_pages_workspace(ctypes.byref(_books(refs, page_table, 16)))
+    return torch.empty(max(need, 16), dtype=torch.uint8, device=refs.device)
+
+
+def _check_books(refs, page_table, ctx, **more):
+    if page_table.dim() != 2 or refs.dim() != 1:
+        raise ValueError("page_table must be [sequences, columns] and refs [pages]")
+    _book(refs.device, refs=refs, page_table=page_table, ctx=ctx, **more)
+    _shape("ctx", ctx, page_table.shape[0])
+
+
+def presto_pages_reserve(refs: torch.Tensor, page_table: torch.Tensor, ctx: torch.Tensor, page_size: int,
+                         add: torch.Tensor | None = None, extra: int = 0, *, out=None, flags=None, workspace=None,
+                         stream=None) -> torch.Tensor:
+    """Gives pages to the positions ctx .. ctx + add + extra - 1 and returns the
+    new lengths (in `out`, which may be ctx); refs and page_table are updated
+    in place.  A sequence the pool has no pages for keeps its length."""
+    _check_books(refs, page_table, ctx, add=add, out=out, flags=flags)
+    b = page_table.shape[0]
+    _shape("add", add, b)
+    _shape("out", out, b)
+    made = None
+    if out is None:
+        out = made = torch.empty_like(ctx)
+    _pages_call("presto_pages_reserve", refs.device, _books(refs, page_table, page_size),
+                (_ptr(refs), _ptr(page_table), _ptr(ctx), _ptr(add), extra, _ptr(out)), flags, workspace, stream,
+                (made,))
+    return out
+
+
+def presto_append_kv(k_new: torch.Tensor, v_new: torch.Tensor, offsets: torch.Tensor, max_new: int,
+                     k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor, ctx: torch.Tensor,
+                     ctx_new: torch.Tensor, *, flags=None, stream=None) -> None:
+    """Writes rows offsets[b] + i of k_new, v_new [rows, Hkv, d] to positions
+    ctx[b] + i < ctx_new[b] of the cache, at most max_new per sequence."""
+    dev = k_new.device
+    b = offsets.shape[0] - 1
+    _same(dev, k_new=k_new, v_new=v_new, k_pages=k_pages, v_pages=v_pages)
+    _book(dev, offsets=offsets, page_table=page_table, ctx=ctx, ctx_new=ctx_new, flags=flags)
+    _shape("page_table", page_table, b, page_table.shape[-1])
+    _shape("ctx", ctx, b)
+    _shape("ctx_new", ctx_new, b)
+    desc = _pool(k_pages, v_pages, page_table, b, False)
+    if k_new.dtype != k_pages.dtype or v_new.dtype != k_pages.dtype:
+        raise TypeError("the new rows and the pages must be of one type")
+    stride = _rows("k_new", k_new, *k_pages.shape[2:])
+    if v_new.shape != k_new.shape or _rows("v_new", v_new, *k_pages.shape[2:]) != stride:
+        raise ValueError("k_new and v_new must have one shape and stride")
+    with _on(dev):
+        st = _queue(dev, stream)
+        _check(lib().presto_append_kv(ctypes.byref(desc), _ptr(k_new), _ptr(v_new), k_new.shape[0], stride,
+                                      _ptr(offsets), max_new, _ptr(k_pages), _ptr(v_pages), _ptr(page_table),
+                                      _ptr(ctx), _ptr(ctx_new), _ptr(flags), st), "presto_append_kv")
+
+
+def presto_pages_fork(refs: torch.Tensor, page_table: torch.Tensor, ctx: torch.Tensor, parent: torch.Tensor,
+                      child: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, *, flags=None,
+                      workspace=None, stream=None) -> None:
+    """Sequence child[i] (empty) becomes a copy of parent[i]: full pages shared,
+    the rows of the last one copied in all layers of k_pages, v_pages
+    [layers, pages, page, Hkv, d] (or of one layer, without that dimension)."""
+    _check_books(refs, page_table, ctx, parent=parent, child=child, flags=flags)
+    _same(refs.device, k_pages=k_pages, v_pages=v_pages)
+    n = parent.numel()
+    _shape("parent", parent, n)
+    _shape("child", child, n)
+    desc = _pool(k_pages, v_pages, page_table, page_table.shape[0], True)
+    _shape("refs", refs, desc.num_pages)
+    _pages_call("presto_pages_fork", refs.device, desc,
+                (_ptr(refs), _ptr(page_table), _ptr(ctx), _ptr(parent), _ptr(child), n, _ptr(k_pages),
+                 _ptr(v_pages)), flags, workspace, stream)
+
+
+def presto_pages_free(refs: torch.Tensor, page_table: torch.Tensor, ctx: torch.Tensor, rows: torch.Tensor, *,
+                      flags=None, stream=None) -> None:
+    """Drops the sequences `rows`: their references go, their lengths are 0."""
+    _check_books(refs, page_table, ctx, rows=rows, flags=flags)
+    _shape("rows", rows, rows.numel())
+    desc = _books(refs, page_table, 16)
+    with _on(refs.device):
+        st = _queue(refs.device, stream)
+        _check(lib().presto_pages_free(ctypes.byref(desc), _ptr(refs), _ptr(page_table), _ptr(ctx), _ptr(rows),
+                                       rows.numel(), _ptr(flags), st), "presto_pages_free")
+
+
+def presto_pages_trim(refs: torch.Tensor, page_table: torch.Tensor, ctx: torch.Tensor, page_size: int, window: int,
+                      sinks: int = 0, *, flags=None, stream=None) -> None:
+    """Drops the pages that no query from position ctx - 1 on sees under the
+    window and sinks."""
+    _check_books(refs, page_table, ctx, flags=flags)
+    desc = _books(refs, page_table, page_size)
+    with _on(refs.device):
+        st = _queue(refs.device, stream)
+        _check(lib().presto_pages_trim(ctypes.byref(desc), _ptr(refs), _ptr(page_table), _ptr(ctx), window, sinks,
+                                       _ptr(flags), st), "presto_pages_trim")
+
+
+def presto_pages_compact(refs: torch.Tensor, page_table: torch.Tensor, k_pages: torch.Tensor,
+                         v_pages: torch.Tensor, *, out=None, flags=None, workspace=None, stream=None) -> dict:
+    """Moves the live pages to the front of the pool, in all layers.  Returns
+    the books afterwards: refs, page_table, n_live [1] (or fills those of
+    `out`, where refs and page_table may be the arguments themselves, and
+    page_map [pages], each live page's new number, if it is there)."""
+    _check_books(refs, page_table, None, flags=flags)
+    dev = refs.device
+    _same(dev, k_pages=k_pages, v_pages=v_pages)
+    made = ()
+    if out is None:
+        out = {"refs": torch.empty_like(refs), "page_table": torch.empty_like(page_table),
+               "n_live": torch.empty(1, dtype=torch.int32, device=dev)}
+        made = tuple(out.values())
+    page_map = out.get("page_map")
+    _book(dev, out_refs=out["refs"], out_page_table=out["page_table"], n_live=out["n_live"], page_map=page_map)
+    desc = _pool(k_pages, v_pages, page_table, page_table.shape[0], True)
+    _shape("refs", refs, desc.num_pages)
+    _shape("out refs", out["refs"], desc.num_pages)
+    _shape("out page_table", out["page_table"], *page_table.shape)
+    _shape("n_live", out["n_live"], 1)
+    _shape("page_map", page_map, desc.num_pages)
+    _pages_call("presto_pages_compact", dev, desc,
+                (_ptr(refs), _ptr(out["refs"]), _ptr(page_table), _ptr(out["page_table"]), _ptr(out["n_live"]),
+                 _ptr(page_map), _ptr(k_pages), _ptr(v_pages)), flags, workspace, stream, made)
+    return out

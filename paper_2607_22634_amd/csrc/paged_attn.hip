@@ -529,6 +529,426 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void paged_attn_rows_kernel(Args
     }
 }
 
+// Many query rows per KV head (bf16): tiles of 64 keys go from memory straight
+// into LDS (a ring of four: one consumed, one resident, two in flight), where
+// eight waves of 32 rows each read them, so that a key is fetched once for 256
+// rows.  32x32x16 instructions, S^T = K Q^T and O^T = V^T P^T as above; a lane
+// holds one row and 16 of a block's 32 keys, and the probabilities are the
+// second product's operand as they are.  K rows lie in LDS with their 16-byte
+// chunks permuted by chunk ^ (row mod 16), V rows by chunk ^ 4 (row mod 4), so
+// that neither the b128 reads of K nor the transposed reads of V meet bank
+// conflicts.
+//
+// Three blocks of 32 keys are in work per wave: a step issues the P V products
+// of block i, the exponentials of block i + 1 and the scores of block i + 2
+// between one another.  Scores start from -m, so that a probability is
+// exp2(c S); the reference m moves only where a block's sum exceeds 2^8 or a
+// row has no mass yet.
+//
+// The page numbers of the workgroup's keys are looked up once and kept in LDS:
+// eight rows of a tile, one wave's share of its loads, lie in one page.
+typedef float floatx16 __attribute__((ext_vector_type(16)));
+typedef short shortx4 __attribute__((ext_vector_type(4)));
+
+constexpr int kKeyTile = 64;
+constexpr int kRing = 4;
+constexpr int kTileWaves = 8;
+constexpr int kTileRows = kTileWaves * 32;
+constexpr int kTilePages = 4096;  // page numbers in LDS
+
+// 16 bytes per lane from memory to LDS: lane l's land at lds + 16 l.  In inline
+// assembly, because the compiler would put a wait for all loads before every
+// later LDS read; the kernel waits for each tile itself.
+__device__ __forceinline__ void lds_load16(const void* lane_ptr, uint32_t lds) {
+    const uint32_t m0v = (uint32_t)__builtin_amdgcn_readfirstlane(lds);
+    asm volatile("global_load_lds_dwordx4 %0, off" ::"v"(lane_ptr), "{m0}"(m0v) : "memory");
+}
+// the same with a wave-uniform base and a 32-bit offset per lane
+__device__ __forceinline__ void lds_load16(const void* base, uint32_t off, uint32_t lds) {
+    const uint64_t b = (uint64_t)(uintptr_t)base;
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)b);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(b >> 32));
+    const uint64_t sb = ((uint64_t)hi << 32) | (uint64_t)lo;
+    const uint32_t m0v = (uint32_t)__builtin_amdgcn_readfirstlane(lds);
+    asm volatile("global_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(sb), "{m0}"(m0v) : "memory");
+}
+
+template <int D>
+__global__ __launch_bounds__(kTileWaves * kWave) void paged_attn_tiles_kernel(Args a) {
+    constexpr int T = kKeyTile;
+    constexpr int KS = D / 16;                // contraction steps of a score block
+    constexpr int DB = D / 32;                // 32-dim blocks of the output
+    constexpr int CH = D / 8;                 // 16-byte chunks per row
+    constexpr int NT = kTileWaves * kWave;
+    constexpr int RPL = 64 / CH;              // key rows per load instruction
+    constexpr int LPT = T / RPL / kTileWaves; // loads per thread and tile, K and V each
+    constexpr int kTile = T * D * 2;          // bytes of a K or V tile
+    constexpr int kV = kRing * kTile;         // K tiles first, then V tiles
+    static_assert(LPT * RPL == 8, "a wave loads eight rows of a tile");
+    __shared__ __align__(16) char s_kv[2 * kRing * kTile];
+    __shared__ int32_t s_page[kTilePages];
+    __shared__ int s_bad[kTileRows];
+
+    int id = blockIdx.x;
+    const int g = id % a.hkv;
+    id /= a.hkv;
+    const int split = id % a.splits;
+    id /= a.splits;
+    const int b = id % a.batch;
+    const int rev = id / a.batch;
+    const Seq sq = seq_of(a, b);
+    const int rows = sq.n * a.G;
+    const int rb = (rows + kTileRows - 1) / kTileRows - 1 - rev;
+    const int tid = threadIdx.x, lane = lane_id();
+    const int wave = uniform(tid / kWave);
+    if (rev == 0 && g == 0 && split == 0 && tid == 0 && sq.bad) raise_flag(a.flags, PRESTO_FLAG_BAD_SEQ);
+    if (rb < 0) return;
+    const int row0 = rb * kTileRows;
+    const int row_end = min(row0 + kTileRows, rows);
+    const Span sp = span_of<T>(a, sq.pos0 + row0 / a.G, sq.pos0 + (row_end - 1) / a.G);
+    const int t_begin = split * a.split_tiles, t_end = min(t_begin + a.split_tiles, sp.tiles);
+    if (split > 0 && t_begin >= t_end) return;  // the merge knows
+    const int64_t bg = (int64_t)b * a.hkv + g, all = (int64_t)a.G * a.max_q;
+
+    // ---- page numbers: those of the sink tiles' keys, then of the others
+    auto key_of = [&](int t) { return t < sp.sink_tiles ? t * T : sp.start + (t - sp.sink_tiles) * T; };
+    const int ka = t_begin * T, ka_end = min(sp.sink, t_end * T);
+    const int kb = key_of(max(t_begin, sp.sink_tiles)), kb_end = min(sp.hi, sp.start + (t_end - sp.sink_tiles) * T);
+    const int pa = ka < ka_end ? ka >> a.page_shift : 0;
+    const int na = ka < ka_end ? ((ka_end - 1) >> a.page_shift) - pa + 1 : 0;
+    const int pb = kb >> a.page_shift;
+    const int nb = kb < kb_end ? ((kb_end - 1) >> a.page_shift) - pb + 1 : 0;
+    {
+        bool bad = na + nb > kTilePages;  // (the host's choice of splits rules it out)
+        const int32_t* trow = a.table + (int64_t)b * a.max_pages;
+        for (int i = tid; i < min(na + nb, kTilePages); i += NT) {
+            const int x = i < na ? pa + i : pb + i - na;
+            const int k0 = max(x << a.page_shift, kb), k1 = min((x + 1) << a.page_shift, kb_end);
+            const bool wanted = i < na || k1 > sp.lo || k0 < a.sinks;
+            const int page = wanted ? trow[x] : 0;
+            const bool ok = (uint32_t)page < (uint32_t)a.num_pages;
+            bad |= !ok;
+            s_page[i] = ok ? page : 0;
+        }
+        if (tid < kTileRows) s_bad[tid] = 0;
+        if (__syncthreads_or(bad)) {
+            // a page that is not there: its keys are left out, row by row
+            if (tid == 0) raise_flag(a.flags, PRESTO_FLAG_BAD_PAGE);
+            if (tid < row_end - row0) s_bad[tid] = 1;
+        }
+    }
+    __syncthreads();
+    const bool skip = s_bad[0] != 0;
+
+    const int l32 = lane & 31, h = lane >> 5;
+    const int wrow0 = row0 + wave * 32;  // this wave's first row
+    const bool active = wrow0 < rows && !skip && t_begin < t_end;
+    const int rho = wrow0 + l32;
+    const int rq = min(rho, rows - 1);
+    const int tok = rq / a.G, qh = rq - tok * a.G;
+    const int pos = sq.pos0 + tok;
+    const int p_lo = uniform(sq.pos0 + min(wrow0, rows - 1) / a.G);
+    const int p_hi = uniform(sq.pos0 + min(wrow0 + 31, rows - 1) / a.G);
+    const float c = a.scale_log2;
+
+    floatx16 o[DB];
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[db][i] = 0.f;
+    float m = 0.f, l_run = 0.f;  // reference (score units) and sum of the row
+
+    if (!skip && t_begin < t_end) {
+        // queries, second operand of S^T: row l32, dims ks * 16 + h * 8 ..
+        bf16x8 qf[KS];
+        {
+            const char* qp = a.q + ((sq.r0 + tok) * a.q_stride + (int64_t)(g * a.G + qh) * D + h * 8) * 2;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks)
+                qf[ks] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(qp + ks * 32));
+        }
+        // ---- loads: instruction j of this wave covers rows 8 wave + RPL j ..
+        // of a tile; lane l writes chunk l % CH of row l / CH and fetches the
+        // chunk that the row's permutation puts there
+        uint32_t goff_k[LPT], goff_v[LPT];
+        int lrow[LPT], lck[LPT], lcv[LPT];
+#pragma unroll
+        for (int j = 0; j < LPT; ++j) {
+            const int r = 8 * wave + RPL * j + lane / CH, pc = lane % CH;
+            lrow[j] = r;
+            lck[j] = pc ^ (r & (CH - 1) & 15);
+            lcv[j] = pc ^ ((4 * (r & 3)) & (CH - 1));
+            goff_k[j] = (uint32_t)(((r - 8 * wave) * a.hkv * D + lck[j] * 8) * 2);
+            goff_v[j] = (uint32_t)(((r - 8 * wave) * a.hkv * D + lcv[j] * 8) * 2);
+        }
+        const uint32_t lds_kv = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)s_kv;
+        const int pmask = (1 << a.page_shift) - 1;
+        auto page_of = [&](bool sink, int key) __attribute__((always_inline)) {
+            return s_page[sink ? (key >> a.page_shift) - pa : na + (key >> a.page_shift) - pb];
+        };
+        const int k_last = min(key_of(t_end - 1) + T, t_end - 1 < sp.sink_tiles ? sp.sink : sp.hi) - 1;
+        auto load_tile = [&](int t, int buf) __attribute__((always_inline)) {
+            const uint32_t kdst = lds_kv + buf * kTile + wave * LPT * 1024;
+            const uint32_t vdst = kdst + kV;
+            const bool sink = t < sp.sink_tiles;
+            const int key0 = key_of(t);
+            if (t < t_end && (sink ? key0 + T <= sp.sink
+                                   : key0 + T <= sp.hi && (key0 >= sp.lo || key0 + T <= a.sinks))) {
+                const int kw = key0 + 8 * wave;
+                const int64_t at = uniform(page_of(sink, kw)) * a.page_stride + ((int64_t)(kw & pmask) * a.hkv + g) * D;
+#pragma unroll
+                for (int j = 0; j < LPT; ++j) {
+                    lds_load16(a.kp + at * 2, goff_k[j], kdst + j * 1024);
+                    lds_load16(a.vp + at * 2, goff_v[j], vdst + j * 1024);
+                }
+            } else {
+                // rows that no query of the workgroup sees repeat one that
+                // some query does (nothing but what is seen is read)
+                const bool last_sink = t_end - 1 < sp.sink_tiles;
+#pragma unroll
+                for (int j = 0; j < LPT; ++j) {
+                    int key = key0 + lrow[j];
+                    bool in_sink = sink;
+                    if (t >= t_end) {
+                        key = k_last;
+                        in_sink = last_sink;
+                    } else if (sink) {
+                        key = min(key, sp.sink - 1);
+                    } else {
+                        if (key < sp.lo && key >= a.sinks) key = key0 < a.sinks ? a.sinks - 1 : sp.lo;
+                        key = min(key, sp.hi - 1);
+                    }
+                    const int64_t at = page_of(in_sink, key) * a.page_stride + ((int64_t)(key & pmask) * a.hkv + g) * D;
+                    lds_load16(a.kp + (at + lck[j] * 8) * 2, kdst + j * 1024);
+                    lds_load16(a.vp + (at + lcv[j] * 8) * 2, vdst + j * 1024);
+                }
+            }
+        };
+        // vmcnt(n) with the other counters left alone
+#define PRESTO_WAIT_VM(n) __builtin_amdgcn_s_waitcnt(((n) & 15) | (((n) >> 4) << 14) | 0x0f70)
+
+        const int ntiles = t_end - t_begin;
+        // (the last window tile may end in its first half)
+        const int nblocks = 2 * ntiles - (t_end > sp.sink_tiles && key_of(t_end - 1) + 32 >= sp.hi ? 1 : 0);
+
+        // per-lane LDS addresses of the fragment reads (ring slot 0, block 0)
+        const int vr = 4 * h + ((lane & 15) >> 2);
+        const int vc = ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
+        uint32_t kaddr[KS], vaddr[DB];
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+            kaddr[ks] = (l32 * (D * 2) + ((h ^ (l32 & 15)) & (CH - 1)) * 16) ^ (ks << 5);
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+            vaddr[db] = kV + ((vr * (D * 2) + ((4 * (vr & 3) + vc) & (CH - 1)) * 16 + (lane & 1) * 8) ^ (db << 6));
+
+        const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
+        floatx16 negm;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) negm[e] = 0.f;
+        typedef __attribute__((address_space(3))) shortx4* lds_s4;
+
+        auto half_swap = [&](float v) __attribute__((always_inline)) {
+            const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+            return __uint_as_float(h == 0 ? sw[1] : sw[0]);
+        };
+        auto row_max = [&](const floatx16& S) __attribute__((always_inline)) {
+            float mx = S[0];
+#pragma unroll
+            for (int e = 1; e < 16; ++e) mx = fmaxf(mx, S[e]);
+            return fmaxf(mx, half_swap(mx));
+        };
+        auto row_sum = [&](float v) __attribute__((always_inline)) { return v + half_swap(v); };
+        // first key and key limit of block i
+        auto j0_of = [&](int i) { return key_of(t_begin + (i >> 1)) + 32 * (i & 1); };
+        auto lim_of = [&](int i) { return t_begin + (i >> 1) < sp.sink_tiles ? sp.sink : sp.hi; };
+        auto masked = [&](int i) __attribute__((always_inline)) {
+            const int j0 = j0_of(i);
+            return j0 + 32 > min(lim_of(i), p_lo + 1) || (a.window > 0 && j0 <= p_hi - a.window && j0 + 32 > a.sinks);
+        };
+        // the block's 32 keys as bits, then a test and a select per element
+        auto apply_mask = [&](floatx16& S, int i) __attribute__((always_inline)) {
+            const int j0 = j0_of(i);
+            auto below = [](int n) { return n >= 32 ? ~0u : (n <= 0 ? 0u : (1u << n) - 1u); };
+            uint32_t vis = below(min(lim_of(i), pos + 1) - j0);
+            if (a.window > 0) vis &= ~below(pos - a.window + 1 - j0) | below(a.sinks - j0);
+            vis >>= 4 * h;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) S[e] = (vis >> (8 * (e >> 2) + (e & 3))) & 1u ? S[e] : -INFINITY;
+        };
+        auto qk = [&](auto bufc, int blk, floatx16& Sx) __attribute__((always_inline)) {
+            constexpr int buf = decltype(bufc)::value;
+#pragma unroll
+            for (int ks = 0; ks < KS; ++ks) {
+                const uint4 u = *reinterpret_cast<const uint4*>(s_kv + kaddr[ks] + buf * kTile + blk * 32 * D * 2);
+                Sx = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, u), qf[ks],
+                                                             ks == 0 ? negm : Sx, 0, 0, 0);
+            }
+        };
+        // two probabilities, rounded to the product's bf16; the sum takes the
+        // rounded values
+        auto pair = [&](const floatx16& S, int e, float& ls) __attribute__((always_inline)) {
+            const uint32_t w = pack2(__builtin_amdgcn_exp2f(S[e] * c), __builtin_amdgcn_exp2f(S[e + 1] * c));
+            ls = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w), ones, ls, false);
+            return w;
+        };
+        // moves m to the block's maximum in the rows that need it and takes the
+        // block's probabilities again (Sy: a block scored against the old m)
+        auto exact = [&](floatx16& Sx, uint32_t(&Px)[8], float& ls, bool need, floatx16& Sy) __attribute__((always_inline)) {
+            const float mx = row_max(Sx);
+            const float delta = need && mx != -INFINITY ? mx : 0.f;
+            const float alpha = l_run > 0.f ? __builtin_amdgcn_exp2f(-delta * c) : 0.f;
+            m += delta;
+            l_run *= alpha;
+#pragma unroll
+            for (int db = 0; db < DB; ++db) o[db] *= alpha;
+            ls = 0.f;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                Sx[e] -= delta;
+                Sy[e] -= delta;
+                negm[e] = -m;
+            }
+#pragma unroll
+            for (int e = 0; e < 16; e += 2) Px[e >> 1] = pair(Sx, e, ls);
+            ls = row_sum(ls);
+        };
+
+        constexpr int EPK = 16 / KS;  // exponentials per score instruction
+        static_assert(EPK * KS == 16 && EPK % 2 == 0 && KS == 2 * DB, "head_dim 64 or 128");
+        floatx16 Sa = negm, Sb = negm;  // scores of blocks i + 1 and i + 2
+        uint32_t Pp[8];                 // probabilities of block i
+        auto step = [&](auto bvc, auto bkc, int i, int q) __attribute__((always_inline)) {
+            constexpr int bv = decltype(bvc)::value, bk = decltype(bkc)::value;
+            const bool more = i + 1 < nblocks;
+            if (more && masked(i + 1)) apply_mask(Sa, i + 1);
+            uint32_t Pn[8];
+            float ls = 0.f;
+#pragma unroll
+            for (int st = 0; st < 2; ++st) {
+                const bf16x8 pv =
+                    __builtin_bit_cast(bf16x8, make_uint4(Pp[4 * st], Pp[4 * st + 1], Pp[4 * st + 2], Pp[4 * st + 3]));
+#pragma unroll
+                for (int db = 0; db < DB; ++db) {
+                    const uint32_t v0 = vaddr[db] + bv * kTile + q * 32 * D * 2 + st * 16 * D * 2;
+                    const shortx4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(s_kv + v0));
+                    const shortx4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(s_kv + v0 + 8 * D * 2));
+                    const uint2 ul = __builtin_bit_cast(uint2, lo), uh = __builtin_bit_cast(uint2, hi);
+                    o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                        __builtin_bit_cast(bf16x8, make_uint4(ul.x, ul.y, uh.x, uh.y)), pv, o[db], 0, 0, 0);
+                    const int ks = st * DB + db;
+                    const uint4 u = *reinterpret_cast<const uint4*>(s_kv + kaddr[ks] + bk * kTile + q * 32 * D * 2);
+                    Sb = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, u), qf[ks],
+                                                                 ks == 0 ? negm : Sb, 0, 0, 0);
+#pragma unroll
+                    for (int e = ks * EPK; e < ks * EPK + EPK; e += 2) Pn[e >> 1] = pair(Sa, e, ls);
+                }
+            }
+            if (more) {
+                ls = row_sum(ls);
+                const bool need = !(ls <= 256.f) || l_run + ls == 0.f;
+                if (__ballot(need)) exact(Sa, Pn, ls, need, Sb);
+                l_run += ls;
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) Pp[j] = Pn[j];
+            Sa = Sb;
+        };
+        // one tile: its two blocks, the load of tile t + 3 into the slot that
+        // every wave left before the last barrier, the wait for tile t + 2
+        auto tile = [&](auto uc, int t) __attribute__((always_inline)) {
+            constexpr int u = decltype(uc)::value;
+            using BV = std::integral_constant<int, u>;
+            using BK = std::integral_constant<int, (u + 1) % kRing>;
+            load_tile(t_begin + t + 3, (u + 3) % kRing);
+            if (active) {
+                step(BV{}, BK{}, 2 * t, 0);
+                if (2 * t + 1 < nblocks) step(BV{}, BK{}, 2 * t + 1, 1);
+            }
+            PRESTO_WAIT_VM(2 * LPT);
+            __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): this wave's LDS reads are done
+            __builtin_amdgcn_s_barrier();
+        };
+        load_tile(t_begin, 0);
+        load_tile(t_begin + 1, 1);
+        load_tile(t_begin + 2, 2);
+        PRESTO_WAIT_VM(2 * LPT);  // (the queries too: they were asked for first)
+        __syncthreads();
+        if (active) {
+            using B0 = std::integral_constant<int, 0>;
+            floatx16 S0 = negm;
+            qk(B0{}, 0, S0);
+            if (masked(0)) apply_mask(S0, 0);
+            float ls;
+            exact(S0, Pp, ls, true, Sb);
+            l_run = ls;
+            qk(B0{}, 1, Sa);
+        }
+        for (int t = 0; t < ntiles; t += kRing) {
+            tile(std::integral_constant<int, 0>{}, t);
+            if (t + 1 < ntiles) tile(std::integral_constant<int, 1>{}, t + 1);
+            if (t + 2 < ntiles) tile(std::integral_constant<int, 2>{}, t + 2);
+            if (t + 3 < ntiles) tile(std::integral_constant<int, 3>{}, t + 3);
+        }
+        PRESTO_WAIT_VM(0);  // no load into LDS outlives its buffer
+#undef PRESTO_WAIT_VM
+    }
+
+    // ---- lane: row rho, dims db * 32 + 8 q4 + 4 h + 0 .. 3
+    auto out_row = [&](int r) {
+        const int tk = r / a.G;
+        return reinterpret_cast<uint16_t*>(a.out) + ((sq.r0 + tk) * a.hq + g * a.G + r - tk * a.G) * D;
+    };
+    auto part_row = [&](int r) { return a.part_o + ((bg * a.splits + split) * all + r) * D; };
+    if (rho < rows && !skip) {
+        const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
+        bool fine = true;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                o[db][e] *= inv;
+                fine &= fabsf(o[db][e]) < INFINITY;
+            }
+        if (!fine) s_bad[rho - row0] = 1;
+        if (a.splits == 1) {
+            uint16_t* op = out_row(rho);
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int q4 = 0; q4 < 4; ++q4)
+                    *reinterpret_cast<uint2*>(op + db * 32 + 8 * q4 + 4 * h) =
+                        make_uint2(pack2(o[db][4 * q4], o[db][4 * q4 + 1]), pack2(o[db][4 * q4 + 2], o[db][4 * q4 + 3]));
+        } else {
+            float* op = part_row(rho);
+#pragma unroll
+            for (int db = 0; db < DB; ++db)
+#pragma unroll
+                for (int q4 = 0; q4 < 4; ++q4)
+                    *reinterpret_cast<floatx4*>(op + db * 32 + 8 * q4 + 4 * h) =
+                        (floatx4){o[db][4 * q4], o[db][4 * q4 + 1], o[db][4 * q4 + 2], o[db][4 * q4 + 3]};
+            if (h == 0) a.part_ml[(bg * all + rho) * a.splits + split] = make_float2(l_run == 0.f ? -INFINITY : m * c, l_run);
+        }
+    }
+    // ---- rows whose sums are not all finite: a key that only others see may
+    // be the cause
+    __syncthreads();
+    float* const f = reinterpret_cast<float*>(s_kv);
+    for (int r = 0; r < row_end - row0; ++r) {
+        if (!s_bad[r]) continue;
+        const int rr = row0 + r, tk = rr / a.G;
+        const float2 ml = row_alone<true, D, T>(a, sp, b, g, sq.r0 + tk, g * a.G + rr - tk * a.G, sq.pos0 + tk, t_begin,
+                                                t_end, f + D, f + 2 * D, f + 2 * D + NT, f);
+        for (int d = tid; d < D / 2; d += NT) {
+            if (a.splits == 1)
+                *reinterpret_cast<uint32_t*>(out_row(rr) + 2 * d) = pack2(f[2 * d], f[2 * d + 1]);
+            else
+                *reinterpret_cast<float2*>(part_row(rr) + 2 * d) = make_float2(f[2 * d], f[2 * d + 1]);
+        }
+        if (tid == 0 && a.splits > 1) a.part_ml[(bg * all + rr) * a.splits + split] = ml;
+    }
+}
+
 // Joins the splits of a row: D / 4 lanes per row.  Splits past a sequence's
 // keys have written nothing.
 template <bool BF16, int D, int T>
@@ -597,7 +1017,8 @@ using namespace presto::paged;
 namespace {
 
 struct PagedPlan {
-    int nb;          // 16-row blocks per workgroup
+    bool tiles;      // the kernel of 256-row workgroups
+    int nb;          // else: 16-row blocks per workgroup
     int rows_per_block, row_blocks, splits, split_tiles;
     int64_t blocks;
     size_t o_bytes, bytes;
@@ -610,9 +1031,10 @@ PagedPlan paged_plan(const presto_paged_attn_desc* d) {
     const bool bf16 = d->pages.dt == PRESTO_DT_BF16;
     const int G = d->hq / d->pages.hkv;
     const int64_t rows = (int64_t)G * d->max_q;
-    const int T = bf16 ? 32 : 16;
+    p.tiles = bf16 && d->max_q > 1 && rows > 32;
+    const int T = p.tiles ? kKeyTile : bf16 ? 32 : 16;
     p.nb = rows > 16 ? 2 : 1;
-    p.rows_per_block = 16 * p.nb;
+    p.rows_per_block = p.tiles ? kTileRows : 16 * p.nb;
     p.row_blocks = (int)cdiv(rows, p.rows_per_block);
     // keys of one row block: all of the context, or the sinks and the window
     // of its first to its last row
@@ -624,11 +1046,22 @@ PagedPlan paged_plan(const presto_paged_attn_desc* d) {
     const int64_t all = (int64_t)d->pages.batch * d->pages.hkv * p.row_blocks;
     int64_t mean = longest;
     if (d->total_ctx > 0 && d->total_ctx / d->pages.batch < mean) mean = d->total_ctx / d->pages.batch + 1;
-    const int64_t tiles = cdiv(longest, T);
-    // enough workgroups to fill the chip twice, of at least one tile per wave
-    int64_t per = cdiv(all * cdiv(mean, T), 1536);
-    per = cdiv(per, kWaves) * kWaves;
-    if (per >= tiles) per = tiles;
+    // (a span's first and last tile may be partly filled)
+    const int64_t tiles = cdiv(longest, T) + (d->window > 0 ? 2 : 0);
+    int64_t per;
+    if (p.tiles) {
+        // one workgroup per CU: split only where the rows leave CUs idle, at
+        // 512 keys or more each
+        per = cdiv(tiles * all, 256);
+        if (per < 8) per = 8;
+        const int64_t most = (int64_t)(kTilePages - 8) * d->pages.page_size / T;  // the page numbers fit in LDS
+        if (all >= 192) per = tiles;
+        if (per > most) per = most;
+    } else {
+        // enough workgroups to fill the chip twice, of at least one tile per wave
+        per = cdiv(cdiv(all * cdiv(mean, T), 1536), kWaves) * kWaves;
+    }
+    if (per > tiles) per = tiles;
     p.splits = (int)cdiv(tiles, per);
     p.split_tiles = (int)per;
     p.blocks = all * p.splits;
@@ -641,16 +1074,22 @@ PagedPlan paged_plan(const presto_paged_attn_desc* d) {
 }
 
 template <bool BF16, int D>
-void launch_rows(const PagedPlan& p, const Args& a, hipStream_t stream) {
-    if (p.nb == 1)
+void launch_attn(const PagedPlan& p, const Args& a, hipStream_t stream) {
+    if (p.tiles) {
+        if constexpr (BF16)
+            paged_attn_tiles_kernel<D><<<(unsigned)p.blocks, kTileWaves * kWave, 0, stream>>>(a);
+    } else if (p.nb == 1) {
         paged_attn_rows_kernel<BF16, D, 1><<<(unsigned)p.blocks, kWaves * kWave, 0, stream>>>(a);
-    else
+    } else {
         paged_attn_rows_kernel<BF16, D, 2><<<(unsigned)p.blocks, kWaves * kWave, 0, stream>>>(a);
+    }
     if (p.splits > 1) {
         constexpr int T = BF16 ? 32 : 16;
-        const int64_t rows = (int64_t)a.batch * a.max_q * a.hq;
-        paged_attn_merge_kernel<BF16, D, T>
-            <<<(unsigned)cdiv(rows, 256 / (D / 4)), 256, 0, stream>>>(a, p.rows_per_block);
+        const unsigned grid = (unsigned)cdiv((int64_t)a.batch * a.max_q * a.hq, 256 / (D / 4));
+        if (p.tiles)
+            paged_attn_merge_kernel<BF16, D, kKeyTile><<<grid, 256, 0, stream>>>(a, p.rows_per_block);
+        else
+            paged_attn_merge_kernel<BF16, D, T><<<grid, 256, 0, stream>>>(a, p.rows_per_block);
     }
 }
 
@@ -700,10 +1139,10 @@ presto_status launch_paged_attn(const presto_paged_attn_desc* d, const void* q, 
     a.scale_log2 = d->scale * kLog2e;
     const bool bf16 = d->pages.dt == PRESTO_DT_BF16;
     if (d->pages.head_dim == 128)
-        bf16 ? launch_rows<true, 128>(p, a, stream) : launch_rows<false, 128>(p, a, stream);
+        bf16 ? launch_attn<true, 128>(p, a, stream) : launch_attn<false, 128>(p, a, stream);
     else
-        bf16 ? launch_rows<true, 64>(p, a, stream) : launch_rows<false, 64>(p, a, stream);
-    return check_launch("paged_attn_rows_kernel");
+        bf16 ? launch_attn<true, 64>(p, a, stream) : launch_attn<false, 64>(p, a, stream);
+    return check_launch("paged_attn kernel");
 }
 
 }  // namespace presto_host

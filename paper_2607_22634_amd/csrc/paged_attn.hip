@@ -10,9 +10,9 @@
 //
 // Rows are packed per KV head: row rho = i * G + (h - g * G), so that the G
 // query heads of a KV head share every key that is read.  The keys that the
-// rows of a workgroup see are a list of tiles: those that hold sinks, then
-// those from the window's start to the last row's position; what lies between
-// is never touched, so its pages may have been given back.
+// rows of a workgroup see are one list: the sinks, then the keys from the
+// window's start to the last row's position; what lies between is never
+// touched, so its pages may have been given back.
 #include <math.h>
 
 #include <type_traits>
@@ -85,39 +85,38 @@ __device__ __forceinline__ Seq seq_of(const Args& a, int b) {
     return {o0, min(n, a.max_q), ctx - n, c != ctx || n > a.max_q};
 }
 
-// Keys that rows at positions p_lo .. p_hi see: [0, sinks) and [lo, hi), as
-// tiles of T keys: sink_tiles of them from key 0 up to key `sink`, the others
-// from `start` (a multiple of 16, so that sixteen keys from a tile's 16-key
-// step lie in one page) up to `hi`.
+// Keys that rows at positions p_lo .. p_hi see, [0, sinks) and [lo, hi), as a
+// list of n entries: entry v is key v below `head`, and key v + gap from there
+// on.  Head and gap are multiples of 16, so that sixteen entries from a
+// multiple of 16 lie in one page.
 struct Span {
-    int lo, hi, start, sink, sink_tiles, tiles;
+    int lo, hi, head, gap, n;
 };
-template <int T>
 __device__ __forceinline__ Span span_of(const Args& a, int p_lo, int p_hi) {
     Span s;
     s.hi = max(p_hi + 1, 0);
     s.lo = a.window > 0 ? max(max(p_lo, 0) - a.window + 1, 0) : 0;
-    s.start = s.lo & ~15;
-    s.sink = min(a.sinks, s.start);
-    s.sink_tiles = (s.sink + T - 1) / T;
-    if (s.sink_tiles * T >= s.start) s.start = s.sink = s.sink_tiles = 0;
-    s.tiles = s.sink_tiles + (s.hi - s.start + T - 1) / T;
+    const int start = s.lo & ~15, head = (a.sinks + 15) & ~15;
+    s.head = head < start ? head : 0;
+    s.gap = head < start ? start - head : 0;
+    s.n = s.hi - s.gap;
     return s;
 }
+__device__ __forceinline__ int key_of(const Span& s, int v) { return v < s.head ? v : v + s.gap; }
 
 __device__ __forceinline__ bool sees(const Args& a, int pos, int key) {
     return key <= pos && (a.window == 0 || key > pos - a.window || key < a.sinks);
 }
 
 // One row on its own, key by key: what the matrix instructions cannot do when
-// a row does not see a key whose V is not finite (0 * inf).  Tiles t0 .. t1 - 1
-// of the span; O normalised into s_acc[D], (reference, sum) returned.
-template <bool BF16, int D, int T>
-__device__ float2 row_alone(const Args& a, const Span& sp, int b, int g, int64_t qrow, int head, int pos, int t0,
-                            int t1, float* s_q, float* s_p, float* s_red, float* s_acc) {
+// a row does not see a key whose V is not finite (0 * inf).  Entries v0 .. v1
+// - 1 of the list; O normalised into s_acc[D], (reference, sum) returned.
+template <bool BF16, int D>
+__device__ float2 row_alone(const Args& a, const Span& sp, int b, int g, int64_t qrow, int head, int pos, int v0,
+                            int v1, float* s_q, float* s_p, float* s_red, float* s_acc) {
     constexpr int E = BF16 ? 2 : 4;
     const int tid = threadIdx.x, NT = blockDim.x;
-    const int keys = (t1 - t0) * T;
+    const int keys = min(v1, sp.n) - v0;
     auto value = [](const char* p) {
         if constexpr (BF16)
             return bf16_to_f(*reinterpret_cast<const uint16_t*>(p));
@@ -131,10 +130,8 @@ __device__ float2 row_alone(const Args& a, const Span& sp, int b, int g, int64_t
     }
     __syncthreads();
     auto key_at = [&](int i) {
-        const int t = t0 + i / T, r = i % T;
-        const bool sink = t < sp.sink_tiles;
-        const int key = (sink ? t * T : sp.start + (t - sp.sink_tiles) * T) + r;
-        return key < (sink ? sp.sink : sp.hi) && sees(a, pos, key) ? key : -1;
+        const int key = key_of(sp, v0 + i);
+        return sees(a, pos, key) ? key : -1;
     };
     auto row_at = [&](const char* pool, int key) -> const char* {
         const int page = a.table[(int64_t)b * a.max_pages + (key >> a.page_shift)];
@@ -226,8 +223,8 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void paged_attn_rows_kernel(Args
     if (rb < 0) return;
     const int row0 = rb * R;
     const int p_lo = sq.pos0 + row0 / a.G, p_hi = sq.pos0 + (min(row0 + R, rows) - 1) / a.G;
-    const Span sp = span_of<T>(a, p_lo, p_hi);
-    const int t_begin = split * a.split_tiles, t_end = min(t_begin + a.split_tiles, sp.tiles);
+    const Span sp = span_of(a, p_lo, p_hi);
+    const int t_begin = split * a.split_tiles, t_end = min(t_begin + a.split_tiles, (sp.n + T - 1) / T);
     if (split > 0 && t_begin >= t_end) return;  // the merge knows
 
     const int t16 = lane & 15, tq = lane >> 4;
@@ -248,21 +245,19 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void paged_attn_rows_kernel(Args
 
     // ---- where a tile lies; all of it is the same for the whole wave
     struct Tile {
-        int key0, limit;
+        int key0[KB];
         int page[KB];  // -1: nothing to read
     };
     bool bad_page = false;
     const int32_t* trow = a.table + (int64_t)b * a.max_pages;
     auto locate = [&](int t) {
         Tile x;
-        const bool sink = t < sp.sink_tiles;
-        x.key0 = uniform(sink ? t * T : sp.start + (t - sp.sink_tiles) * T);
-        x.limit = sink ? sp.sink : sp.hi;
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) {
             // (sixteen keys that no row sees may be without a page)
-            const int k0 = x.key0 + 16 * kb;
-            const bool wanted = k0 < x.limit && (k0 + 16 > sp.lo || k0 < a.sinks);
+            const int k0 = uniform(key_of(sp, t * T + 16 * kb));
+            const bool wanted = k0 < sp.hi && (k0 + 16 > sp.lo || k0 < a.sinks);
+            x.key0[kb] = k0;
             x.page[kb] = wanted ? trow[k0 >> a.page_shift] : -1;
             if (wanted && (uint32_t)x.page[kb] >= (uint32_t)a.num_pages) {
                 bad_page = true;
@@ -272,7 +267,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void paged_attn_rows_kernel(Args
         return x;
     };
     auto group = [&](const char* pool, const Tile& x, int kb) {
-        const int r = (x.key0 + 16 * kb) & ((1 << a.page_shift) - 1);
+        const int r = x.key0[kb] & ((1 << a.page_shift) - 1);
         const int64_t at = x.page[kb] < 0 ? 0 : x.page[kb] * a.page_stride + (int64_t)r * a.hkv * D;
         return pool + (at + g * D) * E;  // (page 0 stands for one that is not there)
     };
@@ -357,22 +352,25 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void paged_attn_rows_kernel(Args
         if (more) load_k(nxt);
 
         // ---- masks, on the tiles that need them
-        bool edge = cur.key0 + T > min(cur.limit, p_lo + 1) ||
-                    (a.window > 0 && cur.key0 <= p_hi - a.window && cur.key0 + T > a.sinks);
+        bool edge = false;
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb) edge |= cur.page[kb] < 0;
+        for (int kb = 0; kb < KB; ++kb) {
+            const int k0 = cur.key0[kb];
+            edge |= cur.page[kb] < 0 || k0 + 16 > p_lo + 1 ||
+                    (a.window > 0 && k0 <= p_hi - a.window && k0 + 16 > a.sinks);
+        }
         if (edge) {
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
                 for (int r = 0; r < 4; ++r) {
-                    const int key = cur.key0 + 16 * kb + 4 * tq + r;
-                    const bool here = cur.page[kb] >= 0 && key < cur.limit;
+                    const int key = cur.key0[kb] + 4 * tq + r;
+                    const bool here = cur.page[kb] >= 0;
 #pragma unroll
                     for (int nb = 0; nb < NB; ++nb)
                         S[nb][kb][r] = here && sees(a, pos[nb], key) ? S[nb][kb][r] : -INFINITY;
                     // rows that nobody sees may hold anything
-                    const bool any = here && (key >= sp.lo || key < a.sinks);
+                    const bool any = here && key < sp.hi && (key >= sp.lo || key < a.sinks);
 #pragma unroll
                     for (int w = 0; w < VW; ++w) vf[4 * kb + r][w] = any ? vf[4 * kb + r][w] : 0u;
                 }
@@ -485,6 +483,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void paged_attn_rows_kernel(Args
     auto put_ml = [&](int rho, float M, float L) {
         if (a.splits > 1) a.part_ml[(bg * all + rho) * a.splits + split] = make_float2(M, L);
     };
+    bool bad = false;
     for (int i = tid; i < R * (D / 4); i += NT) {
         const int r = i / (D / 4), d = i % (D / 4) * 4;
         const int rho = row0 + r;
@@ -510,20 +509,22 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void paged_attn_rows_kernel(Args
             acc[e] *= inv;
             fine &= fabsf(acc[e]) < INFINITY;
         }
-        if (!fine) s_bad[r] = 1;
+        if (!fine) {
+            s_bad[r] = 1;
+            bad = true;
+        }
         put(rho, d, acc);
         if (d == 0) put_ml(rho, M, L);
     }
     // ---- rows of several positions whose sums are not all finite: a key that
     // only others see may be the cause
-    if (p_lo == p_hi) return;
-    __syncthreads();
+    if (p_lo == p_hi || !__syncthreads_or(bad)) return;
     for (int r = 0; r < R; ++r) {
         if (!s_bad[r]) continue;
         const int rho = row0 + r, tok = rho / a.G;
         float* const s_acc = s_o;
-        const float2 ml = row_alone<BF16, D, T>(a, sp, b, g, sq.r0 + tok, g * a.G + rho - tok * a.G, sq.pos0 + tok,
-                                                t_begin, t_end, s_o + D, s_o + 2 * D, s_o + 2 * D + NT, s_acc);
+        const float2 ml = row_alone<BF16, D>(a, sp, b, g, sq.r0 + tok, g * a.G + rho - tok * a.G, sq.pos0 + tok,
+                                             t_begin * T, t_end * T, s_o + D, s_o + 2 * D, s_o + 2 * D + NT, s_acc);
         for (int d = tid * 4; d < D; d += NT * 4) put(rho, d, *reinterpret_cast<const floatx4*>(&s_acc[d]));
         if (tid == 0) put_ml(rho, ml.x, ml.y);
     }
@@ -605,17 +606,34 @@ __global__ __launch_bounds__(kTileWaves * kWave) void paged_attn_tiles_kernel(Ar
     if (rb < 0) return;
     const int row0 = rb * kTileRows;
     const int row_end = min(row0 + kTileRows, rows);
-    const Span sp = span_of<T>(a, sq.pos0 + row0 / a.G, sq.pos0 + (row_end - 1) / a.G);
-    const int t_begin = split * a.split_tiles, t_end = min(t_begin + a.split_tiles, sp.tiles);
+    const Span sp = span_of(a, sq.pos0 + row0 / a.G, sq.pos0 + (row_end - 1) / a.G);
+    const int t_begin = split * a.split_tiles, t_end = min(t_begin + a.split_tiles, (sp.n + T - 1) / T);
     if (split > 0 && t_begin >= t_end) return;  // the merge knows
     const int64_t bg = (int64_t)b * a.hkv + g, all = (int64_t)a.G * a.max_q;
 
-    // ---- page numbers: those of the sink tiles' keys, then of the others
-    auto key_of = [&](int t) { return t < sp.sink_tiles ? t * T : sp.start + (t - sp.sink_tiles) * T; };
-    const int ka = t_begin * T, ka_end = min(sp.sink, t_end * T);
-    const int kb = key_of(max(t_begin, sp.sink_tiles)), kb_end = min(sp.hi, sp.start + (t_end - sp.sink_tiles) * T);
-    const int pa = ka < ka_end ? ka >> a.page_shift : 0;
-    const int na = ka < ka_end ? ((ka_end - 1) >> a.page_shift) - pa + 1 : 0;
+    const int l32 = lane & 31, h = lane >> 5;
+    const int wrow0 = row0 + wave * 32;  // this wave's first row
+    const int rho = wrow0 + l32;
+    const int rq = min(rho, rows - 1);
+    const int tok = rq / a.G, qh = rq - tok * a.G;
+    const int pos = sq.pos0 + tok;
+    const int p_lo = uniform(sq.pos0 + min(wrow0, rows - 1) / a.G);
+    const int p_hi = uniform(sq.pos0 + min(wrow0 + 31, rows - 1) / a.G);
+    const float c = a.scale_log2;
+    // queries, second operand of S^T: row l32, dims ks * 16 + h * 8 ..
+    bf16x8 qf[KS];
+    {
+        const char* qp = a.q + ((sq.r0 + tok) * a.q_stride + (int64_t)(g * a.G + qh) * D + h * 8) * 2;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks)
+            qf[ks] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(qp + ks * 32));
+    }
+
+    // ---- page numbers: those of the entries before the gap, then of the others
+    const int va = t_begin * T, va_end = min(sp.head, t_end * T);
+    const int pa = va >> a.page_shift;
+    const int na = va < va_end ? ((va_end - 1) >> a.page_shift) - pa + 1 : 0;
+    const int kb = max(va, sp.head) + sp.gap, kb_end = min(sp.hi, t_end * T + sp.gap);
     const int pb = kb >> a.page_shift;
     const int nb = kb < kb_end ? ((kb_end - 1) >> a.page_shift) - pb + 1 : 0;
     {
@@ -623,8 +641,8 @@ __global__ __launch_bounds__(kTileWaves * kWave) void paged_attn_tiles_kernel(Ar
         const int32_t* trow = a.table + (int64_t)b * a.max_pages;
         for (int i = tid; i < min(na + nb, kTilePages); i += NT) {
             const int x = i < na ? pa + i : pb + i - na;
-            const int k0 = max(x << a.page_shift, kb), k1 = min((x + 1) << a.page_shift, kb_end);
-            const bool wanted = i < na || k1 > sp.lo || k0 < a.sinks;
+            const int k0 = max(x << a.page_shift, i < na ? va : kb), k1 = min((x + 1) << a.page_shift, kb_end);
+            const bool wanted = k0 < a.sinks || (i >= na && k1 > sp.lo);
             const int page = wanted ? trow[x] : 0;
             const bool ok = (uint32_t)page < (uint32_t)a.num_pages;
             bad |= !ok;
@@ -640,17 +658,6 @@ __global__ __launch_bounds__(kTileWaves * kWave) void paged_attn_tiles_kernel(Ar
     __syncthreads();
     const bool skip = s_bad[0] != 0;
 
-    const int l32 = lane & 31, h = lane >> 5;
-    const int wrow0 = row0 + wave * 32;  // this wave's first row
-    const bool active = wrow0 < rows && !skip && t_begin < t_end;
-    const int rho = wrow0 + l32;
-    const int rq = min(rho, rows - 1);
-    const int tok = rq / a.G, qh = rq - tok * a.G;
-    const int pos = sq.pos0 + tok;
-    const int p_lo = uniform(sq.pos0 + min(wrow0, rows - 1) / a.G);
-    const int p_hi = uniform(sq.pos0 + min(wrow0 + 31, rows - 1) / a.G);
-    const float c = a.scale_log2;
-
     floatx16 o[DB];
 #pragma unroll
     for (int db = 0; db < DB; ++db)
@@ -659,14 +666,6 @@ __global__ __launch_bounds__(kTileWaves * kWave) void paged_attn_tiles_kernel(Ar
     float m = 0.f, l_run = 0.f;  // reference (score units) and sum of the row
 
     if (!skip && t_begin < t_end) {
-        // queries, second operand of S^T: row l32, dims ks * 16 + h * 8 ..
-        bf16x8 qf[KS];
-        {
-            const char* qp = a.q + ((sq.r0 + tok) * a.q_stride + (int64_t)(g * a.G + qh) * D + h * 8) * 2;
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks)
-                qf[ks] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(qp + ks * 32));
-        }
         // ---- loads: instruction j of this wave covers rows 8 wave + RPL j ..
         // of a tile; lane l writes chunk l % CH of row l / CH and fetches the
         // chunk that the row's permutation puts there
@@ -683,42 +682,34 @@ __global__ __launch_bounds__(kTileWaves * kWave) void paged_attn_tiles_kernel(Ar
         }
         const uint32_t lds_kv = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)s_kv;
         const int pmask = (1 << a.page_shift) - 1;
-        auto page_of = [&](bool sink, int key) __attribute__((always_inline)) {
-            return s_page[sink ? (key >> a.page_shift) - pa : na + (key >> a.page_shift) - pb];
+        auto page_of = [&](bool head, int key) __attribute__((always_inline)) {
+            return s_page[(key >> a.page_shift) - (head ? pa : pb - na)];
         };
-        const int k_last = min(key_of(t_end - 1) + T, t_end - 1 < sp.sink_tiles ? sp.sink : sp.hi) - 1;
         auto load_tile = [&](int t, int buf) __attribute__((always_inline)) {
             const uint32_t kdst = lds_kv + buf * kTile + wave * LPT * 1024;
             const uint32_t vdst = kdst + kV;
-            const bool sink = t < sp.sink_tiles;
-            const int key0 = key_of(t);
-            if (t < t_end && (sink ? key0 + T <= sp.sink
-                                   : key0 + T <= sp.hi && (key0 >= sp.lo || key0 + T <= a.sinks))) {
+            const int v0 = t * T, key0 = v0 + sp.gap;
+            if (t < t_end && v0 >= sp.head && key0 + T <= sp.hi && (key0 >= sp.lo || key0 + T <= a.sinks)) {
                 const int kw = key0 + 8 * wave;
-                const int64_t at = uniform(page_of(sink, kw)) * a.page_stride + ((int64_t)(kw & pmask) * a.hkv + g) * D;
+                const int64_t at = uniform(page_of(false, kw)) * a.page_stride + ((int64_t)(kw & pmask) * a.hkv + g) * D;
 #pragma unroll
                 for (int j = 0; j < LPT; ++j) {
                     lds_load16(a.kp + at * 2, goff_k[j], kdst + j * 1024);
                     lds_load16(a.vp + at * 2, goff_v[j], vdst + j * 1024);
                 }
             } else {
-                // rows that no query of the workgroup sees repeat one that
-                // some query does (nothing but what is seen is read)
-                const bool last_sink = t_end - 1 < sp.sink_tiles;
+                // entries that no query of the workgroup sees repeat one of
+                // their tile that some query does (nothing else is read: there
+                // may be no page, and V must be a number where P is 0); past
+                // the last tile, its last entry
+                const int vt = min(t, t_end - 1) * T;
 #pragma unroll
                 for (int j = 0; j < LPT; ++j) {
-                    int key = key0 + lrow[j];
-                    bool in_sink = sink;
-                    if (t >= t_end) {
-                        key = k_last;
-                        in_sink = last_sink;
-                    } else if (sink) {
-                        key = min(key, sp.sink - 1);
-                    } else {
-                        if (key < sp.lo && key >= a.sinks) key = key0 < a.sinks ? a.sinks - 1 : sp.lo;
-                        key = min(key, sp.hi - 1);
-                    }
-                    const int64_t at = page_of(in_sink, key) * a.page_stride + ((int64_t)(key & pmask) * a.hkv + g) * D;
+                    const int v = t < t_end ? v0 + lrow[j] : vt + T - 1;
+                    const bool head = v < sp.head;
+                    int key = head ? min(v, a.sinks - 1) : min(v + sp.gap, sp.hi - 1);
+                    if (!head && key < sp.lo && key >= a.sinks) key = sp.gap == 0 && vt < a.sinks ? a.sinks - 1 : sp.lo;
+                    const int64_t at = page_of(head, key) * a.page_stride + ((int64_t)(key & pmask) * a.hkv + g) * D;
                     lds_load16(a.kp + (at + lck[j] * 8) * 2, kdst + j * 1024);
                     lds_load16(a.vp + (at + lcv[j] * 8) * 2, vdst + j * 1024);
                 }
@@ -727,9 +718,11 @@ __global__ __launch_bounds__(kTileWaves * kWave) void paged_attn_tiles_kernel(Ar
         // vmcnt(n) with the other counters left alone
 #define PRESTO_WAIT_VM(n) __builtin_amdgcn_s_waitcnt(((n) & 15) | (((n) >> 4) << 14) | 0x0f70)
 
+        // the blocks of the workgroup, and of this wave up to its last row's
+        // position
         const int ntiles = t_end - t_begin;
-        // (the last window tile may end in its first half)
-        const int nblocks = 2 * ntiles - (t_end > sp.sink_tiles && key_of(t_end - 1) + 32 >= sp.hi ? 1 : 0);
+        const int nblocks = (min(min(p_hi + 1 - sp.gap, sp.n), t_end * T) - t_begin * T + 31) / 32;
+        const bool active = wrow0 < rows && nblocks > 0;
 
         // per-lane LDS addresses of the fragment reads (ring slot 0, block 0)
         const int vr = 4 * h + ((lane & 15) >> 2);
@@ -759,19 +752,19 @@ __global__ __launch_bounds__(kTileWaves * kWave) void paged_attn_tiles_kernel(Ar
             return fmaxf(mx, half_swap(mx));
         };
         auto row_sum = [&](float v) __attribute__((always_inline)) { return v + half_swap(v); };
-        // first key and key limit of block i
-        auto j0_of = [&](int i) { return key_of(t_begin + (i >> 1)) + 32 * (i & 1); };
-        auto lim_of = [&](int i) { return t_begin + (i >> 1) < sp.sink_tiles ? sp.sink : sp.hi; };
         auto masked = [&](int i) __attribute__((always_inline)) {
-            const int j0 = j0_of(i);
-            return j0 + 32 > min(lim_of(i), p_lo + 1) || (a.window > 0 && j0 <= p_hi - a.window && j0 + 32 > a.sinks);
+            const int v0 = t_begin * T + 32 * i, k0 = v0 + sp.gap;
+            return k0 + 32 > p_lo + 1 || v0 < sp.head || (a.window > 0 && k0 <= p_hi - a.window && k0 + 32 > a.sinks);
         };
-        // the block's 32 keys as bits, then a test and a select per element
+        // the block's 32 entries as bits, then a test and a select per element
         auto apply_mask = [&](floatx16& S, int i) __attribute__((always_inline)) {
-            const int j0 = j0_of(i);
+            const int v0 = t_begin * T + 32 * i;
             auto below = [](int n) { return n >= 32 ? ~0u : (n <= 0 ? 0u : (1u << n) - 1u); };
-            uint32_t vis = below(min(lim_of(i), pos + 1) - j0);
-            if (a.window > 0) vis &= ~below(pos - a.window + 1 - j0) | below(a.sinks - j0);
+            uint32_t vis = below(pos + 1 - sp.gap - v0);
+            if (a.window > 0) {
+                vis &= ~below(max(pos - a.window + 1 - sp.gap, sp.head) - v0);
+                vis |= below(min(a.sinks, pos + 1) - v0);
+            }
             vis >>= 4 * h;
 #pragma unroll
             for (int e = 0; e < 16; ++e) S[e] = (vis >> (8 * (e >> 2) + (e & 3))) & 1u ? S[e] : -INFINITY;
@@ -862,7 +855,7 @@ __global__ __launch_bounds__(kTileWaves * kWave) void paged_attn_tiles_kernel(Ar
             using BK = std::integral_constant<int, (u + 1) % kRing>;
             load_tile(t_begin + t + 3, (u + 3) % kRing);
             if (active) {
-                step(BV{}, BK{}, 2 * t, 0);
+                if (2 * t < nblocks) step(BV{}, BK{}, 2 * t, 0);
                 if (2 * t + 1 < nblocks) step(BV{}, BK{}, 2 * t + 1, 1);
             }
             PRESTO_WAIT_VM(2 * LPT);
@@ -900,6 +893,7 @@ __global__ __launch_bounds__(kTileWaves * kWave) void paged_attn_tiles_kernel(Ar
         return reinterpret_cast<uint16_t*>(a.out) + ((sq.r0 + tk) * a.hq + g * a.G + r - tk * a.G) * D;
     };
     auto part_row = [&](int r) { return a.part_o + ((bg * a.splits + split) * all + r) * D; };
+    bool bad = skip;
     if (rho < rows && !skip) {
         const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
         bool fine = true;
@@ -910,7 +904,10 @@ __global__ __launch_bounds__(kTileWaves * kWave) void paged_attn_tiles_kernel(Ar
                 o[db][e] *= inv;
                 fine &= fabsf(o[db][e]) < INFINITY;
             }
-        if (!fine) s_bad[rho - row0] = 1;
+        if (!fine) {
+            s_bad[rho - row0] = 1;
+            bad = true;
+        }
         if (a.splits == 1) {
             uint16_t* op = out_row(rho);
 #pragma unroll
@@ -932,13 +929,13 @@ __global__ __launch_bounds__(kTileWaves * kWave) void paged_attn_tiles_kernel(Ar
     }
     // ---- rows whose sums are not all finite: a key that only others see may
     // be the cause
-    __syncthreads();
+    if (!__syncthreads_or(bad)) return;
     float* const f = reinterpret_cast<float*>(s_kv);
     for (int r = 0; r < row_end - row0; ++r) {
         if (!s_bad[r]) continue;
         const int rr = row0 + r, tk = rr / a.G;
-        const float2 ml = row_alone<true, D, T>(a, sp, b, g, sq.r0 + tk, g * a.G + rr - tk * a.G, sq.pos0 + tk, t_begin,
-                                                t_end, f + D, f + 2 * D, f + 2 * D + NT, f);
+        const float2 ml = row_alone<true, D>(a, sp, b, g, sq.r0 + tk, g * a.G + rr - tk * a.G, sq.pos0 + tk, t_begin * T,
+                                             t_end * T, f + D, f + 2 * D, f + 2 * D + NT, f);
         for (int d = tid; d < D / 2; d += NT) {
             if (a.splits == 1)
                 *reinterpret_cast<uint32_t*>(out_row(rr) + 2 * d) = pack2(f[2 * d], f[2 * d + 1]);
@@ -965,9 +962,8 @@ __global__ __launch_bounds__(256) void paged_attn_merge_kernel(Args a, int rows_
     if (tok >= sq.n) return;
     const int g = head / a.G, rho = tok * a.G + head - g * a.G;
     const int row0 = rho / rows_per_block * rows_per_block;
-    const Span sp = span_of<T>(a, sq.pos0 + row0 / a.G,
-                               sq.pos0 + (min(row0 + rows_per_block, sq.n * a.G) - 1) / a.G);
-    const int live = max(min((sp.tiles + a.split_tiles - 1) / a.split_tiles, a.splits), 1);
+    const Span sp = span_of(a, sq.pos0 + row0 / a.G, sq.pos0 + (min(row0 + rows_per_block, sq.n * a.G) - 1) / a.G);
+    const int live = max(min(((sp.n + T - 1) / T + a.split_tiles - 1) / a.split_tiles, a.splits), 1);
     const int64_t bg = (int64_t)b * a.hkv + g, all = (int64_t)a.G * a.max_q;
     const float2* ml = a.part_ml + (bg * all + rho) * a.splits;
     const float* po = a.part_o + (bg * a.splits * all + rho) * D + ln * 4;
@@ -1040,14 +1036,13 @@ PagedPlan paged_plan(const presto_paged_attn_desc* d) {
     // of its first to its last row
     int64_t longest = d->max_ctx > 0 ? d->max_ctx : 1;
     if (d->window > 0) {
-        const int64_t span = (int64_t)d->window + p.rows_per_block / G + 1 + d->sinks + 16 + T;
+        const int64_t span = (int64_t)d->window + (p.rows_per_block - 1) / G + 1 + 15 + (d->sinks + 15) / 16 * 16;
         if (span < longest) longest = span;
     }
     const int64_t all = (int64_t)d->pages.batch * d->pages.hkv * p.row_blocks;
     int64_t mean = longest;
     if (d->total_ctx > 0 && d->total_ctx / d->pages.batch < mean) mean = d->total_ctx / d->pages.batch + 1;
-    // (a span's first and last tile may be partly filled)
-    const int64_t tiles = cdiv(longest, T) + (d->window > 0 ? 2 : 0);
+    const int64_t tiles = cdiv(longest, T);
     int64_t per;
     if (p.tiles) {
         // one workgroup per CU: split only where the rows leave CUs idle, at

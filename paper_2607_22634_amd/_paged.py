@@ -14,18 +14,18 @@ import torch
 from ._lib import PagedAttnDesc, PagesDesc, _check, _dt, _ptr, lib
 
 
-def _same(dev, **ts):
-    for name, t in ts.items():
+def _same(dev, names: str, *ts) -> None:
+    """Tensors on one GPU (None: left out)."""
+    for i, t in enumerate(ts):
         if t is not None and (not t.is_cuda or t.device != dev):
-            raise ValueError(f"{name} must be a tensor on {dev}")
+            raise ValueError(f"{names.split()[i]} must be a tensor on the GPU of the others, {dev}")
 
 
-def _book(dev, **ts):
-    """int32 bookkeeping tensors, contiguous, on one device."""
-    _same(dev, **ts)
-    for name, t in ts.items():
-        if t is not None and (t.dtype != torch.int32 or not t.is_contiguous()):
-            raise ValueError(f"{name} must be a contiguous int32 tensor")
+def _book(dev, names: str, *ts) -> None:
+    """int32 bookkeeping tensors, contiguous, on one GPU."""
+    for i, t in enumerate(ts):
+        if t is not None and not (t.dtype is torch.int32 and t.is_cuda and t.device == dev and t.is_contiguous()):
+            raise ValueError(f"{names.split()[i]} must be a contiguous int32 tensor on the GPU of the others, {dev}")
 
 
 def _shape(name, t, *shape):
@@ -33,17 +33,12 @@ def _shape(name, t, *shape):
         raise ValueError(f"{name} must be of shape {list(shape)}, not {list(t.shape)}")
 
 
-@contextlib.contextmanager
-def _switch(dev):
-    with torch.cuda.device(dev):
-        yield
+_HERE = contextlib.nullcontext()
 
 
 def _on(dev):
     """Makes `dev` the current device (free when it is already)."""
-    if dev.index is None or dev.index == torch._C._cuda_getDevice():
-        return contextlib.nullcontext()
-    return _switch(dev)
+    return _HERE if dev.index == torch._C._cuda_getDevice() else torch.cuda.device(dev)
 
 
 def _queue(dev, stream, *made):
@@ -62,86 +57,83 @@ def _queue(dev, stream, *made):
 def _pool(k, v, page_table, batch, layers: bool) -> PagesDesc:
     """Descriptor of the pools k, v: [pages, page, hkv, dim], or with a leading
     layer dimension where `layers` allows it."""
-    if k.dim() not in ((4, 5) if layers else (4,)):
+    shape, stride = k.shape, k.stride()
+    if len(shape) != 4 and not (layers and len(shape) == 5):
         raise ValueError("the page pools must be [pages, page, hkv, dim]" + (" or with layers first" if layers else ""))
-    if v.shape != k.shape or v.stride() != k.stride() or v.dtype != k.dtype:
+    if v.shape != shape or v.stride() != stride or v.dtype != k.dtype:
         raise ValueError("k_pages and v_pages must have one shape, stride and type")
-    n, page, hkv, d = k.shape[-4:]
-    if k.stride()[-3:] != (hkv * d, d, 1) and k.numel() > 0:
+    n, page, hkv, d = shape[-4:]
+    if stride[-3:] != (hkv * d, d, 1) and k.numel() > 0:
         raise ValueError("a page must be contiguous")
-    desc = PagesDesc()
-    desc.batch, desc.max_pages = batch, page_table.shape[1]
-    desc.num_pages, desc.page_size, desc.hkv, desc.head_dim = n, page, hkv, d
-    desc.dt = _dt(k)
-    desc.layers = k.shape[0] if k.dim() == 5 else 1
-    # (the stride of a single page or layer is free: the default)
-    desc.page_stride = k.stride(-4) if n > 1 else 0
-    desc.layer_stride = k.stride(0) if k.dim() == 5 and k.shape[0] > 1 else 0
-    if (n > 1 and desc.page_stride == 0) or (desc.layers > 1 and desc.layer_stride == 0):
-        raise ValueError("pages and layers must not overlap")
-    if k.dim() == 5 and desc.layers > 1:
-        # layers apart, or pages apart and the layers inside a page's stride
-        # would be interleaved: only the former is a layout of the pool
-        if desc.layer_stride < (n - 1) * k.stride(-4) + page * hkv * d:
+    # (the stride of a single page or layer is free: the default, 0)
+    page_stride, n_layers, layer_stride = stride[-4] if n > 1 else 0, 1, 0
+    if n > 1 and page_stride < page * hkv * d:
+        raise ValueError("pages must not overlap")
+    if len(shape) == 5 and shape[0] != 1:
+        n_layers, layer_stride = shape[0], stride[0]
+        if layer_stride < (n - 1) * page_stride + page * hkv * d:
             raise ValueError("layers must not overlap")
-    return desc
+    return PagesDesc(batch, page_table.shape[1], n, page, hkv, d, _dt(k), n_layers, page_stride, layer_stride)
 
 
 def _books(refs, page_table, page_size) -> PagesDesc:
     """Descriptor for the calls that look at the books only."""
-    desc = PagesDesc()
-    desc.batch, desc.max_pages = page_table.shape
-    desc.num_pages, desc.page_size = refs.numel(), page_size
-    desc.hkv, desc.head_dim, desc.dt, desc.layers = 1, 64, 0, 1
-    return desc
+    batch, cols = page_table.shape
+    return PagesDesc(batch, cols, refs.numel(), page_size, 1, 64, 0, 1, 0, 0)
 
 
-def _rows(name, t, hkv, d):
+def _rows(name, t, heads, d):
     """Token rows [n, heads, dim], any stride between tokens; the stride."""
-    if t.dim() != 3 or tuple(t.shape[1:]) != (hkv, d):
-        raise ValueError(f"{name} must be [tokens, {hkv}, {d}]")
-    if t.numel() > 0 and t.stride()[1:] != (d, 1) and not (hkv == 1 and t.stride(2) == 1):
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or shape[1] != heads or shape[2] != d:
+        raise ValueError(f"{name} must be [tokens, {heads}, {d}]")
+    if (stride[2] != 1 or (stride[1] != d and heads > 1)) and t.numel() > 0:
         raise ValueError(f"the heads of a token of {name} must be contiguous")
-    return t.stride(0) if t.shape[0] > 1 else 0
+    return stride[0] if shape[0] > 1 else 0
 
 
 def _attn_desc(q, k_pages, v_pages, page_table, batch, max_q, max_ctx, scale, window, sinks, total_ctx):
-    if page_table.dim() != 2:
+    if page_table.dim() != 2 or page_table.shape[0] != batch:
         raise ValueError("page_table must be [sequences, columns]")
-    _shape("page_table", page_table, batch, page_table.shape[1])
-    desc = PagedAttnDesc()
-    desc.pages = _pool(k_pages, v_pages, page_table, batch, False)
+    pages = _pool(k_pages, v_pages, page_table, batch, False)
     if q.dtype != k_pages.dtype:
         raise TypeError("q and the pages must be of one type")
-    hkv, d = k_pages.shape[2:]
-    desc.hq = q.shape[1]
-    desc.q_stride = _rows("q", q, q.shape[1], d)
-    desc.max_q, desc.total_q = max_q, q.shape[0]
-    desc.max_ctx = page_table.shape[1] * k_pages.shape[1] if max_ctx is None else max_ctx
-    desc.window, desc.sinks, desc.total_ctx = window, sinks, total_ctx
-    desc.scale = d ** -0.5 if scale is None else scale
-    return desc
+    d = pages.head_dim
+    n, hq = q.shape[:2]
+    stride = _rows("q", q, hq, d)
+    if max_ctx is None:
+        max_ctx = pages.max_pages * pages.page_size
+    return PagedAttnDesc(pages, hq, max_q, max_ctx, window, sinks, d ** -0.5 if scale is None else scale, n, stride,
+                         total_ctx)
 
 
-def _attend(who, q, q_offsets, k_pages, v_pages, page_table, ctx, desc, out, flags, workspace, stream):
+def _attend(call, need_of, q, q_offsets, k_pages, v_pages, page_table, ctx, desc, out, flags, workspace, stream):
     dev = q.device
-    _same(dev, q=q, k_pages=k_pages, v_pages=v_pages, out=out, workspace=workspace)
-    _book(dev, page_table=page_table, ctx=ctx, q_offsets=q_offsets, flags=flags)
-    made = None
+    _same(dev, "q k_pages v_pages out workspace", q, k_pages, v_pages, out, workspace)
+    _book(dev, "page_table ctx q_offsets flags", page_table, ctx, q_offsets, flags)
+    ref = ctypes.byref(desc)
+    made, ws, nb = [], workspace, 0
     if out is None:
-        out = made = torch.empty(q.shape, dtype=q.dtype, device=dev)
+        out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+        made.append(out)
     elif out.shape != q.shape or out.dtype != q.dtype or not out.is_contiguous():
         raise ValueError("out must be a contiguous tensor of q's shape and type")
-    need = getattr(lib(), who + "_workspace")(ctypes.byref(desc))
-    ws, made_ws = workspace, None
-    if need and ws is None:
-        ws = made_ws = torch.empty(need, dtype=torch.uint8, device=dev)
-    nb = 0 if ws is None else ws.numel() * ws.element_size()
+    if ws is None:
+        nb = need_of(ref)
+        if nb:
+            ws = torch.empty(nb, dtype=torch.uint8, device=dev)
+            made.append(ws)
+    else:
+        nb = ws.numel() * ws.element_size()
     with _on(dev):
-        st = _queue(dev, stream, made, made_ws)
-        offs = () if q_offsets is None else (_ptr(q_offsets),)
-        _check(getattr(lib(), who)(ctypes.byref(desc), _ptr(q), *offs, _ptr(k_pages), _ptr(v_pages),
-                                   _ptr(page_table), _ptr(ctx), _ptr(out), _ptr(flags), _ptr(ws), nb, st), who)
+        tail = (page_table.data_ptr(), ctx.data_ptr(), out.data_ptr(), _ptr(flags), _ptr(ws), nb,
+                _queue(dev, stream, *made))
+        if q_offsets is None:
+            status = call(ref, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), *tail)
+        else:
+            status = call(ref, q.data_ptr(), q_offsets.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), *tail)
+        if status:
+            _check(status, "presto_paged_attention" if q_offsets is None else "presto_window_attention")
     return out
 
 
@@ -155,8 +147,9 @@ def presto_paged_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torc
     b = q.shape[0]
     desc = _attn_desc(q, k_pages, v_pages, page_table, b, 1, max_ctx, scale, window, sinks, total_ctx)
     _shape("ctx", ctx, b)
-    return _attend("presto_paged_attention", q, None, k_pages, v_pages, page_table, ctx, desc, out, flags,
-                   workspace, stream)
+    L = lib()
+    return _attend(L.presto_paged_attention, L.presto_paged_attention_workspace, q, None, k_pages, v_pages,
+                   page_table, ctx, desc, out, flags, workspace, stream)
 
 
 def presto_window_attention(q: torch.Tensor, q_offsets: torch.Tensor, max_q: int, k_pages: torch.Tensor,
@@ -168,9 +161,11 @@ def presto_window_attention(q: torch.Tensor, q_offsets: torch.Tensor, max_q: int
     q [total, Hq, d] are the last positions of sequence b, at most max_q."""
     b = q_offsets.shape[0] - 1
     desc = _attn_desc(q, k_pages, v_pages, page_table, b, max_q, max_ctx, scale, window, sinks, total_ctx)
+    _shape("q_offsets", q_offsets, b + 1)
     _shape("ctx", ctx, b)
-    return _attend("presto_window_attention", q, q_offsets, k_pages, v_pages, page_table, ctx, desc, out, flags,
-                   workspace, stream)
+    L = lib()
+    return _attend(L.presto_window_attention, L.presto_window_attention_workspace, q, q_offsets, k_pages, v_pages,
+                   page_table, ctx, desc, out, flags, workspace, stream)
 
 
 def paged_attention_workspace(q: torch.Tensor, k_pages: torch.Tensor, page_table: torch.Tensor, *, max_q: int = 1,
@@ -187,15 +182,14 @@ def paged_attention_workspace(q: torch.Tensor, k_pages: torch.Tensor, page_table
 
 def _pages_call(who, dev, desc, args, flags, workspace, stream, made=()):
     """args: the call's pointers up to flags."""
-    need = lib().presto_pages_workspace(ctypes.byref(desc))
-    _same(dev, workspace=workspace)
-    ws, made_ws = workspace, None
+    L, ref, ws = lib(), ctypes.byref(desc), workspace
+    _same(dev, "workspace", ws)
     if ws is None:
-        ws = made_ws = torch.empty(max(need, 16), dtype=torch.uint8, device=dev)
+        ws = torch.empty(max(L.presto_pages_workspace(ref), 16), dtype=torch.uint8, device=dev)
+        made = (*made, ws)
     with _on(dev):
-        st = _queue(dev, stream, made_ws, *made)
-        _check(getattr(lib(), who)(ctypes.byref(desc), *args, _ptr(flags), _ptr(ws),
-                                   ws.numel() * ws.element_size(), st), who)
+        _check(getattr(L, who)(ref, *args, _ptr(flags), ws.data_ptr(), ws.numel() * ws.element_size(),
+                               _queue(dev, stream, *made)), who)
 
 
 def pages_workspace(refs: torch.Tensor, page_table: torch.Tensor) -> torch.Tensor:
@@ -204,10 +198,10 @@ def pages_workspace(refs: torch.Tensor, page_table: torch.Tensor) -> torch.Tenso
     return torch.empty(max(need, 16), dtype=torch.uint8, device=refs.device)
 
 
-def _check_books(refs, page_table, ctx, **more):
+def _check_books(refs, page_table, ctx, names: str = "", *more):
     if page_table.dim() != 2 or refs.dim() != 1:
         raise ValueError("page_table must be [sequences, columns] and refs [pages]")
-    _book(refs.device, refs=refs, page_table=page_table, ctx=ctx, **more)
+    _book(refs.device, "refs page_table ctx " + names, refs, page_table, ctx, *more)
     _shape("ctx", ctx, page_table.shape[0])
 
 
@@ -217,7 +211,7 @@ def presto_pages_reserve(refs: torch.Tensor, page_table: torch.Tensor, ctx: torc
     """Gives pages to the positions ctx .. ctx + add + extra - 1 and returns the
     new lengths (in `out`, which may be ctx); refs and page_table are updated
     in place.  A sequence the pool has no pages for keeps its length."""
-    _check_books(refs, page_table, ctx, add=add, out=out, flags=flags)
+    _check_books(refs, page_table, ctx, "add out flags", add, out, flags)
     b = page_table.shape[0]
     _shape("add", add, b)
     _shape("out", out, b)
@@ -237,22 +231,25 @@ def presto_append_kv(k_new: torch.Tensor, v_new: torch.Tensor, offsets: torch.Te
     ctx[b] + i < ctx_new[b] of the cache, at most max_new per sequence."""
     dev = k_new.device
     b = offsets.shape[0] - 1
-    _same(dev, k_new=k_new, v_new=v_new, k_pages=k_pages, v_pages=v_pages)
-    _book(dev, offsets=offsets, page_table=page_table, ctx=ctx, ctx_new=ctx_new, flags=flags)
-    _shape("page_table", page_table, b, page_table.shape[-1])
+    _same(dev, "k_new v_new k_pages v_pages", k_new, v_new, k_pages, v_pages)
+    _book(dev, "offsets page_table ctx ctx_new flags", offsets, page_table, ctx, ctx_new, flags)
+    _shape("offsets", offsets, b + 1)
+    if page_table.dim() != 2 or page_table.shape[0] != b:
+        raise ValueError("page_table must be [sequences, columns]")
     _shape("ctx", ctx, b)
     _shape("ctx_new", ctx_new, b)
     desc = _pool(k_pages, v_pages, page_table, b, False)
     if k_new.dtype != k_pages.dtype or v_new.dtype != k_pages.dtype:
         raise TypeError("the new rows and the pages must be of one type")
-    stride = _rows("k_new", k_new, *k_pages.shape[2:])
-    if v_new.shape != k_new.shape or _rows("v_new", v_new, *k_pages.shape[2:]) != stride:
+    hkv, d = k_pages.shape[2:]
+    stride = _rows("k_new", k_new, hkv, d)
+    if v_new.shape != k_new.shape or _rows("v_new", v_new, hkv, d) != stride:
         raise ValueError("k_new and v_new must have one shape and stride")
     with _on(dev):
-        st = _queue(dev, stream)
-        _check(lib().presto_append_kv(ctypes.byref(desc), _ptr(k_new), _ptr(v_new), k_new.shape[0], stride,
-                                      _ptr(offsets), max_new, _ptr(k_pages), _ptr(v_pages), _ptr(page_table),
-                                      _ptr(ctx), _ptr(ctx_new), _ptr(flags), st), "presto_append_kv")
+        _check(lib().presto_append_kv(ctypes.byref(desc), k_new.data_ptr(), v_new.data_ptr(), k_new.shape[0], stride,
+                                      offsets.data_ptr(), max_new, k_pages.data_ptr(), v_pages.data_ptr(),
+                                      page_table.data_ptr(), ctx.data_ptr(), ctx_new.data_ptr(), _ptr(flags),
+                                      _queue(dev, stream)), "presto_append_kv")
 
 
 def presto_pages_fork(refs: torch.Tensor, page_table: torch.Tensor, ctx: torch.Tensor, parent: torch.Tensor,
@@ -261,8 +258,8 @@ def presto_pages_fork(refs: torch.Tensor, page_table: torch.Tensor, ctx: torch.T
     """Sequence child[i] (empty) becomes a copy of parent[i]: full pages shared,
     the rows of the last one copied in all layers of k_pages, v_pages
     [layers, pages, page, Hkv, d] (or of one layer, without that dimension)."""
-    _check_books(refs, page_table, ctx, parent=parent, child=child, flags=flags)
-    _same(refs.device, k_pages=k_pages, v_pages=v_pages)
+    _check_books(refs, page_table, ctx, "parent child flags", parent, child, flags)
+    _same(refs.device, "k_pages v_pages", k_pages, v_pages)
     n = parent.numel()
     _shape("parent", parent, n)
     _shape("child", child, n)
@@ -276,7 +273,7 @@ def presto_pages_fork(refs: torch.Tensor, page_table: torch.Tensor, ctx: torch.T
 def presto_pages_free(refs: torch.Tensor, page_table: torch.Tensor, ctx: torch.Tensor, rows: torch.Tensor, *,
                       flags=None, stream=None) -> None:
     """Drops the sequences `rows`: their references go, their lengths are 0."""
-    _check_books(refs, page_table, ctx, rows=rows, flags=flags)
+    _check_books(refs, page_table, ctx, "rows flags", rows, flags)
     _shape("rows", rows, rows.numel())
     desc = _books(refs, page_table, 16)
     with _on(refs.device):
@@ -289,7 +286,7 @@ def presto_pages_trim(refs: torch.Tensor, page_table: torch.Tensor, ctx: torch.T
                       sinks: int = 0, *, flags=None, stream=None) -> None:
     """Drops the pages that no query from position ctx - 1 on sees under the
     window and sinks."""
-    _check_books(refs, page_table, ctx, flags=flags)
+    _check_books(refs, page_table, ctx, "flags", flags)
     desc = _books(refs, page_table, page_size)
     with _on(refs.device):
         st = _queue(refs.device, stream)
@@ -303,16 +300,16 @@ def presto_pages_compact(refs: torch.Tensor, page_table: torch.Tensor, k_pages: 
     the books afterwards: refs, page_table, n_live [1] (or fills those of
     `out`, where refs and page_table may be the arguments themselves, and
     page_map [pages], each live page's new number, if it is there)."""
-    _check_books(refs, page_table, None, flags=flags)
+    _check_books(refs, page_table, None, "flags", flags)
     dev = refs.device
-    _same(dev, k_pages=k_pages, v_pages=v_pages)
+    _same(dev, "k_pages v_pages", k_pages, v_pages)
     made = ()
     if out is None:
         out = {"refs": torch.empty_like(refs), "page_table": torch.empty_like(page_table),
                "n_live": torch.empty(1, dtype=torch.int32, device=dev)}
         made = tuple(out.values())
     page_map = out.get("page_map")
-    _book(dev, out_refs=out["refs"], out_page_table=out["page_table"], n_live=out["n_live"], page_map=page_map)
+    _book(dev, "out_refs out_page_table n_live page_map", out["refs"], out["page_table"], out["n_live"], page_map)
     desc = _pool(k_pages, v_pages, page_table, page_table.shape[0], True)
     _shape("refs", refs, desc.num_pages)
     _shape("out refs", out["refs"], desc.num_pages)

@@ -172,11 +172,11 @@ __device__ float2 row_alone(const Args& a, const Span& sp, int b, int g, int64_t
     return make_float2(m, l);
 }
 
-// The keys straight from memory into the registers of the matrix
-// instructions: nothing is shared between waves, so there is no LDS and no
-// barrier in the key loop.  A workgroup's four waves take every fourth tile of
-// its keys (32 in bf16, 16 in fp32) and its 16 NB rows, and their states
-// (reference, sum, O) are joined through LDS at the end.
+// The keys from memory into the registers of the matrix instructions: nothing
+// is shared between waves, so there is no barrier in the key loop.  A
+// workgroup's four waves take every fourth tile of its keys (32 in bf16, 16 in
+// fp32) and its 16 NB rows, and their states (reference, sum, O) are joined
+// through LDS at the end.
 //
 // Scores are computed transposed, S^T = K Q^T with 16x16 instructions: lane
 // (t16, tq) takes key t16 of sixteen and 16 bytes of its row per step, and
@@ -185,33 +185,51 @@ __device__ float2 row_alone(const Args& a, const Span& sp, int b, int g, int64_t
 // just those keys, D / 16 neighbouring dims of each (so sixteen lanes read a
 // whole row), and the dims of an instruction are t16 * (D / 16) + t.  In fp32
 // that is the operand; in bf16 it takes one v_perm per pair of keys and dim.
+// K is read whole rows at a time too and turned through LDS, by each wave for
+// itself (chunks permuted: no bank conflicts): read as the instruction wants
+// it, 64 bytes of sixteen rows at a time, a long cache came at 5.65 TB/s, and
+// comes at 6.3 this way.
 //
 // The reference m of a row moves only when a score exceeds it by 8 (in log2
 // units), so that the common tile needs no reduction across lanes.
+//
+// ONCE: every key is read by one workgroup, past the caches (5.45 against 5.65
+// TB/s without).
 constexpr int kWaves = 4;
 
-template <bool BF16, int D, int NB>
-__global__ __launch_bounds__(kWaves * kWave, 2) void paged_attn_rows_kernel(Args a) {
+template <bool ONCE>
+__device__ __forceinline__ uint4 load16(const char* p) {
+    if constexpr (ONCE) return load_stream16(p);
+    return *reinterpret_cast<const uint4*>(p);
+}
+
+template <bool BF16, int D, int NB, bool ONCE>
+__global__ __launch_bounds__(kWaves * kWave, NB == 1 ? 3 : 2) void paged_attn_rows_kernel(Args a) {
     constexpr int E = BF16 ? 2 : 4;
     constexpr int KB = BF16 ? 2 : 1;  // 16-key groups per tile
     constexpr int T = 16 * KB;
-    constexpr int KC = D * E / 64;        // 16-byte chunks of a K row per lane
+    constexpr int KC = D * E / 64;        // 16-byte chunks of a K row per lane and operand
+    constexpr int CPR = D * E / 16;       // 16-byte chunks of a row
+    constexpr int KL = T * CPR / 64;      // loads of a K tile per lane
     constexpr int VD = D / 16;            // dims of a V row per lane
     constexpr int VW = VD * E / 4;        // the same in words
     constexpr int R = 16 * NB;            // rows of the workgroup
     constexpr int SD = D + 4;             // row stride of the states in LDS
     constexpr int NT = kWaves * kWave;
-    __shared__ __align__(16) float s_o[kWaves * R * SD];
+    __shared__ __align__(16) float s_o[kWaves * R * SD];  // a wave's part: its K tile first
+    static_assert(R * SD * 4 >= T * D * E, "a K tile fits");
     __shared__ float s_ml[2 * kWaves * R];
     __shared__ int s_bad[R];
 
-    // blocks: the last row block (the longest key range) first, neighbours
-    // differ in the KV head
+    // blocks: the last row block (the longest key range) first; neighbours
+    // differ in the split, so that an XCD (every eighth block) meets all KV
+    // heads: rows of one head alone fall on few of its L2's channels (5.65
+    // against 6.2 TB/s)
     int id = blockIdx.x;
-    const int g = id % a.hkv;
-    id /= a.hkv;
     const int split = id % a.splits;
     id /= a.splits;
+    const int g = id % a.hkv;
+    id /= a.hkv;
     const int b = id % a.batch;
     const int rev = id / a.batch;
     const Seq sq = seq_of(a, b);
@@ -271,16 +289,33 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void paged_attn_rows_kernel(Args
         const int64_t at = x.page[kb] < 0 ? 0 : x.page[kb] * a.page_stride + (int64_t)r * a.hkv * D;
         return pool + (at + g * D) * E;  // (page 0 stands for one that is not there)
     };
-    uint4 kf[KB][KC];
+    // K: load j covers rows j * 64 / CPR .. of the tile; row r's chunk c lies
+    // at c ^ swz(r) in LDS, and operand (key t16, chunk 4 i + tq) is read back
+    auto swz = [](int r) { return CPR == 8 ? (r >> 1) & 7 : r & 15; };
+    char* const s_k = reinterpret_cast<char*>(s_o + wave * R * SD);
+    uint4 kf[KL];
     uint32_t vf[4 * KB][VW];
+    const uint32_t k_off = (uint32_t)(lane / CPR * RS + lane % CPR * 16);
+    const uint32_t v_off = (uint32_t)(4 * tq * RS + t16 * VW * 4);
     auto load_k = [&](const Tile& x) {
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) {
             const char* p = group(a.kp, x, kb);
 #pragma unroll
-            for (int i = 0; i < KC; ++i)
-                kf[kb][i] = *reinterpret_cast<const uint4*>(p + (uint32_t)(t16 * RS + tq * 16 + i * 64));
+            for (int j = 0; j < KL / KB; ++j)
+                kf[kb * (KL / KB) + j] = load16<ONCE>(p + (int64_t)j * (64 / CPR) * RS + k_off);
         }
+    };
+    auto store_k = [&]() {
+#pragma unroll
+        for (int j = 0; j < KL; ++j) {
+            const int r = j * (64 / CPR) + lane / CPR;
+            *reinterpret_cast<uint4*>(s_k + r * (D * E) + ((lane % CPR) ^ swz(r)) * 16) = kf[j];
+        }
+    };
+    auto k_at = [&](int kb, int i) {
+        const int r = 16 * kb + t16;
+        return *reinterpret_cast<const uint4*>(s_k + r * (D * E) + ((4 * i + tq) ^ swz(r)) * 16);
     };
     auto load_v = [&](const Tile& x) {
 #pragma unroll
@@ -288,7 +323,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void paged_attn_rows_kernel(Args
             const char* p = group(a.vp, x, kb);
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                const char* pr = p + (uint32_t)((4 * tq + r) * RS + t16 * VW * 4);
+                const char* pr = p + (int64_t)r * RS + v_off;
                 if constexpr (VW == 2) {
                     const uint2 u = *reinterpret_cast<const uint2*>(pr);
                     vf[4 * kb + r][0] = u.x;
@@ -296,7 +331,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void paged_attn_rows_kernel(Args
                 } else {
 #pragma unroll
                     for (int w = 0; w < VW; w += 4) {
-                        const uint4 u = *reinterpret_cast<const uint4*>(pr + w * 4);
+                        const uint4 u = load16<ONCE>(pr + w * 4);
                         vf[4 * kb + r][w] = u.x;
                         vf[4 * kb + r][w + 1] = u.y;
                         vf[4 * kb + r][w + 2] = u.z;
@@ -327,21 +362,27 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void paged_attn_rows_kernel(Args
     }
     for (; t < t_end; t += kWaves) {
         const bool more = t + kWaves < t_end;
-        // ---- scores
+        // ---- scores (a wave's LDS accesses stay in order)
+        store_k();
+        if (more) load_k(nxt);
+        __builtin_amdgcn_wave_barrier();
         floatx4 S[NB][KB];
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-            for (int kb = 0; kb < KB; ++kb) {
-                S[nb][kb] = (floatx4){0.f, 0.f, 0.f, 0.f};
+            for (int kb = 0; kb < KB; ++kb) S[nb][kb] = (floatx4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int i = 0; i < KC; ++i) {
+        for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+            for (int i = 0; i < KC; ++i) {
+                const uint4 ku = k_at(kb, i);
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
                     if constexpr (BF16) {
                         S[nb][kb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                            __builtin_bit_cast(bf16x8, kf[kb][i]), __builtin_bit_cast(bf16x8, qf[nb][i]), S[nb][kb],
-                            0, 0, 0);
+                            __builtin_bit_cast(bf16x8, ku), __builtin_bit_cast(bf16x8, qf[nb][i]), S[nb][kb], 0, 0, 0);
                     } else {
-                        const floatx4 kv = __builtin_bit_cast(floatx4, kf[kb][i]);
+                        const floatx4 kv = __builtin_bit_cast(floatx4, ku);
                         const floatx4 qv = __builtin_bit_cast(floatx4, qf[nb][i]);
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
@@ -349,7 +390,7 @@ __global__ __launch_bounds__(kWaves * kWave, 2) void paged_attn_rows_kernel(Args
                     }
                 }
             }
-        if (more) load_k(nxt);
+        __builtin_amdgcn_wave_barrier();
 
         // ---- masks, on the tiles that need them
         bool edge = false;
@@ -946,53 +987,93 @@ __global__ __launch_bounds__(kTileWaves * kWave) void paged_attn_tiles_kernel(Ar
     }
 }
 
-// Joins the splits of a row: D / 4 lanes per row.  Splits past a sequence's
-// keys have written nothing.
+// Joins the splits of a row.  D / 4 lanes read a split's row; `parts` groups of
+// them share a row's splits and join theirs through LDS, so that all of a row's
+// partials are asked for at once (32 rows of 32 splits: 13.9 us with one group,
+// a memory round trip per eight splits).  Splits past a sequence's keys have
+// written nothing.
+constexpr int kMergeThreads = 256;
+
 template <bool BF16, int D, int T>
-__global__ __launch_bounds__(256) void paged_attn_merge_kernel(Args a, int rows_per_block) {
+__global__ __launch_bounds__(kMergeThreads) void paged_attn_merge_kernel(Args a, int rows_per_block, int parts) {
     constexpr int E = BF16 ? 2 : 4;
-    constexpr int LR = D / 4;  // lanes per row: 16 or 32
+    constexpr int LR = D / 4;  // lanes per row and part: 16 or 32
+    constexpr int GROUPS = kMergeThreads / LR;
+    __shared__ __align__(16) float s_acc[GROUPS][D];
+    __shared__ float s_ml[2][GROUPS];
     const int per_seq = a.max_q * a.hq;
-    const int64_t idx = (int64_t)blockIdx.x * (256 / LR) + threadIdx.x / LR;
-    const int ln = threadIdx.x % LR;
+    const int grp = threadIdx.x / LR, ln = threadIdx.x % LR, part = grp % parts;
+    const int64_t idx = (int64_t)blockIdx.x * (GROUPS / parts) + grp / parts;
     const int b = (int)(idx / per_seq), rest = (int)(idx % per_seq);
-    if (b >= a.batch) return;
-    const Seq sq = seq_of(a, b);
+    const bool in = b < a.batch;
+    const Seq sq = in ? seq_of(a, b) : Seq{0, 0, 0, false};
     const int tok = rest / a.hq, head = rest - tok * a.hq;
-    if (tok >= sq.n) return;
-    const int g = head / a.G, rho = tok * a.G + head - g * a.G;
-    const int row0 = rho / rows_per_block * rows_per_block;
-    const Span sp = span_of(a, sq.pos0 + row0 / a.G, sq.pos0 + (min(row0 + rows_per_block, sq.n * a.G) - 1) / a.G);
-    const int live = max(min(((sp.n + T - 1) / T + a.split_tiles - 1) / a.split_tiles, a.splits), 1);
-    const int64_t bg = (int64_t)b * a.hkv + g, all = (int64_t)a.G * a.max_q;
-    const float2* ml = a.part_ml + (bg * all + rho) * a.splits;
-    const float* po = a.part_o + (bg * a.splits * all + rho) * D + ln * 4;
-    float M = -INFINITY;
-    for (int s = ln; s < live; s += LR) M = fmaxf(M, ml[s].x);
-#pragma unroll
-    for (int o = LR / 2; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor(M, o, LR));
-    float L = 0.f;
+    const bool live_row = tok < sq.n;
+    float M = -INFINITY, L = 0.f;
     floatx4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int s0 = 0; s0 < live; s0 += 8) {
-        floatx4 v[8];
-        float w[8];
+    if (live_row) {
+        const int g = head / a.G, rho = tok * a.G + head - g * a.G;
+        const int row0 = rho / rows_per_block * rows_per_block;
+        const Span sp = span_of(a, sq.pos0 + row0 / a.G, sq.pos0 + (min(row0 + rows_per_block, sq.n * a.G) - 1) / a.G);
+        const int live = max(min(((sp.n + T - 1) / T + a.split_tiles - 1) / a.split_tiles, a.splits), 1);
+        const int64_t bg = (int64_t)b * a.hkv + g, all = (int64_t)a.G * a.max_q;
+        const float2* ml = a.part_ml + (bg * all + rho) * a.splits;
+        const float* po = a.part_o + (bg * a.splits * all + rho) * D + ln * 4;
+        for (int s0 = part; s0 < live; s0 += 4 * parts) {
+            floatx4 v[4];
+            float2 x[4];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int s = min(s0 + j, live - 1);
-            v[j] = *reinterpret_cast<const floatx4*>(po + (int64_t)s * all * D);
-            const float2 x = ml[s];
-            // a split in which the row sees nothing has sum 0
-            const bool part = s0 + j < live && x.y != 0.f;
-            w[j] = part ? x.y * __builtin_amdgcn_exp2f(x.x - M) : 0.f;
-            if (!part) v[j] = (floatx4){0.f, 0.f, 0.f, 0.f};
-        }
+            for (int j = 0; j < 4; ++j) {
+                const int s = min(s0 + j * parts, live - 1);
+                v[j] = *reinterpret_cast<const floatx4*>(po + (int64_t)s * all * D);
+                x[j] = ml[s];
+            }
+            // (a split in which the row sees nothing has reference -inf and sum 0)
+            float mn = M;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            L += w[j];
+            for (int j = 0; j < 4; ++j) mn = fmaxf(mn, x[j].x);
+            const float f = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - mn);
+            M = mn;
+            if (L != 0.f) {
+                L *= f;
+                acc *= f;
+            }
 #pragma unroll
-            for (int e = 0; e < 4; ++e) acc[e] = fmaf(w[j], v[j][e], acc[e]);
+            for (int j = 0; j < 4; ++j) {
+                if (s0 + j * parts >= live || x[j].y == 0.f) continue;
+                const float w = x[j].y * __builtin_amdgcn_exp2f(x[j].x - M);
+                L += w;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[e] = fmaf(w, v[j][e], acc[e]);
+            }
         }
     }
+    if (parts > 1) {
+        *reinterpret_cast<floatx4*>(&s_acc[grp][ln * 4]) = acc;
+        if (ln == 0) {
+            s_ml[0][grp] = M;
+            s_ml[1][grp] = L;
+        }
+        __syncthreads();
+        if (part != 0) return;
+        const float own = M;
+        for (int i = 1; i < parts; ++i) M = fmaxf(M, s_ml[0][grp + i]);
+        const float f = L == 0.f ? 0.f : __builtin_amdgcn_exp2f(own - M);
+        if (L != 0.f) {
+            L *= f;
+            acc *= f;
+        }
+        for (int i = 1; i < parts; ++i) {
+            const float l = s_ml[1][grp + i];
+            if (l == 0.f) continue;
+            const float w = __builtin_amdgcn_exp2f(s_ml[0][grp + i] - M);
+            L = fmaf(w, l, L);
+            const floatx4 v = *reinterpret_cast<const floatx4*>(&s_acc[grp + i][ln * 4]);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[e] = fmaf(w, v[e], acc[e]);
+        }
+    }
+    if (!live_row) return;
     const float inv = L == 0.f ? 0.f : 1.f / L;
     char* p = a.out + (((sq.r0 + tok) * a.hq + head) * D + ln * 4) * E;
     if constexpr (BF16)
@@ -1068,23 +1149,35 @@ PagedPlan paged_plan(const presto_paged_attn_desc* d) {
     return p;
 }
 
+template <bool BF16, int D, int NB>
+void launch_rows(const PagedPlan& p, const Args& a, hipStream_t stream) {
+    if (p.row_blocks == 1)
+        paged_attn_rows_kernel<BF16, D, NB, true><<<(unsigned)p.blocks, kWaves * kWave, 0, stream>>>(a);
+    else
+        paged_attn_rows_kernel<BF16, D, NB, false><<<(unsigned)p.blocks, kWaves * kWave, 0, stream>>>(a);
+}
+
 template <bool BF16, int D>
 void launch_attn(const PagedPlan& p, const Args& a, hipStream_t stream) {
     if (p.tiles) {
         if constexpr (BF16)
             paged_attn_tiles_kernel<D><<<(unsigned)p.blocks, kTileWaves * kWave, 0, stream>>>(a);
     } else if (p.nb == 1) {
-        paged_attn_rows_kernel<BF16, D, 1><<<(unsigned)p.blocks, kWaves * kWave, 0, stream>>>(a);
+        launch_rows<BF16, D, 1>(p, a, stream);
     } else {
-        paged_attn_rows_kernel<BF16, D, 2><<<(unsigned)p.blocks, kWaves * kWave, 0, stream>>>(a);
+        launch_rows<BF16, D, 2>(p, a, stream);
     }
     if (p.splits > 1) {
-        constexpr int T = BF16 ? 32 : 16;
-        const unsigned grid = (unsigned)cdiv((int64_t)a.batch * a.max_q * a.hq, 256 / (D / 4));
+        constexpr int T = BF16 ? 32 : 16, GROUPS = kMergeThreads / (D / 4);
+        // four splits or fewer per part
+        int parts = 1;
+        while (parts < GROUPS && parts * 4 < p.splits) parts *= 2;
+        const unsigned grid = (unsigned)cdiv((int64_t)a.batch * a.max_q * a.hq, GROUPS / parts);
         if (p.tiles)
-            paged_attn_merge_kernel<BF16, D, kKeyTile><<<grid, 256, 0, stream>>>(a, p.rows_per_block);
+            paged_attn_merge_kernel<BF16, D, kKeyTile>
+                <<<grid, kMergeThreads, 0, stream>>>(a, p.rows_per_block, parts);
         else
-            paged_attn_merge_kernel<BF16, D, T><<<grid, 256, 0, stream>>>(a, p.rows_per_block);
+            paged_attn_merge_kernel<BF16, D, T><<<grid, kMergeThreads, 0, stream>>>(a, p.rows_per_block, parts);
     }
 }
 

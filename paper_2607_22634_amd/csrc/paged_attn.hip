@@ -58,14 +58,21 @@ struct Args {
     const int32_t* ctx;
     const int32_t* q_off;  // null: one row per sequence
     char* out;
-    float* part_o;    // [b, g, split, rho, D] fp32, normalised by the split's own sum
-    float2* part_ml;  // [b, g, rho, split] (reference in log2 units, sum)
+    // partials: the output normalised by the part's own sum [part, rho, D] fp32
+    // and (reference in log2 units, sum) [part, rho]; part = (b, g, split), or
+    // (g, slot) with shares
+    float* part_o;
+    float2* part_ml;
     int32_t* flags;
     int64_t q_stride, page_stride;  // elements
     int64_t total_q;
     int32_t batch, hq, hkv, G, max_q, max_ctx, num_pages, max_pages, page_shift;
     int32_t window, sinks;
     int32_t row_blocks, splits, split_tiles;
+    // shares > 0: the tiles of all sequences are cut into that many equal
+    // shares; share c's part of sequence b is slot c + b < n_slots
+    int32_t shares, n_slots;
+    int2* slots;  // [batch] first and last slot of a sequence
     float scale_log2;  // scale * log2(e)
 };
 
@@ -193,18 +200,29 @@ __device__ float2 row_alone(const Args& a, const Span& sp, int b, int g, int64_t
 // The reference m of a row moves only when a score exceeds it by 8 (in log2
 // units), so that the common tile needs no reduction across lanes.
 //
-// ONCE: every key is read by one workgroup, past the caches (5.45 against 5.65
-// TB/s without).
+// kOnce: every key is read by one workgroup, past the caches (a long cache at
+// 5.45 TB/s through them, 5.65 past them).  kShares: the same, each workgroup
+// taking an equal share of all tiles of the batch (see below).
 constexpr int kWaves = 4;
+enum { kCached, kOnce, kShares };
 
-template <bool ONCE>
+template <int MODE>
 __device__ __forceinline__ uint4 load16(const char* p) {
-    if constexpr (ONCE) return load_stream16(p);
+    if constexpr (MODE != kCached) return load_stream16(p);
     return *reinterpret_cast<const uint4*>(p);
 }
 
-template <bool BF16, int D, int NB, bool ONCE>
-__global__ __launch_bounds__(kWaves * kWave, NB == 1 ? 3 : 2) void paged_attn_rows_kernel(Args a) {
+// Tiles of a sequence, at least one (so that some workgroup clears the rows of
+// an empty one).
+template <int T>
+__device__ __forceinline__ int share_tiles(const Args& a, int b) {
+    if (b >= a.batch) return 0;
+    const Seq sq = seq_of(a, b);
+    return max((span_of(a, sq.pos0, sq.pos0 + max(sq.n, 1) - 1).n + T - 1) / T, 1);
+}
+
+template <bool BF16, int D, int NB, int MODE>
+__global__ __launch_bounds__(kWaves * kWave, NB == 1 && MODE != kShares ? 3 : 2) void paged_attn_rows_kernel(Args a) {
     constexpr int E = BF16 ? 2 : 4;
     constexpr int KB = BF16 ? 2 : 1;  // 16-key groups per tile
     constexpr int T = 16 * KB;
@@ -221,32 +239,23 @@ __global__ __launch_bounds__(kWaves * kWave, NB == 1 ? 3 : 2) void paged_attn_ro
     __shared__ float s_ml[2 * kWaves * R];
     __shared__ int s_bad[R];
 
-    // blocks: the last row block (the longest key range) first; neighbours
-    // differ in the split, so that an XCD (every eighth block) meets all KV
-    // heads: rows of one head alone fall on few of its L2's channels (5.65
-    // against 6.2 TB/s)
-    int id = blockIdx.x;
-    const int split = id % a.splits;
-    id /= a.splits;
-    const int g = id % a.hkv;
-    id /= a.hkv;
-    const int b = id % a.batch;
-    const int rev = id / a.batch;
-    const Seq sq = seq_of(a, b);
-    const int rows = sq.n * a.G;
-    const int rb = (rows + R - 1) / R - 1 - rev;
-    const int tid = threadIdx.x, lane = lane_id();
+    const int tid = threadIdx.x;
     const int wave = uniform(tid / kWave);
-    if (rev == 0 && g == 0 && split == 0 && tid == 0 && sq.bad) raise_flag(a.flags, PRESTO_FLAG_BAD_SEQ);
-    if (rb < 0) return;
+
+    // Tiles t_begin .. t_end - 1 of a row block's keys, to part `part`, or
+    // with part < 0 (the block's only one) to the output.
+    auto segment = [&](int b, int g, const Seq& sq, int rb, int t_begin, int t_end, int64_t part)
+                       __attribute__((always_inline)) {
+    int lane = lane_id();
+    asm volatile("" : "+v"(lane));  // (what follows from it is not kept in registers from segment to segment)
+    const int rows = sq.n * a.G;
     const int row0 = rb * R;
     const int p_lo = sq.pos0 + row0 / a.G, p_hi = sq.pos0 + (min(row0 + R, rows) - 1) / a.G;
     const Span sp = span_of(a, p_lo, p_hi);
-    const int t_begin = split * a.split_tiles, t_end = min(t_begin + a.split_tiles, (sp.n + T - 1) / T);
-    if (split > 0 && t_begin >= t_end) return;  // the merge knows
+    t_end = min(t_end, (sp.n + T - 1) / T);
 
     const int t16 = lane & 15, tq = lane >> 4;
-    const int RS = a.hkv * D * E;  // bytes from a cache row to the next
+    const uint32_t RS = (uint32_t)(a.hkv * D * E);  // bytes from a cache row to the next
 
     // ---- queries, as the second operand: row t16, chunk i at byte 64 i + 16 tq
     uint4 qf[NB][KC];
@@ -295,15 +304,16 @@ __global__ __launch_bounds__(kWaves * kWave, NB == 1 ? 3 : 2) void paged_attn_ro
     char* const s_k = reinterpret_cast<char*>(s_o + wave * R * SD);
     uint4 kf[KL];
     uint32_t vf[4 * KB][VW];
-    const uint32_t k_off = (uint32_t)(lane / CPR * RS + lane % CPR * 16);
-    const uint32_t v_off = (uint32_t)(4 * tq * RS + t16 * VW * 4);
+    const uint32_t k_off = lane / CPR * RS + lane % CPR * 16;
+    const uint32_t v_off = 4 * tq * RS + t16 * VW * 4;
+    // (the steps from load to load go to the scalar base: in the offset they
+    // would cost a register each)
     auto load_k = [&](const Tile& x) {
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) {
             const char* p = group(a.kp, x, kb);
 #pragma unroll
-            for (int j = 0; j < KL / KB; ++j)
-                kf[kb * (KL / KB) + j] = load16<ONCE>(p + (int64_t)j * (64 / CPR) * RS + k_off);
+            for (int j = 0; j < KL / KB; ++j) kf[kb * (KL / KB) + j] = load16<MODE>(p + (int64_t)(j * (64 / CPR)) * RS + k_off);
         }
     };
     auto store_k = [&]() {
@@ -331,7 +341,7 @@ __global__ __launch_bounds__(kWaves * kWave, NB == 1 ? 3 : 2) void paged_attn_ro
                 } else {
 #pragma unroll
                     for (int w = 0; w < VW; w += 4) {
-                        const uint4 u = load16<ONCE>(pr + w * 4);
+                        const uint4 u = load16<MODE>(pr + w * 4);
                         vf[4 * kb + r][w] = u.x;
                         vf[4 * kb + r][w + 1] = u.y;
                         vf[4 * kb + r][w + 2] = u.z;
@@ -508,10 +518,10 @@ __global__ __launch_bounds__(kWaves * kWave, NB == 1 ? 3 : 2) void paged_attn_ro
     if (tid < R) s_bad[tid] = 0;
     __syncthreads();
 
-    const int64_t bg = (int64_t)b * a.hkv + g, all = (int64_t)a.G * a.max_q;
+    const int64_t prow = part * a.G * a.max_q;
     auto put = [&](int rho, int d, floatx4 v) {
-        if (a.splits > 1) {
-            *reinterpret_cast<floatx4*>(a.part_o + ((bg * a.splits + split) * all + rho) * D + d) = v;
+        if (part >= 0) {
+            *reinterpret_cast<floatx4*>(a.part_o + (prow + rho) * D + d) = v;
             return;
         }
         const int tok = rho / a.G, h = rho - tok * a.G;
@@ -522,7 +532,7 @@ __global__ __launch_bounds__(kWaves * kWave, NB == 1 ? 3 : 2) void paged_attn_ro
             *reinterpret_cast<floatx4*>(p) = v;
     };
     auto put_ml = [&](int rho, float M, float L) {
-        if (a.splits > 1) a.part_ml[(bg * all + rho) * a.splits + split] = make_float2(M, L);
+        if (part >= 0) a.part_ml[prow + rho] = make_float2(M, L);
     };
     bool bad = false;
     for (int i = tid; i < R * (D / 4); i += NT) {
@@ -568,6 +578,72 @@ __global__ __launch_bounds__(kWaves * kWave, NB == 1 ? 3 : 2) void paged_attn_ro
                                              t_begin * T, t_end * T, s_o + D, s_o + 2 * D, s_o + 2 * D + NT, s_acc);
         for (int d = tid * 4; d < D; d += NT * 4) put(rho, d, *reinterpret_cast<const floatx4*>(&s_acc[d]));
         if (tid == 0) put_ml(rho, ml.x, ml.y);
+    }
+    };
+
+    // Neighbouring blocks differ in the split or share, so that an XCD (every
+    // eighth block) meets all KV heads: rows of one head alone fall on few of
+    // its L2's channels (a long cache at 5.65 against 6.2 TB/s).
+    int id = blockIdx.x;
+    if constexpr (MODE != kShares) {
+        // the last row block (the longest key range) first
+        const int split = id % a.splits;
+        id /= a.splits;
+        const int g = id % a.hkv;
+        id /= a.hkv;
+        const int b = id % a.batch, rev = id / a.batch;
+        const Seq sq = seq_of(a, b);
+        const int rb = (sq.n * a.G + R - 1) / R - 1 - rev;
+        if (rev == 0 && g == 0 && split == 0 && tid == 0 && sq.bad) raise_flag(a.flags, PRESTO_FLAG_BAD_SEQ);
+        if (rb < 0) return;
+        if (split > 0) {
+            const int row0 = rb * R;
+            const Span sp = span_of(a, sq.pos0 + row0 / a.G, sq.pos0 + (min(row0 + R, sq.n * a.G) - 1) / a.G);
+            if (split * a.split_tiles * T >= sp.n) return;  // the merge knows
+        }
+        segment(b, g, sq, rb, split * a.split_tiles, (split + 1) * a.split_tiles,
+                a.splits > 1 ? ((int64_t)b * a.hkv + g) * a.splits + split : -1);
+    } else {
+        // a share: part of one sequence, or the end of one, whole ones and the
+        // start of another; it and the sequence never advance together past a
+        // boundary, so share + sequence numbers the parts
+        const int lane = lane_id();
+        const int share = id % a.shares, g = id / a.shares;
+        int total = 0;
+        for (int b0 = 0; b0 < a.batch; b0 += kWave)
+            total += __builtin_amdgcn_readlane((int)wave_scan_dpp(share_tiles<T>(a, b0 + lane)), kWave - 1);
+        const int shares = min(a.shares, (total + kWaves - 1) / kWaves);  // a tile per wave at least
+        if (share >= shares) return;
+        const int q = total / shares, r = total % shares;
+        int from = share * q + min(share, r), base = 0, b = 0;
+        const int to = from + q + (share < r ? 1 : 0);
+        for (int b0 = 0; b0 < a.batch; b0 += kWave) {
+            const int n = share_tiles<T>(a, b0 + lane), incl = (int)wave_scan_dpp(n);
+            const uint64_t hit = __ballot(base + incl > from);
+            if (hit) {
+                const int at = __ffsll((unsigned long long)hit) - 1;
+                b = b0 + at;
+                base += __builtin_amdgcn_readlane(incl - n, at);
+                break;
+            }
+            base += __builtin_amdgcn_readlane(incl, kWave - 1);
+        }
+        for (bool first = true; b < a.batch; ++b, first = false) {
+            if (!first) __syncthreads();  // the states in LDS have been read
+            const int tiles = uniform(share_tiles<T>(a, b));
+            const Seq sq = seq_of(a, b);
+            const int t0 = from - base, t1 = min(to - base, tiles);
+            const bool whole = t0 == 0 && t1 == tiles;
+            if (g == 0 && tid == 0) {
+                if (t0 == 0 && sq.bad) raise_flag(a.flags, PRESTO_FLAG_BAD_SEQ);
+                if (t0 == 0) a.slots[b].x = share + b;
+                if (t1 == tiles) a.slots[b].y = share + b;
+            }
+            if (sq.n > 0) segment(b, g, sq, 0, t0, t1, whole ? -1 : (int64_t)g * a.n_slots + share + b);
+            if (base + tiles >= to) return;
+            base += tiles;
+            from = base;
+        }
     }
 }
 
@@ -650,7 +726,7 @@ __global__ __launch_bounds__(kTileWaves * kWave) void paged_attn_tiles_kernel(Ar
     const Span sp = span_of(a, sq.pos0 + row0 / a.G, sq.pos0 + (row_end - 1) / a.G);
     const int t_begin = split * a.split_tiles, t_end = min(t_begin + a.split_tiles, (sp.n + T - 1) / T);
     if (split > 0 && t_begin >= t_end) return;  // the merge knows
-    const int64_t bg = (int64_t)b * a.hkv + g, all = (int64_t)a.G * a.max_q;
+    const int64_t prow = (((int64_t)b * a.hkv + g) * a.splits + split) * a.G * a.max_q;
 
     const int l32 = lane & 31, h = lane >> 5;
     const int wrow0 = row0 + wave * 32;  // this wave's first row
@@ -933,7 +1009,7 @@ __global__ __launch_bounds__(kTileWaves * kWave) void paged_attn_tiles_kernel(Ar
         const int tk = r / a.G;
         return reinterpret_cast<uint16_t*>(a.out) + ((sq.r0 + tk) * a.hq + g * a.G + r - tk * a.G) * D;
     };
-    auto part_row = [&](int r) { return a.part_o + ((bg * a.splits + split) * all + r) * D; };
+    auto part_row = [&](int r) { return a.part_o + (prow + r) * D; };
     bool bad = skip;
     if (rho < rows && !skip) {
         const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
@@ -965,7 +1041,7 @@ __global__ __launch_bounds__(kTileWaves * kWave) void paged_attn_tiles_kernel(Ar
                 for (int q4 = 0; q4 < 4; ++q4)
                     *reinterpret_cast<floatx4*>(op + db * 32 + 8 * q4 + 4 * h) =
                         (floatx4){o[db][4 * q4], o[db][4 * q4 + 1], o[db][4 * q4 + 2], o[db][4 * q4 + 3]};
-            if (h == 0) a.part_ml[(bg * all + rho) * a.splits + split] = make_float2(l_run == 0.f ? -INFINITY : m * c, l_run);
+            if (h == 0) a.part_ml[prow + rho] = make_float2(l_run == 0.f ? -INFINITY : m * c, l_run);
         }
     }
     // ---- rows whose sums are not all finite: a key that only others see may
@@ -983,7 +1059,7 @@ __global__ __launch_bounds__(kTileWaves * kWave) void paged_attn_tiles_kernel(Ar
             else
                 *reinterpret_cast<float2*>(part_row(rr) + 2 * d) = make_float2(f[2 * d], f[2 * d + 1]);
         }
-        if (tid == 0 && a.splits > 1) a.part_ml[(bg * all + rr) * a.splits + split] = ml;
+        if (tid == 0 && a.splits > 1) a.part_ml[prow + rr] = ml;
     }
 }
 
@@ -1009,24 +1085,35 @@ __global__ __launch_bounds__(kMergeThreads) void paged_attn_merge_kernel(Args a,
     const Seq sq = in ? seq_of(a, b) : Seq{0, 0, 0, false};
     const int tok = rest / a.hq, head = rest - tok * a.hq;
     const bool live_row = tok < sq.n;
+    int live = 1;
     float M = -INFINITY, L = 0.f;
     floatx4 acc = {0.f, 0.f, 0.f, 0.f};
     if (live_row) {
         const int g = head / a.G, rho = tok * a.G + head - g * a.G;
-        const int row0 = rho / rows_per_block * rows_per_block;
-        const Span sp = span_of(a, sq.pos0 + row0 / a.G, sq.pos0 + (min(row0 + rows_per_block, sq.n * a.G) - 1) / a.G);
-        const int live = max(min(((sp.n + T - 1) / T + a.split_tiles - 1) / a.split_tiles, a.splits), 1);
-        const int64_t bg = (int64_t)b * a.hkv + g, all = (int64_t)a.G * a.max_q;
-        const float2* ml = a.part_ml + (bg * all + rho) * a.splits;
-        const float* po = a.part_o + (bg * a.splits * all + rho) * D + ln * 4;
-        for (int s0 = part; s0 < live; s0 += 4 * parts) {
+        const int64_t all = (int64_t)a.G * a.max_q;
+        int64_t first;
+        if (a.shares > 0) {
+            const int2 s = a.slots[b];
+            first = (int64_t)g * a.n_slots + s.x;
+            live = s.y - s.x + 1;
+        } else {
+            const int row0 = rho / rows_per_block * rows_per_block;
+            const Span sp =
+                span_of(a, sq.pos0 + row0 / a.G, sq.pos0 + (min(row0 + rows_per_block, sq.n * a.G) - 1) / a.G);
+            first = ((int64_t)b * a.hkv + g) * a.splits;
+            live = max(min(((sp.n + T - 1) / T + a.split_tiles - 1) / a.split_tiles, a.splits), 1);
+        }
+        const int64_t prow = first * all + rho;
+        const float2* ml = a.part_ml + prow;
+        const float* po = a.part_o + prow * D + ln * 4;
+        for (int s0 = part; s0 < (a.shares > 0 && live == 1 ? 0 : live); s0 += 4 * parts) {
             floatx4 v[4];
             float2 x[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int s = min(s0 + j * parts, live - 1);
                 v[j] = *reinterpret_cast<const floatx4*>(po + (int64_t)s * all * D);
-                x[j] = ml[s];
+                x[j] = ml[s * all];
             }
             // (a split in which the row sees nothing has reference -inf and sum 0)
             float mn = M;
@@ -1073,7 +1160,7 @@ __global__ __launch_bounds__(kMergeThreads) void paged_attn_merge_kernel(Args a,
             for (int e = 0; e < 4; ++e) acc[e] = fmaf(w, v[e], acc[e]);
         }
     }
-    if (!live_row) return;
+    if (!live_row || (a.shares > 0 && live == 1)) return;  // (written by the one share that held it)
     const float inv = L == 0.f ? 0.f : 1.f / L;
     char* p = a.out + (((sq.r0 + tok) * a.hq + head) * D + ln * 4) * E;
     if constexpr (BF16)
@@ -1096,9 +1183,9 @@ namespace {
 struct PagedPlan {
     bool tiles;      // the kernel of 256-row workgroups
     int nb;          // else: 16-row blocks per workgroup
-    int rows_per_block, row_blocks, splits, split_tiles;
+    int rows_per_block, row_blocks, splits, split_tiles, shares, n_slots;
     int64_t blocks;
-    size_t o_bytes, bytes;
+    size_t o_bytes, ml_bytes, bytes;
 };
 
 int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
@@ -1140,21 +1227,59 @@ PagedPlan paged_plan(const presto_paged_attn_desc* d) {
     if (per > tiles) per = tiles;
     p.splits = (int)cdiv(tiles, per);
     p.split_tiles = (int)per;
-    p.blocks = all * p.splits;
-    if (p.splits > 1) {
-        const int64_t parts = (int64_t)d->pages.batch * d->pages.hkv * p.splits * rows;
-        p.o_bytes = (size_t)parts * d->pages.head_dim * sizeof(float);
-        p.bytes = p.o_bytes + (size_t)parts * sizeof(float2);
+    int64_t parts = all / p.row_blocks * p.splits;
+    if (!p.tiles && p.row_blocks == 1) {
+        // Decoding is a stream of the cache: what counts is that all CUs end
+        // together, and few launches.
+        // * Sequences of up to three tiles per wave are not cut (no merge:
+        //   384 keys 8.8 against 11.5 us).
+        // * Sequences of about one length (known from total_ctx) are cut into
+        //   as many splits as the chip holds workgroups at once, three per CU
+        //   by registers at head_dim 128 (two where there are 32 rows): 32 x
+        //   2048 keys in 3 splits 48 us, in 6 52; 80 x 2048 uncut 114, in 2
+        //   splits 143.
+        // * Others, and those that would leave much of a last round empty, in
+        //   equal shares: 24 sequences of 200 .. 12000 keys 157 us in splits,
+        //   100 in shares.  16 x 32768 in shares 328, in 6 splits 322: shares
+        //   take more registers, two workgroups per CU, and two such rounds.
+        const int wgs = 256 * (d->pages.head_dim == 64 ? (p.nb == 1 ? 4 : 3) : (p.nb == 1 ? 3 : 2));
+        p.splits = all < wgs ? (int)(wgs / all) : 1;
+        p.split_tiles = (int)(cdiv(cdiv(tiles, p.splits), kWaves) * kWaves);
+        if (tiles <= 3 * kWaves) p.split_tiles = (int)tiles;
+        p.splits = (int)cdiv(tiles, p.split_tiles);
+        const bool even = d->total_ctx > 0 && 10 * mean >= 9 * longest;
+        const bool idle = all > wgs && cdiv(all, wgs) * wgs * 7 > all * 8;
+        // (every workgroup looks through the batch for its share)
+        const bool can = d->pages.batch <= 2048 && d->pages.batch * tiles < ((int64_t)1 << 30);
+        if (tiles > 3 * kWaves && (!even || idle) && can) {
+            p.shares = 1024 / d->pages.hkv > 0 ? 1024 / d->pages.hkv : 1;
+            p.n_slots = p.shares + d->pages.batch;
+            p.blocks = (int64_t)p.shares * d->pages.hkv;
+            parts = (int64_t)d->pages.hkv * p.n_slots;
+        } else {
+            p.blocks = all * p.splits;
+            parts = all * p.splits;
+        }
+    } else {
+        p.blocks = all * p.splits;
+    }
+    if (p.splits > 1 || p.shares > 0) {
+        p.o_bytes = (size_t)(parts * rows) * d->pages.head_dim * sizeof(float);
+        p.ml_bytes = (size_t)(parts * rows) * sizeof(float2);
+        p.bytes = p.o_bytes + p.ml_bytes + (p.shares ? (size_t)d->pages.batch * sizeof(int2) : 0);
     }
     return p;
 }
 
 template <bool BF16, int D, int NB>
 void launch_rows(const PagedPlan& p, const Args& a, hipStream_t stream) {
-    if (p.row_blocks == 1)
-        paged_attn_rows_kernel<BF16, D, NB, true><<<(unsigned)p.blocks, kWaves * kWave, 0, stream>>>(a);
+    const unsigned grid = (unsigned)p.blocks;
+    if (p.shares > 0)
+        paged_attn_rows_kernel<BF16, D, NB, kShares><<<grid, kWaves * kWave, 0, stream>>>(a);
+    else if (p.row_blocks == 1)
+        paged_attn_rows_kernel<BF16, D, NB, kOnce><<<grid, kWaves * kWave, 0, stream>>>(a);
     else
-        paged_attn_rows_kernel<BF16, D, NB, false><<<(unsigned)p.blocks, kWaves * kWave, 0, stream>>>(a);
+        paged_attn_rows_kernel<BF16, D, NB, kCached><<<grid, kWaves * kWave, 0, stream>>>(a);
 }
 
 template <bool BF16, int D>
@@ -1167,11 +1292,12 @@ void launch_attn(const PagedPlan& p, const Args& a, hipStream_t stream) {
     } else {
         launch_rows<BF16, D, 2>(p, a, stream);
     }
-    if (p.splits > 1) {
+    if (p.splits > 1 || p.shares > 0) {
         constexpr int T = BF16 ? 32 : 16, GROUPS = kMergeThreads / (D / 4);
         // four splits or fewer per part
         int parts = 1;
-        while (parts < GROUPS && parts * 4 < p.splits) parts *= 2;
+        const int each = p.shares ? p.shares / a.batch + 2 : p.splits;
+        while (parts < GROUPS && parts * 4 < each) parts *= 2;
         const unsigned grid = (unsigned)cdiv((int64_t)a.batch * a.max_q * a.hq, GROUPS / parts);
         if (p.tiles)
             paged_attn_merge_kernel<BF16, D, kKeyTile>
@@ -1224,6 +1350,9 @@ presto_status launch_paged_attn(const presto_paged_attn_desc* d, const void* q, 
     a.row_blocks = p.row_blocks;
     a.splits = p.splits;
     a.split_tiles = p.split_tiles;
+    a.shares = p.shares;
+    a.n_slots = p.n_slots;
+    a.slots = reinterpret_cast<int2*>(static_cast<char*>(ws) + p.o_bytes + p.ml_bytes);
     a.scale_log2 = d->scale * kLog2e;
     const bool bf16 = d->pages.dt == PRESTO_DT_BF16;
     if (d->pages.head_dim == 128)

@@ -691,6 +691,14 @@ __device__ __forceinline__ void lds_load16(const void* base, uint32_t off, uint3
     asm volatile("global_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(sb), "{m0}"(m0v) : "memory");
 }
 
+// A barrier for what is in LDS: loads and stores of global memory stay on their
+// way across it.
+__device__ __forceinline__ void lds_barrier() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
 template <int D>
 __global__ __launch_bounds__(kTileWaves * kWave) void paged_attn_tiles_kernel(Args a) {
     constexpr int T = kKeyTile;
@@ -705,7 +713,7 @@ __global__ __launch_bounds__(kTileWaves * kWave) void paged_attn_tiles_kernel(Ar
     static_assert(LPT * RPL == 8, "a wave loads eight rows of a tile");
     __shared__ __align__(16) char s_kv[2 * kRing * kTile];
     __shared__ int32_t s_page[kTilePages];
-    __shared__ int s_bad[kTileRows];
+    __shared__ int s_bad[kTileRows], s_any;
 
     int id = blockIdx.x;
     const int g = id % a.hkv;
@@ -737,6 +745,19 @@ __global__ __launch_bounds__(kTileWaves * kWave) void paged_attn_tiles_kernel(Ar
     const int p_lo = uniform(sq.pos0 + min(wrow0, rows - 1) / a.G);
     const int p_hi = uniform(sq.pos0 + min(wrow0 + 31, rows - 1) / a.G);
     const float c = a.scale_log2;
+    // ---- page numbers: those of the entries before the gap, then of the others
+    const int va = t_begin * T, va_end = min(sp.head, t_end * T);
+    const int pa = va >> a.page_shift;
+    const int na = va < va_end ? ((va_end - 1) >> a.page_shift) - pa + 1 : 0;
+    const int kb = max(va, sp.head) + sp.gap, kb_end = min(sp.hi, t_end * T + sp.gap);
+    const int pb = kb >> a.page_shift;
+    const int nb = kb < kb_end ? ((kb_end - 1) >> a.page_shift) - pb + 1 : 0;
+    // (the first number of each thread is asked for before the queries, so that
+    // waiting for it leaves them on their way)
+    const int32_t* trow = a.table + (int64_t)b * a.max_pages;
+    const int pages = min(na + nb, kTilePages);
+    auto column = [&](int i) { return i < na ? pa + i : pb + i - na; };
+    const int first_page = tid < pages ? trow[column(tid)] : 0;
     // queries, second operand of S^T: row l32, dims ks * 16 + h * 8 ..
     bf16x8 qf[KS];
     {
@@ -745,35 +766,27 @@ __global__ __launch_bounds__(kTileWaves * kWave) void paged_attn_tiles_kernel(Ar
         for (int ks = 0; ks < KS; ++ks)
             qf[ks] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const uint4*>(qp + ks * 32));
     }
-
-    // ---- page numbers: those of the entries before the gap, then of the others
-    const int va = t_begin * T, va_end = min(sp.head, t_end * T);
-    const int pa = va >> a.page_shift;
-    const int na = va < va_end ? ((va_end - 1) >> a.page_shift) - pa + 1 : 0;
-    const int kb = max(va, sp.head) + sp.gap, kb_end = min(sp.hi, t_end * T + sp.gap);
-    const int pb = kb >> a.page_shift;
-    const int nb = kb < kb_end ? ((kb_end - 1) >> a.page_shift) - pb + 1 : 0;
-    {
-        bool bad = na + nb > kTilePages;  // (the host's choice of splits rules it out)
-        const int32_t* trow = a.table + (int64_t)b * a.max_pages;
-        for (int i = tid; i < min(na + nb, kTilePages); i += NT) {
-            const int x = i < na ? pa + i : pb + i - na;
-            const int k0 = max(x << a.page_shift, i < na ? va : kb), k1 = min((x + 1) << a.page_shift, kb_end);
-            const bool wanted = k0 < a.sinks || (i >= na && k1 > sp.lo);
-            const int page = wanted ? trow[x] : 0;
-            const bool ok = (uint32_t)page < (uint32_t)a.num_pages;
-            bad |= !ok;
-            s_page[i] = ok ? page : 0;
-        }
-        if (tid < kTileRows) s_bad[tid] = 0;
-        if (__syncthreads_or(bad)) {
-            // a page that is not there: its keys are left out, row by row
-            if (tid == 0) raise_flag(a.flags, PRESTO_FLAG_BAD_PAGE);
-            if (tid < row_end - row0) s_bad[tid] = 1;
-        }
+    bool bad_page = na + nb > kTilePages;  // (the host's choice of splits rules it out)
+    for (int i = tid; i < pages; i += NT) {
+        const int x = column(i);
+        const int k0 = max(x << a.page_shift, i < na ? va : kb), k1 = min((x + 1) << a.page_shift, kb_end);
+        const bool wanted = k0 < a.sinks || (i >= na && k1 > sp.lo);
+        const int page = !wanted ? 0 : i == tid ? first_page : trow[x];
+        const bool ok = (uint32_t)page < (uint32_t)a.num_pages;
+        bad_page |= !ok;
+        s_page[i] = ok ? page : 0;
     }
-    __syncthreads();
-    const bool skip = s_bad[0] != 0;
+    if (tid < kTileRows) s_bad[tid] = 0;
+    if (tid == 0) s_any = 0;
+    lds_barrier();
+    if (bad_page) s_any = 1;
+    lds_barrier();
+    const bool skip = s_any != 0;
+    if (skip) {
+        // a page that is not there: its keys are left out, row by row
+        if (tid == 0) raise_flag(a.flags, PRESTO_FLAG_BAD_PAGE);
+        if (tid < row_end - row0) s_bad[tid] = 1;
+    }
 
     floatx16 o[DB];
 #pragma unroll
@@ -983,7 +996,7 @@ __global__ __launch_bounds__(kTileWaves * kWave) void paged_attn_tiles_kernel(Ar
         load_tile(t_begin + 1, 1);
         load_tile(t_begin + 2, 2);
         PRESTO_WAIT_VM(2 * LPT);  // (the queries too: they were asked for first)
-        __syncthreads();
+        lds_barrier();
         if (active) {
             using B0 = std::integral_constant<int, 0>;
             floatx16 S0 = negm;
@@ -1005,48 +1018,56 @@ __global__ __launch_bounds__(kTileWaves * kWave) void paged_attn_tiles_kernel(Ar
     }
 
     // ---- lane: row rho, dims db * 32 + 8 q4 + 4 h + 0 .. 3
+    const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
+    bool fine = true;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            o[db][e] *= inv;
+            fine &= fabsf(o[db][e]) < INFINITY;
+        }
+    if (!fine && rho < rows) {
+        s_bad[rho - row0] = 1;
+        s_any = 1;
+    }
+    lds_barrier();  // (the ring is free, too)
+    const bool any = s_any != 0;
     auto out_row = [&](int r) {
         const int tk = r / a.G;
         return reinterpret_cast<uint16_t*>(a.out) + ((sq.r0 + tk) * a.hq + g * a.G + r - tk * a.G) * D;
     };
     auto part_row = [&](int r) { return a.part_o + (prow + r) * D; };
-    bool bad = skip;
-    if (rho < rows && !skip) {
-        const float inv = l_run == 0.f ? 0.f : 1.f / l_run;
-        bool fine = true;
+    if (a.splits == 1) {
+        // through this wave's part of the ring: whole rows, 16 bytes per lane
+        char* const w = s_kv + wave * (32 * D * 2);
+        static_assert(kTileWaves * 32 * D * 2 <= 2 * kRing * kTile, "the rows fit");
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                o[db][e] *= inv;
-                fine &= fabsf(o[db][e]) < INFINITY;
-            }
-        if (!fine) {
-            s_bad[rho - row0] = 1;
-            bad = true;
+            for (int q4 = 0; q4 < 4; ++q4)
+                *reinterpret_cast<uint2*>(w + l32 * (D * 2) + (((4 * db + q4) ^ (l32 & (CH - 1))) * 16 + 8 * h)) =
+                    make_uint2(pack2(o[db][4 * q4], o[db][4 * q4 + 1]), pack2(o[db][4 * q4 + 2], o[db][4 * q4 + 3]));
+        __builtin_amdgcn_wave_barrier();  // (a wave's LDS accesses stay in order)
+#pragma unroll
+        for (int j = 0; j < 32 / RPL; ++j) {
+            const int r = j * RPL + lane / CH, ck = lane % CH;
+            const uint4 u = *reinterpret_cast<const uint4*>(w + r * (D * 2) + ((ck ^ (r & (CH - 1))) * 16));
+            if (wrow0 + r < rows) *reinterpret_cast<uint4*>(out_row(wrow0 + r) + ck * 8) = u;
         }
-        if (a.splits == 1) {
-            uint16_t* op = out_row(rho);
+    } else if (rho < rows) {
+        float* op = part_row(rho);
 #pragma unroll
-            for (int db = 0; db < DB; ++db)
+        for (int db = 0; db < DB; ++db)
 #pragma unroll
-                for (int q4 = 0; q4 < 4; ++q4)
-                    *reinterpret_cast<uint2*>(op + db * 32 + 8 * q4 + 4 * h) =
-                        make_uint2(pack2(o[db][4 * q4], o[db][4 * q4 + 1]), pack2(o[db][4 * q4 + 2], o[db][4 * q4 + 3]));
-        } else {
-            float* op = part_row(rho);
-#pragma unroll
-            for (int db = 0; db < DB; ++db)
-#pragma unroll
-                for (int q4 = 0; q4 < 4; ++q4)
-                    *reinterpret_cast<floatx4*>(op + db * 32 + 8 * q4 + 4 * h) =
-                        (floatx4){o[db][4 * q4], o[db][4 * q4 + 1], o[db][4 * q4 + 2], o[db][4 * q4 + 3]};
-            if (h == 0) a.part_ml[prow + rho] = make_float2(l_run == 0.f ? -INFINITY : m * c, l_run);
-        }
+            for (int q4 = 0; q4 < 4; ++q4)
+                *reinterpret_cast<floatx4*>(op + db * 32 + 8 * q4 + 4 * h) =
+                    (floatx4){o[db][4 * q4], o[db][4 * q4 + 1], o[db][4 * q4 + 2], o[db][4 * q4 + 3]};
+        if (h == 0) a.part_ml[prow + rho] = make_float2(l_run == 0.f ? -INFINITY : m * c, l_run);
     }
     // ---- rows whose sums are not all finite: a key that only others see may
-    // be the cause
-    if (!__syncthreads_or(bad)) return;
+    // be the cause; or all rows, where a page is not there
+    if (!any) return;
     float* const f = reinterpret_cast<float*>(s_kv);
     for (int r = 0; r < row_end - row0; ++r) {
         if (!s_bad[r]) continue;

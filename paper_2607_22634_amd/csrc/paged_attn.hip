@@ -68,7 +68,8 @@ struct Args {
     int64_t total_q;
     int32_t batch, hq, hkv, G, max_q, max_ctx, num_pages, max_pages, page_shift;
     int32_t window, sinks;
-    int32_t row_blocks, splits, split_tiles;
+    int32_t row_blocks, block_rows, splits, split_tiles;
+    int32_t by_sequence;
     // shares > 0: the tiles of all sequences are cut into that many equal
     // shares; share c's part of sequence b is slot c + b < n_slots
     int32_t shares, n_slots;
@@ -715,22 +716,27 @@ __global__ __launch_bounds__(kTileWaves * kWave) void paged_attn_tiles_kernel(Ar
     __shared__ int32_t s_page[kTilePages];
     __shared__ int s_bad[kTileRows], s_any;
 
+    // Blocks: neighbours differ in the KV head, so that the row blocks of one
+    // head, which read the same keys, meet in the L2 of one XCD (every eighth
+    // block).  The last row block (the longest key range) first, of all
+    // sequences; or one sequence after the other where the keys of a head do
+    // not fit an L2 (see the host).
     int id = blockIdx.x;
     const int g = id % a.hkv;
     id /= a.hkv;
     const int split = id % a.splits;
     id /= a.splits;
-    const int b = id % a.batch;
-    const int rev = id / a.batch;
+    const int b = a.by_sequence ? id / a.row_blocks : id % a.batch;
+    const int rev = a.by_sequence ? id % a.row_blocks : id / a.batch;
     const Seq sq = seq_of(a, b);
     const int rows = sq.n * a.G;
-    const int rb = (rows + kTileRows - 1) / kTileRows - 1 - rev;
+    const int rb = (rows + a.block_rows - 1) / a.block_rows - 1 - rev;
     const int tid = threadIdx.x, lane = lane_id();
     const int wave = uniform(tid / kWave);
     if (rev == 0 && g == 0 && split == 0 && tid == 0 && sq.bad) raise_flag(a.flags, PRESTO_FLAG_BAD_SEQ);
     if (rb < 0) return;
-    const int row0 = rb * kTileRows;
-    const int row_end = min(row0 + kTileRows, rows);
+    const int row0 = rb * a.block_rows;  // (a multiple of 32, at most kTileRows)
+    const int row_end = min(row0 + a.block_rows, rows);
     const Span sp = span_of(a, sq.pos0 + row0 / a.G, sq.pos0 + (row_end - 1) / a.G);
     const int t_begin = split * a.split_tiles, t_end = min(t_begin + a.split_tiles, (sp.n + T - 1) / T);
     if (split > 0 && t_begin >= t_end) return;  // the merge knows
@@ -739,11 +745,11 @@ __global__ __launch_bounds__(kTileWaves * kWave) void paged_attn_tiles_kernel(Ar
     const int l32 = lane & 31, h = lane >> 5;
     const int wrow0 = row0 + wave * 32;  // this wave's first row
     const int rho = wrow0 + l32;
-    const int rq = min(rho, rows - 1);
+    const int rq = min(rho, row_end - 1);
     const int tok = rq / a.G, qh = rq - tok * a.G;
     const int pos = sq.pos0 + tok;
-    const int p_lo = uniform(sq.pos0 + min(wrow0, rows - 1) / a.G);
-    const int p_hi = uniform(sq.pos0 + min(wrow0 + 31, rows - 1) / a.G);
+    const int p_lo = uniform(sq.pos0 + min(wrow0, row_end - 1) / a.G);
+    const int p_hi = uniform(sq.pos0 + min(wrow0 + 31, row_end - 1) / a.G);
     const float c = a.scale_log2;
     // ---- page numbers: those of the entries before the gap, then of the others
     const int va = t_begin * T, va_end = min(sp.head, t_end * T);
@@ -852,7 +858,7 @@ __global__ __launch_bounds__(kTileWaves * kWave) void paged_attn_tiles_kernel(Ar
         // position
         const int ntiles = t_end - t_begin;
         const int nblocks = (min(min(p_hi + 1 - sp.gap, sp.n), t_end * T) - t_begin * T + 31) / 32;
-        const bool active = wrow0 < rows && nblocks > 0;
+        const bool active = wrow0 < row_end && nblocks > 0;
 
         // per-lane LDS addresses of the fragment reads (ring slot 0, block 0)
         const int vr = 4 * h + ((lane & 15) >> 2);
@@ -1027,7 +1033,7 @@ __global__ __launch_bounds__(kTileWaves * kWave) void paged_attn_tiles_kernel(Ar
             o[db][e] *= inv;
             fine &= fabsf(o[db][e]) < INFINITY;
         }
-    if (!fine && rho < rows) {
+    if (!fine && rho < row_end) {
         s_bad[rho - row0] = 1;
         s_any = 1;
     }
@@ -1053,9 +1059,9 @@ __global__ __launch_bounds__(kTileWaves * kWave) void paged_attn_tiles_kernel(Ar
         for (int j = 0; j < 32 / RPL; ++j) {
             const int r = j * RPL + lane / CH, ck = lane % CH;
             const uint4 u = *reinterpret_cast<const uint4*>(w + r * (D * 2) + ((ck ^ (r & (CH - 1))) * 16));
-            if (wrow0 + r < rows) *reinterpret_cast<uint4*>(out_row(wrow0 + r) + ck * 8) = u;
+            if (wrow0 + r < row_end) *reinterpret_cast<uint4*>(out_row(wrow0 + r) + ck * 8) = u;
         }
-    } else if (rho < rows) {
+    } else if (rho < row_end) {
         float* op = part_row(rho);
 #pragma unroll
         for (int db = 0; db < DB; ++db)
@@ -1092,7 +1098,7 @@ __global__ __launch_bounds__(kTileWaves * kWave) void paged_attn_tiles_kernel(Ar
 constexpr int kMergeThreads = 256;
 
 template <bool BF16, int D, int T>
-__global__ __launch_bounds__(kMergeThreads) void paged_attn_merge_kernel(Args a, int rows_per_block, int parts) {
+__global__ __launch_bounds__(kMergeThreads) void paged_attn_merge_kernel(Args a, int parts) {
     constexpr int E = BF16 ? 2 : 4;
     constexpr int LR = D / 4;  // lanes per row and part: 16 or 32
     constexpr int GROUPS = kMergeThreads / LR;
@@ -1118,9 +1124,8 @@ __global__ __launch_bounds__(kMergeThreads) void paged_attn_merge_kernel(Args a,
             first = (int64_t)g * a.n_slots + s.x;
             live = s.y - s.x + 1;
         } else {
-            const int row0 = rho / rows_per_block * rows_per_block;
-            const Span sp =
-                span_of(a, sq.pos0 + row0 / a.G, sq.pos0 + (min(row0 + rows_per_block, sq.n * a.G) - 1) / a.G);
+            const int row0 = rho / a.block_rows * a.block_rows;
+            const Span sp = span_of(a, sq.pos0 + row0 / a.G, sq.pos0 + (min(row0 + a.block_rows, sq.n * a.G) - 1) / a.G);
             first = ((int64_t)b * a.hkv + g) * a.splits;
             live = max(min(((sp.n + T - 1) / T + a.split_tiles - 1) / a.split_tiles, a.splits), 1);
         }
@@ -1202,89 +1207,119 @@ using namespace presto::paged;
 namespace {
 
 struct PagedPlan {
-    bool tiles;      // the kernel of 256-row workgroups
+    bool tiles;      // the kernel that shares tiles in LDS
+    bool by_sequence;
     int nb;          // else: 16-row blocks per workgroup
-    int rows_per_block, row_blocks, splits, split_tiles, shares, n_slots;
+    int block_rows, row_blocks, splits, split_tiles, shares, n_slots;
     int64_t blocks;
     size_t o_bytes, ml_bytes, bytes;
 };
 
 int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-PagedPlan paged_plan(const presto_paged_attn_desc* d) {
-    PagedPlan p{};
-    const bool bf16 = d->pages.dt == PRESTO_DT_BF16;
+// Entries of the longest key list of a block of `rows` rows: all of the
+// context, or the sinks and the window of its first to its last row.
+int64_t longest_list(const presto_paged_attn_desc* d, int64_t rows) {
+    const int64_t all = d->max_ctx > 0 ? d->max_ctx : 1;
+    if (d->window == 0) return all;
     const int G = d->hq / d->pages.hkv;
-    const int64_t rows = (int64_t)G * d->max_q;
-    p.tiles = bf16 && d->max_q > 1 && rows > 32;
-    const int T = p.tiles ? kKeyTile : bf16 ? 32 : 16;
-    p.nb = rows > 16 ? 2 : 1;
-    p.rows_per_block = p.tiles ? kTileRows : 16 * p.nb;
-    p.row_blocks = (int)cdiv(rows, p.rows_per_block);
-    // keys of one row block: all of the context, or the sinks and the window
-    // of its first to its last row
-    int64_t longest = d->max_ctx > 0 ? d->max_ctx : 1;
-    if (d->window > 0) {
-        const int64_t span = (int64_t)d->window + (p.rows_per_block - 1) / G + 1 + 15 + (d->sinks + 15) / 16 * 16;
-        if (span < longest) longest = span;
+    const int64_t span = (int64_t)d->window + (rows - 1) / G + 1 + 15 + (d->sinks + 15) / 16 * 16;
+    return span < all ? span : all;
+}
+
+// The kernel of tiles: rows per workgroup and splits.  A workgroup takes about
+// 8 us beside its tiles (page numbers, queries, first tiles, output); a tile of
+// 64 keys takes 2.0 us with two waves of rows per SIMD, 1.05 with one (up to 128
+// rows); a merge 5 us and its partials' traffic.  One workgroup per CU.  (64
+// rows per workgroup or 128: 512 new tokens of one sequence 24 us at 256 rows.)
+void plan_tiles(const presto_paged_attn_desc* d, int64_t rows, PagedPlan& p) {
+    const int64_t heads = (int64_t)d->pages.batch * d->pages.hkv;
+    const int64_t most = (int64_t)(kTilePages - 8) * d->pages.page_size / kKeyTile;  // page numbers in LDS
+    double best = 1e300;
+    for (int r = kTileRows; r >= 64; r /= 2) {
+        const int64_t blocks = heads * cdiv(rows, r), tiles = cdiv(longest_list(d, r), kKeyTile);
+        for (int64_t s = cdiv(tiles, most); s <= tiles; ++s) {
+            const int64_t per = cdiv(tiles, s);
+            if (cdiv(tiles, per) != s) continue;  // the same splits as for a smaller s
+            const double rounds = (double)cdiv(blocks * s, 256);
+            const double traffic = 2.0 * (double)(heads * s * rows) * d->pages.head_dim * 4 / 4e6;
+            const double cost = rounds * (8.0 + (double)per * (r > 128 ? 2.0 : 1.05)) + (s > 1 ? 5.0 + traffic : 0.0);
+            if (cost < best) {
+                best = cost;
+                p.block_rows = r;
+                p.splits = (int)s;
+                p.split_tiles = (int)per;
+            }
+            if (blocks * s > 1024 && s > cdiv(tiles, most)) break;  // more splits only add
+        }
     }
+    p.row_blocks = (int)cdiv(rows, p.block_rows);
+    p.blocks = heads * p.row_blocks * p.splits;
+    // K and V of a head past the 4 MB of an XCD's L2: its row blocks side by
+    // side (4 sequences of 2048 new tokens on 30720: 4178 -> 4037 us; on 4096:
+    // 668 -> 677)
+    p.by_sequence = longest_list(d, p.block_rows) * d->pages.head_dim * 4 > (4 << 20);
+}
+
+// The kernel of rows.
+void plan_rows(const presto_paged_attn_desc* d, int64_t rows, PagedPlan& p) {
+    const bool bf16 = d->pages.dt == PRESTO_DT_BF16;
+    const int T = bf16 ? 32 : 16;
+    p.nb = rows > 16 ? 2 : 1;
+    p.block_rows = 16 * p.nb;
+    p.row_blocks = (int)cdiv(rows, p.block_rows);
+    const int64_t longest = longest_list(d, p.block_rows), tiles = cdiv(longest, T);
     const int64_t all = (int64_t)d->pages.batch * d->pages.hkv * p.row_blocks;
     int64_t mean = longest;
     if (d->total_ctx > 0 && d->total_ctx / d->pages.batch < mean) mean = d->total_ctx / d->pages.batch + 1;
-    const int64_t tiles = cdiv(longest, T);
-    int64_t per;
-    if (p.tiles) {
-        // one workgroup per CU: split only where the rows leave CUs idle, at
-        // 512 keys or more each
-        per = cdiv(tiles * all, 256);
-        if (per < 8) per = 8;
-        const int64_t most = (int64_t)(kTilePages - 8) * d->pages.page_size / T;  // the page numbers fit in LDS
-        if (all >= 192) per = tiles;
-        if (per > most) per = most;
-    } else {
-        // enough workgroups to fill the chip twice, of at least one tile per wave
-        per = cdiv(cdiv(all * cdiv(mean, T), 1536), kWaves) * kWaves;
-    }
-    if (per > tiles) per = tiles;
-    p.splits = (int)cdiv(tiles, per);
-    p.split_tiles = (int)per;
-    int64_t parts = all / p.row_blocks * p.splits;
-    if (!p.tiles && p.row_blocks == 1) {
-        // Decoding is a stream of the cache: what counts is that all CUs end
-        // together, and few launches.
-        // * Sequences of up to three tiles per wave are not cut (no merge:
-        //   384 keys 8.8 against 11.5 us).
-        // * Sequences of about one length (known from total_ctx) are cut into
-        //   as many splits as the chip holds workgroups at once, three per CU
-        //   by registers at head_dim 128 (two where there are 32 rows): 32 x
-        //   2048 keys in 3 splits 48 us, in 6 52; 80 x 2048 uncut 114, in 2
-        //   splits 143.
-        // * Others, and those that would leave much of a last round empty, in
-        //   equal shares: 24 sequences of 200 .. 12000 keys 157 us in splits,
-        //   100 in shares.  16 x 32768 in shares 328, in 6 splits 322: shares
-        //   take more registers, two workgroups per CU, and two such rounds.
-        const int wgs = 256 * (d->pages.head_dim == 64 ? (p.nb == 1 ? 4 : 3) : (p.nb == 1 ? 3 : 2));
-        p.splits = all < wgs ? (int)(wgs / all) : 1;
-        p.split_tiles = (int)(cdiv(cdiv(tiles, p.splits), kWaves) * kWaves);
-        if (tiles <= 3 * kWaves) p.split_tiles = (int)tiles;
+    // Workgroups that the chip holds at once: three per CU by registers at
+    // head_dim 128, two where they have 32 rows
+    const int wgs = 256 * (d->pages.head_dim == 64 ? (p.nb == 1 ? 4 : 3) : (p.nb == 1 ? 3 : 2));
+    if (p.row_blocks > 1) {
+        // twice as many, of at least one tile per wave
+        p.split_tiles = (int)(cdiv(cdiv(all * cdiv(mean, T), 2 * wgs), kWaves) * kWaves);
+        if (p.split_tiles > tiles) p.split_tiles = (int)tiles;
         p.splits = (int)cdiv(tiles, p.split_tiles);
-        const bool even = d->total_ctx > 0 && 10 * mean >= 9 * longest;
-        const bool idle = all > wgs && cdiv(all, wgs) * wgs * 7 > all * 8;
-        // (every workgroup looks through the batch for its share)
-        const bool can = d->pages.batch <= 2048 && d->pages.batch * tiles < ((int64_t)1 << 30);
-        if (tiles > 3 * kWaves && (!even || idle) && can) {
-            p.shares = 1024 / d->pages.hkv > 0 ? 1024 / d->pages.hkv : 1;
-            p.n_slots = p.shares + d->pages.batch;
-            p.blocks = (int64_t)p.shares * d->pages.hkv;
-            parts = (int64_t)d->pages.hkv * p.n_slots;
-        } else {
-            p.blocks = all * p.splits;
-            parts = all * p.splits;
-        }
-    } else {
         p.blocks = all * p.splits;
+        return;
     }
+    // Few rows are a stream of the cache: what counts is that all CUs end
+    // together, and few launches.
+    // * Sequences of up to three tiles per wave are not cut (no merge: 384 keys
+    //   8.8 against 11.5 us).
+    // * Sequences of about one length (known from total_ctx) are cut into as
+    //   many splits as fill one round: 32 x 2048 keys in 3 splits 48 us, in 6
+    //   52; 80 x 2048 uncut 114, in 2 splits 143.
+    // * Others, and those that would leave much of a last round empty, in equal
+    //   shares: 24 sequences of 200 .. 12000 keys 157 us in splits, 100 in
+    //   shares.  16 x 32768 in shares 328, in 6 splits 322: shares take more
+    //   registers, two workgroups per CU, and two such rounds.
+    p.splits = all < wgs ? (int)(wgs / all) : 1;
+    p.split_tiles = (int)(cdiv(cdiv(tiles, p.splits), kWaves) * kWaves);
+    if (tiles <= 3 * kWaves || p.split_tiles > tiles) p.split_tiles = (int)tiles;
+    p.splits = (int)cdiv(tiles, p.split_tiles);
+    p.blocks = all * p.splits;
+    const bool even = d->total_ctx > 0 && 10 * mean >= 9 * longest;
+    const bool idle = all > wgs && cdiv(all, wgs) * wgs * 7 > all * 8;
+    // (every workgroup looks through the batch for its share)
+    const bool can = d->pages.batch <= 2048 && d->pages.batch * tiles < ((int64_t)1 << 30);
+    if (tiles > 3 * kWaves && (!even || idle) && can) {
+        p.shares = 1024 / d->pages.hkv > 0 ? 1024 / d->pages.hkv : 1;
+        p.n_slots = p.shares + d->pages.batch;
+        p.blocks = (int64_t)p.shares * d->pages.hkv;
+    }
+}
+
+PagedPlan paged_plan(const presto_paged_attn_desc* d) {
+    PagedPlan p{};
+    const int64_t rows = (int64_t)(d->hq / d->pages.hkv) * d->max_q;
+    p.tiles = d->pages.dt == PRESTO_DT_BF16 && d->max_q > 1 && rows > 32;
+    if (p.tiles)
+        plan_tiles(d, rows, p);
+    else
+        plan_rows(d, rows, p);
     if (p.splits > 1 || p.shares > 0) {
+        const int64_t parts = d->pages.hkv * (p.shares ? (int64_t)p.n_slots : (int64_t)d->pages.batch * p.splits);
         p.o_bytes = (size_t)(parts * rows) * d->pages.head_dim * sizeof(float);
         p.ml_bytes = (size_t)(parts * rows) * sizeof(float2);
         p.bytes = p.o_bytes + p.ml_bytes + (p.shares ? (size_t)d->pages.batch * sizeof(int2) : 0);
@@ -1322,9 +1357,9 @@ void launch_attn(const PagedPlan& p, const Args& a, hipStream_t stream) {
         const unsigned grid = (unsigned)cdiv((int64_t)a.batch * a.max_q * a.hq, GROUPS / parts);
         if (p.tiles)
             paged_attn_merge_kernel<BF16, D, kKeyTile>
-                <<<grid, kMergeThreads, 0, stream>>>(a, p.rows_per_block, parts);
+                <<<grid, kMergeThreads, 0, stream>>>(a, parts);
         else
-            paged_attn_merge_kernel<BF16, D, T><<<grid, kMergeThreads, 0, stream>>>(a, p.rows_per_block, parts);
+            paged_attn_merge_kernel<BF16, D, T><<<grid, kMergeThreads, 0, stream>>>(a, parts);
     }
 }
 
@@ -1369,6 +1404,8 @@ presto_status launch_paged_attn(const presto_paged_attn_desc* d, const void* q, 
     a.window = d->window;
     a.sinks = d->window > 0 ? d->sinks : 0;
     a.row_blocks = p.row_blocks;
+    a.block_rows = p.block_rows;
+    a.by_sequence = p.by_sequence;
     a.splits = p.splits;
     a.split_tiles = p.split_tiles;
     a.shares = p.shares;

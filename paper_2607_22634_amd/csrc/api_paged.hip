@@ -3,14 +3,10 @@
 #include <math.h>
 
 #include "common.hpp"
+#include "paged.hpp"
 
 namespace presto_host {
 
-size_t paged_attn_workspace_bytes(const presto_paged_attn_desc* d);
-bool paged_attn_fits(const presto_paged_attn_desc* d);
-presto_status launch_paged_attn(const presto_paged_attn_desc* d, const void* q, const int32_t* q_off,
-                                const void* kp, const void* vp, const int32_t* table, const int32_t* ctx, void* out,
-                                int32_t* flags, void* ws, hipStream_t stream);
 size_t pages_workspace_bytes(const presto_pages_desc* d, int64_t n);
 presto_status launch_pages_reserve(const presto_pages_desc* d, int32_t* refs, int32_t* table, const int32_t* ctx,
                                    const int32_t* add, int32_t extra, int32_t* ctx_out, int32_t* flags, void* ws,
@@ -77,7 +73,8 @@ static bool aligned16(const void* a, const void* b, const void* c = nullptr, con
     return (((uintptr_t)a | (uintptr_t)b | (uintptr_t)c | (uintptr_t)d) & 15) == 0;
 }
 
-static presto_status check_paged_attn(presto_paged_attn_desc& d, bool decode, const char* who) {
+// Checks a call, fills in its default strides and plans it.
+static presto_status check_paged_attn(presto_paged_attn_desc& d, PagedPlan& plan, bool decode, const char* who) {
     presto_status st = check_pages(d.pages, who);
     if (st != PRESTO_OK) return st;
     if (decode) {
@@ -98,16 +95,18 @@ static presto_status check_paged_attn(presto_paged_attn_desc& d, bool decode, co
     REQUIRE(d.q_stride >= (int64_t)d.hq * d.pages.head_dim && d.q_stride <= ((int64_t)1 << 31) &&
                 d.q_stride % (d.pages.dt == PRESTO_DT_BF16 ? 8 : 4) == 0,
             "%s: q_stride %lld", who, (long long)d.q_stride);
-    if (d.pages.batch > 0 && d.max_q > 0 && !paged_attn_fits(&d))
-        return set_error(PRESTO_ERR_UNSUPPORTED, "%s: too many query rows for one call", who);
+    if (d.pages.batch > 0 && d.max_q > 0) {
+        plan = paged_plan(&d);
+        if (!plan.fits) return set_error(PRESTO_ERR_UNSUPPORTED, "%s: too many query rows for one call", who);
+    }
     return PRESTO_OK;
 }
 
 static size_t paged_attn_ws(const presto_paged_attn_desc* desc, bool decode) {
     if (!desc) return 0;
     presto_paged_attn_desc d = *desc;
-    if (check_paged_attn(d, decode, "workspace") != PRESTO_OK || d.pages.batch == 0 || d.max_q == 0) return 0;
-    return paged_attn_workspace_bytes(&d);
+    PagedPlan plan{};
+    return check_paged_attn(d, plan, decode, "workspace") == PRESTO_OK ? plan.bytes : 0;
 }
 
 static presto_status paged_attn(const presto_paged_attn_desc* desc, bool decode, const char* who, const void* q,
@@ -117,15 +116,16 @@ static presto_status paged_attn(const presto_paged_attn_desc* desc, bool decode,
     set_error(PRESTO_OK, "%s", "");
     REQUIRE(desc, "%s: null descriptor", who);
     presto_paged_attn_desc d = *desc;
-    presto_status st = check_paged_attn(d, decode, who);
+    PagedPlan plan{};
+    presto_status st = check_paged_attn(d, plan, decode, who);
     if (st != PRESTO_OK) return st;
     if (d.pages.batch == 0 || d.max_q == 0 || d.total_q == 0) return PRESTO_OK;
     REQUIRE(q && (decode || q_offsets) && k_pages && v_pages && page_table && ctx && out, "%s: null pointer", who);
     REQUIRE(aligned16(q, k_pages, v_pages, out), "%s: tensors must be 16-byte aligned", who);
-    st = check_ws(ws, ws_bytes, paged_attn_workspace_bytes(&d));
+    st = check_ws(ws, ws_bytes, plan.bytes);
     if (st != PRESTO_OK) return st;
     REQUIRE(aligned16(ws, nullptr), "%s: the workspace must be 16-byte aligned", who);
-    return launch_paged_attn(&d, q, decode ? nullptr : q_offsets, k_pages, v_pages, page_table, ctx, out, flags, ws,
+    return launch_paged_attn(&d, plan, q, decode ? nullptr : q_offsets, k_pages, v_pages, page_table, ctx, out, flags, ws,
                              stream);
 }
 

@@ -18,6 +18,7 @@
 #include <type_traits>
 
 #include "common.hpp"
+#include "paged.hpp"
 
 namespace presto {
 namespace paged {
@@ -1206,15 +1207,6 @@ using namespace presto::paged;
 
 namespace {
 
-struct PagedPlan {
-    bool tiles;      // the kernel that shares tiles in LDS
-    bool by_sequence;
-    int nb;          // else: 16-row blocks per workgroup
-    int block_rows, row_blocks, splits, split_tiles, shares, n_slots;
-    int64_t blocks;
-    size_t o_bytes, ml_bytes, bytes;
-};
-
 int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Entries of the longest key list of a block of `rows` rows: all of the
@@ -1227,30 +1219,39 @@ int64_t longest_list(const presto_paged_attn_desc* d, int64_t rows) {
     return span < all ? span : all;
 }
 
-// The kernel of tiles: rows per workgroup and splits.  A workgroup takes about
-// 8 us beside its tiles (page numbers, queries, first tiles, output); a tile of
-// 64 keys takes 2.0 us with two waves of rows per SIMD, 1.05 with one (up to 128
-// rows); a merge 5 us and its partials' traffic.  One workgroup per CU.  (64
-// rows per workgroup or 128: 512 new tokens of one sequence 24 us at 256 rows.)
+// The kernel of tiles: rows per workgroup and splits, by modelled time in us.
+// A workgroup takes about 8 beside its tiles (page numbers, queries, first
+// tiles, output), a tile of 64 keys 1.75 with two waves of rows per SIMD and
+// 1.25 with one (up to 128 rows), a merge 5 and its partials' traffic.  One
+// workgroup per CU: whole rounds where all are alike, else the longest or the
+// sum.  Measured: 512 new tokens alone 18.2 in blocks of 128 rows, 22.4 of 256;
+// 64 on 65536 cached 99 in 32 splits of 256 rows, 114 in 16 of 128; 16 x 300
+// on 1700 217 in blocks of 256, 238 of 128.
 void plan_tiles(const presto_paged_attn_desc* d, int64_t rows, PagedPlan& p) {
     const int64_t heads = (int64_t)d->pages.batch * d->pages.hkv;
     const int64_t most = (int64_t)(kTilePages - 8) * d->pages.page_size / kKeyTile;  // page numbers in LDS
     double best = 1e300;
     for (int r = kTileRows; r >= 64; r /= 2) {
-        const int64_t blocks = heads * cdiv(rows, r), tiles = cdiv(longest_list(d, r), kKeyTile);
-        for (int64_t s = cdiv(tiles, most); s <= tiles; ++s) {
-            const int64_t per = cdiv(tiles, s);
-            if (cdiv(tiles, per) != s) continue;  // the same splits as for a smaller s
-            const double rounds = (double)cdiv(blocks * s, 256);
-            const double traffic = 2.0 * (double)(heads * s * rows) * d->pages.head_dim * 4 / 4e6;
-            const double cost = rounds * (8.0 + (double)per * (r > 128 ? 2.0 : 1.05)) + (s > 1 ? 5.0 + traffic : 0.0);
+        const int64_t blocks = heads * cdiv(rows, r), list = longest_list(d, r), tiles = cdiv(list, kKeyTile);
+        // the earlier row blocks of a sequence see fewer keys
+        const int64_t mean = list - (list == d->max_ctx ? (d->max_q < list ? d->max_q : list) / 2 : 0);
+        const int64_t least = cdiv(tiles, most);
+        for (int64_t want = least; want <= tiles && (want == least || blocks * want <= 4096); want += 1 + want / 8) {
+            const int64_t per = cdiv(tiles, want), s = cdiv(tiles, per);
+            const double step = r > 128 ? 1.75 : 1.25;
+            const double longest = 8.0 + (double)per * step;
+            double cost = (double)cdiv(blocks * s, 256) * longest;
+            if (10 * mean < 9 * list) {
+                const double sum = (double)(blocks * s) * (8.0 + (double)per * step * (double)mean / (double)list) / 256;
+                cost = longest > 1.1 * sum ? longest : 1.1 * sum;
+            }
+            if (s > 1) cost += 5.0 + 2.0 * (double)(heads * s * rows) * d->pages.head_dim * 4 / 8e6;
             if (cost < best) {
                 best = cost;
                 p.block_rows = r;
                 p.splits = (int)s;
                 p.split_tiles = (int)per;
             }
-            if (blocks * s > 1024 && s > cdiv(tiles, most)) break;  // more splits only add
         }
     }
     p.row_blocks = (int)cdiv(rows, p.block_rows);
@@ -1310,6 +1311,8 @@ void plan_rows(const presto_paged_attn_desc* d, int64_t rows, PagedPlan& p) {
     }
 }
 
+}  // namespace
+
 PagedPlan paged_plan(const presto_paged_attn_desc* d) {
     PagedPlan p{};
     const int64_t rows = (int64_t)(d->hq / d->pages.hkv) * d->max_q;
@@ -1324,8 +1327,12 @@ PagedPlan paged_plan(const presto_paged_attn_desc* d) {
         p.ml_bytes = (size_t)(parts * rows) * sizeof(float2);
         p.bytes = p.o_bytes + p.ml_bytes + (p.shares ? (size_t)d->pages.batch * sizeof(int2) : 0);
     }
+    // (a grid holds fewer than 2^31 workgroups; the merge takes some per row)
+    p.fits = p.blocks < ((int64_t)1 << 31) && (int64_t)d->pages.batch * d->max_q * d->hq < ((int64_t)1 << 31);
     return p;
 }
+
+namespace {
 
 template <bool BF16, int D, int NB>
 void launch_rows(const PagedPlan& p, const Args& a, hipStream_t stream) {
@@ -1365,19 +1372,9 @@ void launch_attn(const PagedPlan& p, const Args& a, hipStream_t stream) {
 
 }  // namespace
 
-size_t paged_attn_workspace_bytes(const presto_paged_attn_desc* d) { return paged_plan(d).bytes; }
-
-// false: more workgroups than a grid holds
-bool paged_attn_fits(const presto_paged_attn_desc* d) {
-    const PagedPlan p = paged_plan(d);
-    const int64_t rows = (int64_t)d->pages.batch * d->max_q * d->hq;
-    return p.blocks < ((int64_t)1 << 31) && rows < ((int64_t)1 << 31);
-}
-
-presto_status launch_paged_attn(const presto_paged_attn_desc* d, const void* q, const int32_t* q_off,
+presto_status launch_paged_attn(const presto_paged_attn_desc* d, const PagedPlan& p, const void* q, const int32_t* q_off,
                                 const void* kp, const void* vp, const int32_t* table, const int32_t* ctx, void* out,
                                 int32_t* flags, void* ws, hipStream_t stream) {
-    const PagedPlan p = paged_plan(d);
     Args a{};
     a.q = static_cast<const char*>(q);
     a.kp = static_cast<const char*>(kp);

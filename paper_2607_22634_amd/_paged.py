@@ -6,7 +6,6 @@ device of their tensors, on that device's current stream unless one is given.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 
 import torch
@@ -14,18 +13,21 @@ import torch
 from ._lib import PagedAttnDesc, PagesDesc, _check, _dt, _ptr, lib
 
 
-def _same(dev, names: str, *ts) -> None:
-    """Tensors on one GPU (None: left out)."""
+def _same(dev: int, names: str, *ts) -> None:
+    """Tensors on GPU `dev` (None: left out)."""
     for i, t in enumerate(ts):
-        if t is not None and (not t.is_cuda or t.device != dev):
-            raise ValueError(f"{names.split()[i]} must be a tensor on the GPU of the others, {dev}")
+        if t is not None and (t.get_device() != dev or dev < 0):
+            raise ValueError(f"{names.split()[i]} must be a tensor on the GPU of the others")
 
 
-def _book(dev, names: str, *ts) -> None:
-    """int32 bookkeeping tensors, contiguous, on one GPU."""
+_I32 = torch.int32
+
+
+def _book(dev: int, names: str, *ts) -> None:
+    """int32 bookkeeping tensors, contiguous, on GPU `dev`."""
     for i, t in enumerate(ts):
-        if t is not None and not (t.dtype is torch.int32 and t.is_cuda and t.device == dev and t.is_contiguous()):
-            raise ValueError(f"{names.split()[i]} must be a contiguous int32 tensor on the GPU of the others, {dev}")
+        if t is not None and (t.dtype is not _I32 or t.get_device() != dev or dev < 0 or not t.is_contiguous()):
+            raise ValueError(f"{names.split()[i]} must be a contiguous int32 tensor on the GPU of the others")
 
 
 def _shape(name, t, *shape):
@@ -33,25 +35,29 @@ def _shape(name, t, *shape):
         raise ValueError(f"{name} must be of shape {list(shape)}, not {list(t.shape)}")
 
 
-_HERE = contextlib.nullcontext()
+_current = torch._C._cuda_getDevice
+_raw_stream = torch._C._cuda_getCurrentRawStream
 
 
-def _on(dev):
-    """Makes `dev` the current device (free when it is already)."""
-    return _HERE if dev.index == torch._C._cuda_getDevice() else torch.cuda.device(dev)
-
-
-def _queue(dev, stream, *made):
-    """The stream's handle; tensors made here for a call on a stream that is
-    not the current one must not be handed out again before it is through."""
+def _launch(call, who: str, dev: int, stream, made, *args) -> None:
+    """Enqueues call(*args, stream) on GPU `dev`.  Tensors made here for a call
+    on a stream that is not the current one must not be handed out again before
+    it is through."""
     if stream is None:
-        return torch._C._cuda_getCurrentRawStream(dev.index)
-    if stream.device != dev:
-        raise ValueError(f"the stream belongs to {stream.device}, the tensors to {dev}")
-    for t in made:
-        if t is not None:
+        queue = _raw_stream(dev)
+    else:
+        if stream.device.index != dev:
+            raise ValueError(f"the stream belongs to {stream.device}, the tensors to GPU {dev}")
+        for t in made:
             t.record_stream(stream)
-    return stream.cuda_stream
+        queue = stream.cuda_stream
+    if dev == _current():
+        status = call(*args, queue)
+    else:
+        with torch.cuda.device(dev):
+            status = call(*args, queue)
+    if status:
+        _check(status, who)
 
 
 def _pool(k, v, page_table, batch, layers: bool) -> PagesDesc:
@@ -107,33 +113,26 @@ def _attn_desc(q, k_pages, v_pages, page_table, batch, max_q, max_ctx, scale, wi
                          total_ctx)
 
 
-def _attend(call, need_of, q, q_offsets, k_pages, v_pages, page_table, ctx, desc, out, flags, workspace, stream):
-    dev = q.device
+def _attend(who, call, need_of, q, q_offsets, k_pages, v_pages, page_table, ctx, desc, out, flags, workspace, stream):
+    dev = q.get_device()
     _same(dev, "q k_pages v_pages out workspace", q, k_pages, v_pages, out, workspace)
     _book(dev, "page_table ctx q_offsets flags", page_table, ctx, q_offsets, flags)
-    ref = ctypes.byref(desc)
-    made, ws, nb = [], workspace, 0
+    ref, made, ws, nb = ctypes.byref(desc), [], workspace, 0
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         made.append(out)
     elif out.shape != q.shape or out.dtype != q.dtype or not out.is_contiguous():
         raise ValueError("out must be a contiguous tensor of q's shape and type")
     if ws is None:
         nb = need_of(ref)
         if nb:
-            ws = torch.empty(nb, dtype=torch.uint8, device=dev)
+            ws = torch.empty(nb, dtype=torch.uint8, device=q.device)
             made.append(ws)
     else:
         nb = ws.numel() * ws.element_size()
-    with _on(dev):
-        tail = (page_table.data_ptr(), ctx.data_ptr(), out.data_ptr(), _ptr(flags), _ptr(ws), nb,
-                _queue(dev, stream, *made))
-        if q_offsets is None:
-            status = call(ref, q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), *tail)
-        else:
-            status = call(ref, q.data_ptr(), q_offsets.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(), *tail)
-        if status:
-            _check(status, "presto_paged_attention" if q_offsets is None else "presto_window_attention")
+    head = (ref, q.data_ptr()) if q_offsets is None else (ref, q.data_ptr(), q_offsets.data_ptr())
+    _launch(call, who, dev, stream, made, *head, k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(),
+            ctx.data_ptr(), out.data_ptr(), _ptr(flags), _ptr(ws), nb)
     return out
 
 
@@ -148,7 +147,7 @@ def presto_paged_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torc
     desc = _attn_desc(q, k_pages, v_pages, page_table, b, 1, max_ctx, scale, window, sinks, total_ctx)
     _shape("ctx", ctx, b)
     L = lib()
-    return _attend(L.presto_paged_attention, L.presto_paged_attention_workspace, q, None, k_pages, v_pages,
+    return _attend("presto_paged_attention", L.presto_paged_attention, L.presto_paged_attention_workspace, q, None, k_pages, v_pages,
                    page_table, ctx, desc, out, flags, workspace, stream)
 
 
@@ -164,7 +163,7 @@ def presto_window_attention(q: torch.Tensor, q_offsets: torch.Tensor, max_q: int
     _shape("q_offsets", q_offsets, b + 1)
     _shape("ctx", ctx, b)
     L = lib()
-    return _attend(L.presto_window_attention, L.presto_window_attention_workspace, q, q_offsets, k_pages, v_pages,
+    return _attend("presto_window_attention", L.presto_window_attention, L.presto_window_attention_workspace, q, q_offsets, k_pages, v_pages,
                    page_table, ctx, desc, out, flags, workspace, stream)
 
 
@@ -180,16 +179,15 @@ def paged_attention_workspace(q: torch.Tensor, k_pages: torch.Tensor, page_table
     return torch.empty(need, dtype=torch.uint8, device=q.device)
 
 
-def _pages_call(who, dev, desc, args, flags, workspace, stream, made=()):
+def _pages_call(who, dev, device, desc, args, flags, workspace, stream, made=()):
     """args: the call's pointers up to flags."""
     L, ref, ws = lib(), ctypes.byref(desc), workspace
     _same(dev, "workspace", ws)
     if ws is None:
-        ws = torch.empty(max(L.presto_pages_workspace(ref), 16), dtype=torch.uint8, device=dev)
+        ws = torch.empty(max(L.presto_pages_workspace(ref), 16), dtype=torch.uint8, device=device)
         made = (*made, ws)
-    with _on(dev):
-        _check(getattr(L, who)(ref, *args, _ptr(flags), ws.data_ptr(), ws.numel() * ws.element_size(),
-                               _queue(dev, stream, *made)), who)
+    _launch(getattr(L, who), who, dev, stream, made, ref, *args, _ptr(flags), ws.data_ptr(),
+            ws.numel() * ws.element_size())
 
 
 def pages_workspace(refs: torch.Tensor, page_table: torch.Tensor) -> torch.Tensor:
@@ -201,8 +199,10 @@ def pages_workspace(refs: torch.Tensor, page_table: torch.Tensor) -> torch.Tenso
 def _check_books(refs, page_table, ctx, names: str = "", *more):
     if page_table.dim() != 2 or refs.dim() != 1:
         raise ValueError("page_table must be [sequences, columns] and refs [pages]")
-    _book(refs.device, "refs page_table ctx " + names, refs, page_table, ctx, *more)
+    dev = refs.get_device()
+    _book(dev, "refs page_table ctx " + names, refs, page_table, ctx, *more)
     _shape("ctx", ctx, page_table.shape[0])
+    return dev
 
 
 def presto_pages_reserve(refs: torch.Tensor, page_table: torch.Tensor, ctx: torch.Tensor, page_size: int,
@@ -211,16 +211,17 @@ def presto_pages_reserve(refs: torch.Tensor, page_table: torch.Tensor, ctx: torc
     """Gives pages to the positions ctx .. ctx + add + extra - 1 and returns the
     new lengths (in `out`, which may be ctx); refs and page_table are updated
     in place.  A sequence the pool has no pages for keeps its length."""
-    _check_books(refs, page_table, ctx, "add out flags", add, out, flags)
+    dev = _check_books(refs, page_table, ctx, "add out flags", add, out, flags)
     b = page_table.shape[0]
     _shape("add", add, b)
     _shape("out", out, b)
-    made = None
+    made = ()
     if out is None:
-        out = made = torch.empty_like(ctx)
-    _pages_call("presto_pages_reserve", refs.device, _books(refs, page_table, page_size),
-                (_ptr(refs), _ptr(page_table), _ptr(ctx), _ptr(add), extra, _ptr(out)), flags, workspace, stream,
-                (made,))
+        out = torch.empty_like(ctx)
+        made = (out,)
+    _pages_call("presto_pages_reserve", dev, refs.device, _books(refs, page_table, page_size),
+                (refs.data_ptr(), page_table.data_ptr(), ctx.data_ptr(), _ptr(add), extra, out.data_ptr()), flags,
+                workspace, stream, made)
     return out
 
 
@@ -229,7 +230,7 @@ def presto_append_kv(k_new: torch.Tensor, v_new: torch.Tensor, offsets: torch.Te
                      ctx_new: torch.Tensor, *, flags=None, stream=None) -> None:
     """Writes rows offsets[b] + i of k_new, v_new [rows, Hkv, d] to positions
     ctx[b] + i < ctx_new[b] of the cache, at most max_new per sequence."""
-    dev = k_new.device
+    dev = k_new.get_device()
     b = offsets.shape[0] - 1
     _same(dev, "k_new v_new k_pages v_pages", k_new, v_new, k_pages, v_pages)
     _book(dev, "offsets page_table ctx ctx_new flags", offsets, page_table, ctx, ctx_new, flags)
@@ -245,11 +246,9 @@ def presto_append_kv(k_new: torch.Tensor, v_new: torch.Tensor, offsets: torch.Te
     stride = _rows("k_new", k_new, hkv, d)
     if v_new.shape != k_new.shape or _rows("v_new", v_new, hkv, d) != stride:
         raise ValueError("k_new and v_new must have one shape and stride")
-    with _on(dev):
-        _check(lib().presto_append_kv(ctypes.byref(desc), k_new.data_ptr(), v_new.data_ptr(), k_new.shape[0], stride,
-                                      offsets.data_ptr(), max_new, k_pages.data_ptr(), v_pages.data_ptr(),
-                                      page_table.data_ptr(), ctx.data_ptr(), ctx_new.data_ptr(), _ptr(flags),
-                                      _queue(dev, stream)), "presto_append_kv")
+    _launch(lib().presto_append_kv, "presto_append_kv", dev, stream, (), ctypes.byref(desc), k_new.data_ptr(),
+            v_new.data_ptr(), k_new.shape[0], stride, offsets.data_ptr(), max_new, k_pages.data_ptr(),
+            v_pages.data_ptr(), page_table.data_ptr(), ctx.data_ptr(), ctx_new.data_ptr(), _ptr(flags))
 
 
 def presto_pages_fork(refs: torch.Tensor, page_table: torch.Tensor, ctx: torch.Tensor, parent: torch.Tensor,
@@ -258,14 +257,14 @@ def presto_pages_fork(refs: torch.Tensor, page_table: torch.Tensor, ctx: torch.T
     """Sequence child[i] (empty) becomes a copy of parent[i]: full pages shared,
     the rows of the last one copied in all layers of k_pages, v_pages
     [layers, pages, page, Hkv, d] (or of one layer, without that dimension)."""
-    _check_books(refs, page_table, ctx, "parent child flags", parent, child, flags)
-    _same(refs.device, "k_pages v_pages", k_pages, v_pages)
+    dev = _check_books(refs, page_table, ctx, "parent child flags", parent, child, flags)
+    _same(dev, "k_pages v_pages", k_pages, v_pages)
     n = parent.numel()
     _shape("parent", parent, n)
     _shape("child", child, n)
     desc = _pool(k_pages, v_pages, page_table, page_table.shape[0], True)
     _shape("refs", refs, desc.num_pages)
-    _pages_call("presto_pages_fork", refs.device, desc,
+    _pages_call("presto_pages_fork", dev, refs.device, desc,
                 (_ptr(refs), _ptr(page_table), _ptr(ctx), _ptr(parent), _ptr(child), n, _ptr(k_pages),
                  _ptr(v_pages)), flags, workspace, stream)
 
@@ -273,25 +272,21 @@ def presto_pages_fork(refs: torch.Tensor, page_table: torch.Tensor, ctx: torch.T
 def presto_pages_free(refs: torch.Tensor, page_table: torch.Tensor, ctx: torch.Tensor, rows: torch.Tensor, *,
                       flags=None, stream=None) -> None:
     """Drops the sequences `rows`: their references go, their lengths are 0."""
-    _check_books(refs, page_table, ctx, "rows flags", rows, flags)
-    _shape("rows", rows, rows.numel())
-    desc = _books(refs, page_table, 16)
-    with _on(refs.device):
-        st = _queue(refs.device, stream)
-        _check(lib().presto_pages_free(ctypes.byref(desc), _ptr(refs), _ptr(page_table), _ptr(ctx), _ptr(rows),
-                                       rows.numel(), _ptr(flags), st), "presto_pages_free")
+    dev = _check_books(refs, page_table, ctx, "rows flags", rows, flags)
+    n = rows.numel()
+    _shape("rows", rows, n)
+    _launch(lib().presto_pages_free, "presto_pages_free", dev, stream, (), ctypes.byref(_books(refs, page_table, 16)),
+            refs.data_ptr(), page_table.data_ptr(), ctx.data_ptr(), rows.data_ptr(), n, _ptr(flags))
 
 
 def presto_pages_trim(refs: torch.Tensor, page_table: torch.Tensor, ctx: torch.Tensor, page_size: int, window: int,
                       sinks: int = 0, *, flags=None, stream=None) -> None:
     """Drops the pages that no query from position ctx - 1 on sees under the
     window and sinks."""
-    _check_books(refs, page_table, ctx, "flags", flags)
-    desc = _books(refs, page_table, page_size)
-    with _on(refs.device):
-        st = _queue(refs.device, stream)
-        _check(lib().presto_pages_trim(ctypes.byref(desc), _ptr(refs), _ptr(page_table), _ptr(ctx), window, sinks,
-                                       _ptr(flags), st), "presto_pages_trim")
+    dev = _check_books(refs, page_table, ctx, "flags", flags)
+    _launch(lib().presto_pages_trim, "presto_pages_trim", dev, stream, (),
+            ctypes.byref(_books(refs, page_table, page_size)), refs.data_ptr(), page_table.data_ptr(), ctx.data_ptr(),
+            window, sinks, _ptr(flags))
 
 
 def presto_pages_compact(refs: torch.Tensor, page_table: torch.Tensor, k_pages: torch.Tensor,
@@ -300,13 +295,12 @@ def presto_pages_compact(refs: torch.Tensor, page_table: torch.Tensor, k_pages: 
     the books afterwards: refs, page_table, n_live [1] (or fills those of
     `out`, where refs and page_table may be the arguments themselves, and
     page_map [pages], each live page's new number, if it is there)."""
-    _check_books(refs, page_table, None, "flags", flags)
-    dev = refs.device
+    dev = _check_books(refs, page_table, None, "flags", flags)
     _same(dev, "k_pages v_pages", k_pages, v_pages)
     made = ()
     if out is None:
         out = {"refs": torch.empty_like(refs), "page_table": torch.empty_like(page_table),
-               "n_live": torch.empty(1, dtype=torch.int32, device=dev)}
+               "n_live": torch.empty(1, dtype=torch.int32, device=refs.device)}
         made = tuple(out.values())
     page_map = out.get("page_map")
     _book(dev, "out_refs out_page_table n_live page_map", out["refs"], out["page_table"], out["n_live"], page_map)
@@ -316,7 +310,7 @@ def presto_pages_compact(refs: torch.Tensor, page_table: torch.Tensor, k_pages: 
     _shape("out page_table", out["page_table"], *page_table.shape)
     _shape("n_live", out["n_live"], 1)
     _shape("page_map", page_map, desc.num_pages)
-    _pages_call("presto_pages_compact", dev, desc,
+    _pages_call("presto_pages_compact", dev, refs.device, desc,
                 (_ptr(refs), _ptr(out["refs"]), _ptr(page_table), _ptr(out["page_table"]), _ptr(out["n_live"]),
                  _ptr(page_map), _ptr(k_pages), _ptr(v_pages)), flags, workspace, stream, made)
     return out

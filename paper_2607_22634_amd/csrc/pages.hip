@@ -33,6 +33,11 @@ __device__ __forceinline__ int block_scan(int v, int* s_wave, int& total) {
     return before + incl - v;
 }
 
+// Keeps a load where it is written: without a use before the branch that needs
+// it, the compiler moves it there, and the loads of a thread then wait for one
+// another.
+__device__ __forceinline__ void arrived(const uint4& u) { asm volatile("" ::"v"(u.x), "v"(u.y), "v"(u.z), "v"(u.w)); }
+
 struct Four {
     int32_t v[4];
 };
@@ -369,7 +374,9 @@ __global__ __launch_bounds__(256) void pages_remap_kernel(const int32_t* table, 
 
 // Copies the first `rows` rows of page src to page dst, in every layer, of K
 // and of V.  A unit is a stretch of kMoveBytes of one page; the pages of a
-// call's moves are all different, so units run in any order.
+// call's moves are all different, so units run in any order.  Neighbouring
+// units belong to different pools (layers, K and V): every eighth block runs on
+// one XCD, which so touches few pools' address translations.
 constexpr int kMoveThreads = 256;
 constexpr int kMoveLoads = 4;
 constexpr int kMoveBytes = kMoveThreads * kMoveLoads * 16;
@@ -382,22 +389,22 @@ __global__ __launch_bounds__(kMoveThreads) void pages_move_kernel(char* __restri
                                                                   int64_t layer_bytes) {
     const int64_t units = (int64_t)*n_moves * layers * 2 * stretches;
     for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
-        const int s = (int)(u % stretches);
-        int64_t r = u / stretches;
-        char* pool = r & 1 ? v : k;
-        r >>= 1;
-        const int layer = (int)(r % layers);
-        const Move mv = moves[r / layers];
+        const int pool_id = (int)(u % (2 * layers)), layer = pool_id >> 1;
+        char* pool = pool_id & 1 ? v : k;
+        const int64_t r = u / (2 * layers);
+        const int s = (int)(r % stretches);
+        const Move mv = moves[r / stretches];
         const int64_t bytes = mv.rows * row_bytes;
         const int64_t at = (int64_t)s * kMoveBytes + threadIdx.x * 16;
         const char* from = pool + layer * layer_bytes + mv.src * page_bytes;
         char* to = pool + layer * layer_bytes + mv.dst * page_bytes;
-        uint4 x[kMoveLoads];
+        if (at >= bytes) continue;
+        uint4 x[kMoveLoads];  // (past the end the last piece is read again)
 #pragma unroll
-        for (int j = 0; j < kMoveLoads; ++j) {
-            const int64_t o = at + j * (kMoveThreads * 16);
-            if (o < bytes) x[j] = *reinterpret_cast<const uint4*>(from + o);
-        }
+        for (int j = 0; j < kMoveLoads; ++j)
+            x[j] = *reinterpret_cast<const uint4*>(from + min(at + j * (kMoveThreads * 16), bytes - 16));
+#pragma unroll
+        for (int j = 0; j < kMoveLoads; ++j) arrived(x[j]);
 #pragma unroll
         for (int j = 0; j < kMoveLoads; ++j) {
             const int64_t o = at + j * (kMoveThreads * 16);
@@ -432,20 +439,39 @@ __global__ __launch_bounds__(kAppendThreads) void append_kv_kernel(
     if (i0 >= m) return;
     const int rows = (int)min((int64_t)kAppendRows, m - i0);
     bool lost = false;
-    for (int i = threadIdx.x; i < rows * row16; i += kAppendThreads) {
-        const int r = i / row16, x = i - r * row16;
-        const int pos = c + i0 + r;
-        const int e = table[(int64_t)b * max_pages + (pos >> shift)];
-        if (e < 0 || e >= num_pages) {
-            lost = true;
-            continue;
+    // four pieces of K and V in flight per thread; past the end the last piece
+    // is read again
+    constexpr int U = 4;
+    const int pieces = rows * row16;
+    for (int p0 = threadIdx.x; p0 < pieces; p0 += U * kAppendThreads) {
+        int e[U], at[U];
+        uint4 kv[U], vv[U];
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            const int i = min(p0 + j * kAppendThreads, pieces - 1);
+            const int r = i / row16, x = i - r * row16, pos = c + i0 + r;
+            e[j] = table[(int64_t)b * max_pages + (pos >> shift)];
+            at[j] = (pos & (page - 1)) * row16 + x;
+            const int64_t src = (o0 + i0 + r) * new_bytes + x * 16;
+            kv[j] = *reinterpret_cast<const uint4*>(k_new + src);
+            vv[j] = *reinterpret_cast<const uint4*>(v_new + src);
         }
-        const int64_t src = (o0 + i0 + r) * new_bytes + x * 16;
-        const int64_t dst = e * page_bytes + ((int64_t)(pos & (page - 1)) * row16 + x) * 16;
-        const uint4 kv = *reinterpret_cast<const uint4*>(k_new + src);
-        const uint4 vv = *reinterpret_cast<const uint4*>(v_new + src);
-        *reinterpret_cast<uint4*>(k + dst) = kv;
-        *reinterpret_cast<uint4*>(v + dst) = vv;
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            arrived(kv[j]);
+            arrived(vv[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < U; ++j) {
+            if (p0 + j * kAppendThreads >= pieces) continue;
+            if (e[j] < 0 || e[j] >= num_pages) {
+                lost = true;
+                continue;
+            }
+            const int64_t dst = e[j] * page_bytes + (int64_t)at[j] * 16;
+            *reinterpret_cast<uint4*>(k + dst) = kv[j];
+            *reinterpret_cast<uint4*>(v + dst) = vv[j];
+        }
     }
     if (lost) raise_flag(flags, PRESTO_FLAG_BAD_PAGE);
 }

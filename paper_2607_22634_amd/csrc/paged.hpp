@@ -12,7 +12,7 @@ namespace presto_host {
 struct PagedPlan {
     bool fits;         // false: more workgroups than a grid holds
     bool tiles;        // the kernel that shares tiles in LDS
-    bool by_sequence;  // (tiles) one sequence after the other
+    int order;         // of the row blocks
     int nb;            // (rows) 16-row blocks per workgroup
     int block_rows, row_blocks;
     int splits, split_tiles;

@@ -70,7 +70,7 @@ struct Args {
     int32_t batch, hq, hkv, G, max_q, max_ctx, num_pages, max_pages, page_shift;
     int32_t window, sinks;
     int32_t row_blocks, block_rows, splits, split_tiles;
-    int32_t by_sequence;
+    int32_t order;  // of the row blocks: kByLength, kBySequence, kByGrid
     // shares > 0: the tiles of all sequences are cut into that many equal
     // shares; share c's part of sequence b is slot c + b < n_slots
     int32_t shares, n_slots;
@@ -92,6 +92,70 @@ __device__ __forceinline__ Seq seq_of(const Args& a, int b) {
     if (o0 < 0 || o1 < o0 || o1 > a.total_q) return {0, 0, 0, true};
     const int n = o1 - o0;
     return {o0, min(n, a.max_q), ctx - n, c != ctx || n > a.max_q};
+}
+
+// Row block number idx of the batch, counting those that hold rows: its sequence
+// and its place from the sequence's end (the last block has the longest key
+// range).  kByLength: the last blocks of all sequences, then those before them,
+// and so on (batches of up to a wave's lanes); kBySequence: one sequence after
+// the other; kByGrid: idx counts `row_blocks` for every sequence, whether it has
+// them or not (batches too large to look through).  Counted by grid, blocks
+// without rows would lie in between at a fixed stride, and those with rows all
+// fall on the same shader engines: four ragged prompts 347 us, 272 counted.
+// false: there is no such block.
+enum { kByLength, kBySequence, kByGrid };
+__device__ __forceinline__ bool find_block(const Args& a, int idx, bool first, int& b, int& rev) {
+    const int lane = lane_id();
+    auto blocks_of = [&](int bb, bool& bad) {
+        if (bb >= a.batch) return 0;
+        const Seq sq = seq_of(a, bb);
+        bad |= sq.bad;
+        return (sq.n * a.G + a.block_rows - 1) / a.block_rows;
+    };
+    bool bad = false, found = false;
+    b = rev = 0;
+    if (a.order == kByLength) {
+        const int n = blocks_of(lane, bad);
+        auto upto = [&](int r) {  // blocks with rev < r
+            return __builtin_amdgcn_readlane((int)wave_scan_dpp(min(n, r)), kWave - 1);
+        };
+        int lo = 0, hi = a.row_blocks;  // upto(lo) <= idx < upto(hi), if any
+        found = idx < upto(hi);
+        while (found && hi - lo > 1) {
+            const int mid = (lo + hi) >> 1;
+            if (upto(mid) <= idx)
+                lo = mid;
+            else
+                hi = mid;
+        }
+        const int j = idx - upto(lo);
+        const int incl = (int)wave_scan_dpp(n > lo ? 1 : 0);
+        const uint64_t hit = __ballot(incl > j);
+        b = hit ? __ffsll((unsigned long long)hit) - 1 : 0;
+        rev = lo;
+    } else if (a.order == kBySequence) {
+        int base = 0;
+        for (int b0 = 0; b0 < a.batch && (!found || first); b0 += kWave) {
+            const int n = blocks_of(b0 + lane, bad), incl = (int)wave_scan_dpp(n);
+            const uint64_t hit = __ballot(base + incl > idx);
+            if (hit && !found) {
+                const int at = __ffsll((unsigned long long)hit) - 1;
+                b = b0 + at;
+                rev = idx - base - __builtin_amdgcn_readlane(incl - n, at);
+                found = true;
+            }
+            base += __builtin_amdgcn_readlane(incl, kWave - 1);
+        }
+    } else {
+        b = idx % a.batch;
+        rev = idx / a.batch;
+        found = rev < blocks_of(b, bad);
+        first = rev == 0;
+    }
+    if (first && __ballot(bad) && lane == 0) raise_flag(a.flags, PRESTO_FLAG_BAD_SEQ);
+    b = uniform(b);
+    rev = uniform(rev);
+    return found;
 }
 
 // Keys that rows at positions p_lo .. p_hi see, [0, sinks) and [lo, hi), as a
@@ -588,16 +652,20 @@ __global__ __launch_bounds__(kWaves * kWave, NB == 1 && MODE != kShares ? 3 : 2)
     // its L2's channels (a long cache at 5.65 against 6.2 TB/s).
     int id = blockIdx.x;
     if constexpr (MODE != kShares) {
-        // the last row block (the longest key range) first
         const int split = id % a.splits;
         id /= a.splits;
         const int g = id % a.hkv;
         id /= a.hkv;
-        const int b = id % a.batch, rev = id / a.batch;
+        int b = id, rev = 0;
+        if constexpr (MODE == kOnce) {
+            const Seq sq = seq_of(a, b);
+            if (g == 0 && split == 0 && tid == 0 && sq.bad) raise_flag(a.flags, PRESTO_FLAG_BAD_SEQ);
+            if (sq.n == 0) return;
+        } else if (!find_block(a, id, id == 0 && g == 0 && split == 0, b, rev)) {
+            return;
+        }
         const Seq sq = seq_of(a, b);
         const int rb = (sq.n * a.G + R - 1) / R - 1 - rev;
-        if (rev == 0 && g == 0 && split == 0 && tid == 0 && sq.bad) raise_flag(a.flags, PRESTO_FLAG_BAD_SEQ);
-        if (rb < 0) return;
         if (split > 0) {
             const int row0 = rb * R;
             const Span sp = span_of(a, sq.pos0 + row0 / a.G, sq.pos0 + (min(row0 + R, sq.n * a.G) - 1) / a.G);
@@ -717,25 +785,21 @@ __global__ __launch_bounds__(kTileWaves * kWave) void paged_attn_tiles_kernel(Ar
     __shared__ int32_t s_page[kTilePages];
     __shared__ int s_bad[kTileRows], s_any;
 
-    // Blocks: neighbours differ in the KV head, so that the row blocks of one
+    // Neighbouring blocks differ in the KV head, so that the row blocks of one
     // head, which read the same keys, meet in the L2 of one XCD (every eighth
-    // block).  The last row block (the longest key range) first, of all
-    // sequences; or one sequence after the other where the keys of a head do
-    // not fit an L2 (see the host).
+    // block).
     int id = blockIdx.x;
     const int g = id % a.hkv;
     id /= a.hkv;
     const int split = id % a.splits;
     id /= a.splits;
-    const int b = a.by_sequence ? id / a.row_blocks : id % a.batch;
-    const int rev = a.by_sequence ? id % a.row_blocks : id / a.batch;
+    int b, rev;
+    if (!find_block(a, id, id == 0 && g == 0 && split == 0, b, rev)) return;
     const Seq sq = seq_of(a, b);
     const int rows = sq.n * a.G;
     const int rb = (rows + a.block_rows - 1) / a.block_rows - 1 - rev;
     const int tid = threadIdx.x, lane = lane_id();
     const int wave = uniform(tid / kWave);
-    if (rev == 0 && g == 0 && split == 0 && tid == 0 && sq.bad) raise_flag(a.flags, PRESTO_FLAG_BAD_SEQ);
-    if (rb < 0) return;
     const int row0 = rb * a.block_rows;  // (a multiple of 32, at most kTileRows)
     const int row_end = min(row0 + a.block_rows, rows);
     const Span sp = span_of(a, sq.pos0 + row0 / a.G, sq.pos0 + (row_end - 1) / a.G);
@@ -1219,6 +1283,15 @@ int64_t longest_list(const presto_paged_attn_desc* d, int64_t rows) {
     return span < all ? span : all;
 }
 
+// Row blocks of a grid, and how they are counted (find_block).
+int64_t counted_blocks(const presto_paged_attn_desc* d, PagedPlan& p) {
+    const int64_t batch = d->pages.batch, all = batch * p.row_blocks;
+    p.order = batch <= kWave ? kByLength : batch <= 2048 ? kBySequence : kByGrid;
+    // (sequences end in a part of a block each)
+    const int64_t most = d->total_q * (d->hq / d->pages.hkv) / p.block_rows + batch;
+    return p.order != kByGrid && most < all ? most : all;
+}
+
 // The kernel of tiles: rows per workgroup and splits, by modelled time in us.
 // A workgroup takes about 8 beside its tiles (page numbers, queries, first
 // tiles, output), a tile of 64 keys 1.75 with two waves of rows per SIMD and
@@ -1255,11 +1328,12 @@ void plan_tiles(const presto_paged_attn_desc* d, int64_t rows, PagedPlan& p) {
         }
     }
     p.row_blocks = (int)cdiv(rows, p.block_rows);
-    p.blocks = heads * p.row_blocks * p.splits;
+    p.blocks = heads / d->pages.batch * counted_blocks(d, p) * p.splits;
     // K and V of a head past the 4 MB of an XCD's L2: its row blocks side by
     // side (4 sequences of 2048 new tokens on 30720: 4178 -> 4037 us; on 4096:
     // 668 -> 677)
-    p.by_sequence = longest_list(d, p.block_rows) * d->pages.head_dim * 4 > (4 << 20);
+    if (p.order == kByLength && longest_list(d, p.block_rows) * d->pages.head_dim * 4 > (4 << 20))
+        p.order = kBySequence;
 }
 
 // The kernel of rows.
@@ -1281,7 +1355,7 @@ void plan_rows(const presto_paged_attn_desc* d, int64_t rows, PagedPlan& p) {
         p.split_tiles = (int)(cdiv(cdiv(all * cdiv(mean, T), 2 * wgs), kWaves) * kWaves);
         if (p.split_tiles > tiles) p.split_tiles = (int)tiles;
         p.splits = (int)cdiv(tiles, p.split_tiles);
-        p.blocks = all * p.splits;
+        p.blocks = d->pages.hkv * counted_blocks(d, p) * p.splits;
         return;
     }
     // Few rows are a stream of the cache: what counts is that all CUs end
@@ -1402,7 +1476,7 @@ presto_status launch_paged_attn(const presto_paged_attn_desc* d, const PagedPlan
     a.sinks = d->window > 0 ? d->sinks : 0;
     a.row_blocks = p.row_blocks;
     a.block_rows = p.block_rows;
-    a.by_sequence = p.by_sequence;
+    a.order = p.order;
     a.splits = p.splits;
     a.split_tiles = p.split_tiles;
     a.shares = p.shares;

@@ -447,9 +447,10 @@ presto_status presto_flatten_slots(int32_t batch, int32_t n_max, int32_t slots,
  *
  * Limits: page_size a power of two, 16 .. 1024; head_dim in {64, 128}; hkv
  * 1 .. 4096; 1 <= num_pages; max_pages 1 .. 2^20, max_pages * page_size <
- * 2^30; batch >= 0 (0: nothing to do); layers >= 1; page_stride >= page_size *
- * hkv * head_dim (0: exactly that), layer_stride >= 0; pools 16-byte aligned
- * with strides of a multiple of 16 bytes.  Layers of a pool must not overlap.
+ * 2^30; batch 0 .. 2^23 - 1 (0: nothing to do), batch * max_pages < 2^31;
+ * layers >= 1; page_stride >= page_size * hkv * head_dim (0: exactly that),
+ * layer_stride >= 0; pools 16-byte aligned with strides of a multiple of 16
+ * bytes.  Layers of a pool must not overlap.
  */
 typedef struct {
     int32_t batch, max_pages;
@@ -479,18 +480,22 @@ typedef struct {
  *   q, out [total_q, hq, head_dim]; every n_b <= max_q
  *
  * q rows are q_stride elements apart (a slice of a wider projection), out is
- * contiguous.  A page-table entry that a visible key needs and that lies
- * outside the pool raises PRESTO_FLAG_BAD_PAGE; its keys count as not
- * visible.  ctx[b] outside 0 .. max_ctx is cut to that range, n_b > max_q to
- * the first max_q rows (the others are not written), and offsets out of
- * order or past total_q skip the sequence; each raises PRESTO_FLAG_BAD_SEQ.
+ * contiguous and overlaps no input.  A page-table entry that a visible key
+ * needs and that lies outside the pool raises PRESTO_FLAG_BAD_PAGE; its keys
+ * count as not visible.  ctx[b] outside 0 .. max_ctx is cut to that range and
+ * n_b > max_q to the first max_q rows (the others are not written); offsets
+ * that run backwards or past total_q skip that sequence (rows of others that
+ * then overlap may be skipped too).  Each raises PRESTO_FLAG_BAD_SEQ.
  * A K or V that is not finite reaches the queries that see it only.
  * Arithmetic: bf16 inputs use bf16 matrix cores with fp32 accumulation and
  * fp32 softmax; fp32 inputs use fp32 throughout.
  * Limits: hq % hkv == 0; max_ctx <= max_pages * page_size; window, sinks 0 ..
  * 2^30 (sinks without a window change nothing); max_q * hq / hkv < 2^30,
- * total_q < 2^30; bf16 and fp32; q and out 16-byte aligned, q_stride a
- * multiple of 16 bytes.
+ * total_q < 2^30, batch * max_q * hq < 2^31 and at most 2^23 workgroups
+ * (PRESTO_ERR_UNSUPPORTED beyond); q, out and the workspace 16-byte aligned,
+ * q_stride a multiple of 16 bytes.
+ * The workspace size depends on every field (a shorter context or fewer new
+ * tokens may be split further and need more): it is asked for per shape.
  */
 typedef struct {
     presto_pages_desc pages;
@@ -541,9 +546,12 @@ presto_status presto_pages_reserve(const presto_pages_desc *desc, int32_t *refs,
  * write fewer rows than offsets gives it.  Positions without a page are
  * skipped (PRESTO_FLAG_BAD_PAGE); a sequence whose lengths or offsets do not
  * fit (more than max_new or than its rows, offsets out of order or past
- * new_rows) is skipped (PRESTO_FLAG_BAD_SEQ).  No page is written that another
- * sequence shares as long as pages come from the calls here.
- * Limits: new_rows < 2^31; 16-byte aligned, new_stride a multiple of 16 bytes.
+ * new_rows) is skipped (PRESTO_FLAG_BAD_SEQ).  Pages that come from the calls
+ * here are not shared where a sequence appends; a program that moves a
+ * sequence's ctx back (to drop rejected tokens) keeps it at or above the length
+ * at which it was last forked.
+ * Limits: new_rows < 2^31, batch * ceil(max_new / 16) < 2^23; 16-byte aligned,
+ * new_stride a multiple of 16 bytes.
  */
 presto_status presto_append_kv(const presto_pages_desc *desc, const void *k_new, const void *v_new,
                                int64_t new_rows, int64_t new_stride, const int32_t *offsets,

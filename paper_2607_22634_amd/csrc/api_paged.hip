@@ -56,6 +56,8 @@ static presto_status check_pages(presto_pages_desc& p, const char* who) {
     REQUIRE(p.max_pages >= 1 && p.max_pages <= (1 << 20) &&
                 (int64_t)p.max_pages * p.page_size < ((int64_t)1 << 30),
             "%s: max_pages=%d outside 1..2^20 or 2^30 positions or more", who, p.max_pages);
+    REQUIRE(p.batch < (1 << 23) && (int64_t)p.batch * p.max_pages < ((int64_t)1 << 31),
+            "%s: 2^23 sequences or 2^31 table entries, or more", who);
     REQUIRE(p.layers >= 1, "%s: layers < 1", who);
     const int64_t page = (int64_t)p.page_size * p.hkv * p.head_dim;
     const int64_t unit = p.dt == PRESTO_DT_BF16 ? 8 : 4;
@@ -198,7 +200,8 @@ presto_status presto_append_kv(const presto_pages_desc* desc, const void* k_new,
     REQUIRE(new_stride >= row && new_stride <= ((int64_t)1 << 31) &&
                 new_stride % (d.dt == PRESTO_DT_BF16 ? 8 : 4) == 0,
             "%s: new_stride %lld", who, (long long)new_stride);
-    REQUIRE((int64_t)d.batch * ((max_new + (int64_t)15) / 16) < ((int64_t)1 << 31), "%s: too many rows", who);
+    REQUIRE((int64_t)d.batch * ((max_new + (int64_t)15) / 16) < ((int64_t)1 << 23),
+            "%s: batch * max_new too large for one call", who);
     if (d.batch == 0 || max_new == 0 || new_rows == 0) return PRESTO_OK;
     REQUIRE(k_new && v_new && offsets && k_pages && v_pages && page_table && ctx && ctx_new, "%s: null pointer",
             who);

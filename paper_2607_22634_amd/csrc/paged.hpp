@@ -17,7 +17,8 @@ struct PagedPlan {
     int block_rows, row_blocks;
     int splits, split_tiles;
     int shares, n_slots;  // shares > 0: equal shares in the place of splits
-    int64_t blocks;
+    int64_t blocks, merge_blocks;
+    int merge_parts;
     size_t o_bytes, ml_bytes, bytes;  // workspace
 };
 

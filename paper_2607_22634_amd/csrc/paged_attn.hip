@@ -114,7 +114,10 @@ __device__ __forceinline__ bool find_block(const Args& a, int idx, bool first, i
     };
     bool bad = false, found = false;
     b = rev = 0;
-    if (a.order == kByLength) {
+    if (a.order == kByLength && a.batch == 1) {
+        rev = idx;
+        found = idx < blocks_of(0, bad);
+    } else if (a.order == kByLength) {
         const int n = blocks_of(lane, bad);
         auto upto = [&](int r) {  // blocks with rev < r
             return __builtin_amdgcn_readlane((int)wave_scan_dpp(min(n, r)), kWave - 1);
@@ -1401,8 +1404,17 @@ PagedPlan paged_plan(const presto_paged_attn_desc* d) {
         p.ml_bytes = (size_t)(parts * rows) * sizeof(float2);
         p.bytes = p.o_bytes + p.ml_bytes + (p.shares ? (size_t)d->pages.batch * sizeof(int2) : 0);
     }
-    // (a grid holds fewer than 2^31 workgroups; the merge takes some per row)
-    p.fits = p.blocks < ((int64_t)1 << 31) && (int64_t)d->pages.batch * d->max_q * d->hq < ((int64_t)1 << 31);
+    const int64_t out_rows = (int64_t)d->pages.batch * d->max_q * d->hq;
+    if (p.splits > 1 || p.shares > 0) {
+        // four splits or fewer per part
+        const int groups = kMergeThreads / (d->pages.head_dim / 4);
+        const int each = p.shares ? p.shares / d->pages.batch + 2 : p.splits;
+        p.merge_parts = 1;
+        while (p.merge_parts < groups && p.merge_parts * 4 < each) p.merge_parts *= 2;
+        p.merge_blocks = cdiv(out_rows, groups / p.merge_parts);
+    }
+    // (fewer than 2^32 threads in a grid, and row numbers of 32 bits)
+    p.fits = p.blocks < ((int64_t)1 << 23) && p.merge_blocks < ((int64_t)1 << 24) && out_rows < ((int64_t)1 << 31);
     return p;
 }
 
@@ -1430,12 +1442,9 @@ void launch_attn(const PagedPlan& p, const Args& a, hipStream_t stream) {
         launch_rows<BF16, D, 2>(p, a, stream);
     }
     if (p.splits > 1 || p.shares > 0) {
-        constexpr int T = BF16 ? 32 : 16, GROUPS = kMergeThreads / (D / 4);
-        // four splits or fewer per part
-        int parts = 1;
-        const int each = p.shares ? p.shares / a.batch + 2 : p.splits;
-        while (parts < GROUPS && parts * 4 < each) parts *= 2;
-        const unsigned grid = (unsigned)cdiv((int64_t)a.batch * a.max_q * a.hq, GROUPS / parts);
+        constexpr int T = BF16 ? 32 : 16;
+        const unsigned grid = (unsigned)p.merge_blocks;
+        const int parts = p.merge_parts;
         if (p.tiles)
             paged_attn_merge_kernel<BF16, D, kKeyTile>
                 <<<grid, kMergeThreads, 0, stream>>>(a, parts);

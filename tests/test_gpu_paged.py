@@ -48,14 +48,15 @@ class Cache:
         pages = len(used) + spare
         order = rng.permutation(pages)
         shape = (pages, 2, page, hkv, d) if pair else (2, pages, page, hkv, d)
-        both = torch.full(shape, float("nan"), dtype=TYPES[dtype])
+        both = torch.from_numpy(rng.standard_normal(shape, dtype=np.float32)).to(TYPES[dtype])
         self.k_h, self.v_h = (both[:, 0], both[:, 1]) if pair else (both[0], both[1])
+        unseen = np.ones((pages, page), bool)
         for i, (b, x) in enumerate(used):
             table[b, x] = order[i]
-            m = torch.from_numpy(keep[b][x * page:(x + 1) * page])
-            for pool in (self.k_h, self.v_h):
-                rows = torch.from_numpy(rng.standard_normal((int(m.sum()), hkv, d), dtype=np.float32))
-                pool[order[i], :len(m)][m] = rows.to(TYPES[dtype])
+            m = keep[b][x * page:(x + 1) * page]
+            unseen[order[i], :len(m)] = ~m
+        for pool in (self.k_h, self.v_h):
+            pool[torch.from_numpy(unseen)] = float("nan")
         both = both.to(DEV)
         self.k, self.v = (both[:, 0], both[:, 1]) if pair else (both[0], both[1])
         self.table_h, self.table, self.ctx = table, ints(table.tolist()), ints(list(ctx))
@@ -75,6 +76,8 @@ def queries(rng, n, hq, d, dtype, wide=False):
 def close(got, q, cache, offs, window, sinks, scale=None):
     got, qh = got.double().cpu().numpy(), q.double().cpu().numpy()
     for b, n in enumerate(cache.new):
+        if n == 0:
+            continue
         k, v = cache.rows(b)
         s = slice(offs[b], offs[b] + n)
         want, bound = R.attention(qh[s], k, v, cache.ctx_l[b] - n, window, sinks, scale, cache.dtype)
@@ -150,13 +153,14 @@ def test_long_contexts_split_and_joined(dtype, batch, n, hint, mask):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("n,past", [(3, 50), (90, 10), (300, 0), (90, 3000)])
-def test_values_that_are_not_finite_reach_their_own_queries_only(dtype, n, past):
+@pytest.mark.parametrize("n,past,window", [(3, 50, 60), (90, 10, 60), (300, 0, 60), (90, 3000, 60), (90, 1000, 0),
+                                           (3, 1500, 0), (200, 0, 0)])
+def test_values_that_are_not_finite_reach_their_own_queries_only(dtype, n, past, window):
     """inf and NaN in K or V of single keys: queries that do not see the key
     are as they were, those that see it are not finite (or, for K = -inf, as
     the definition has it)."""
     rng = np.random.default_rng([3, n, past])
-    L, hq, hkv, d, window, sinks = past + n, 4, 2, 64, 60, 2
+    L, hq, hkv, d, sinks = past + n, 4, 2, 64, 2
     c = Cache(rng, [L], [n], 32, hkv, d, dtype, window, sinks)
     q = queries(rng, n, hq, d, dtype)
     offs = ints([0, n])
@@ -173,11 +177,92 @@ def test_values_that_are_not_finite_reach_their_own_queries_only(dtype, n, past)
         k, v = c.rows(0)
         want, bound = R.attention(q.double().cpu().numpy(), k, v, past, window, sinks, None, dtype)
         g = got.double().cpu().numpy()
-        assert (np.abs(g - want)[~sees] <= bound[~sees]).all(), (key, name, val)
+        with np.errstate(invalid="ignore"):
+            assert (np.abs(g - want)[~sees] <= bound[~sees]).all(), (key, name, val)
         assert not np.isfinite(g[sees, 2:]).any(), (key, name, val)
         good = torch.from_numpy(rng.standard_normal((hkv, d), dtype=np.float32)).to(TYPES[dtype])
         getattr(c, name)[page, row], getattr(c, name + "_h")[page, row] = good.to(DEV), good
         base = run()
+
+
+def _ragged(rng, batch, lo, hi):
+    return [int(x) for x in rng.integers(lo, hi + 1, batch)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("batch,most,past", [(1, 700, 0), (3, 150, 900), (70, 40, 60), (2100, 9, 12)])
+def test_ragged_prompts_of_small_and_large_batches(dtype, batch, most, past):
+    """Row blocks counted by length, by sequence and by grid; a sample of the
+    sequences is compared (all rows of small batches)."""
+    rng = np.random.default_rng([16, batch])
+    new = _ragged(rng, batch, 0, most)
+    new[-1] = most
+    ctx = [n + p for n, p in zip(new, _ragged(rng, batch, 0, past))]
+    mask = (0, 0) if batch % 2 else (50, 3)
+    c = Cache(rng, ctx, new, 16, 1, 64, dtype, *mask)
+    offs = np.concatenate([[0], np.cumsum(new)]).tolist()
+    q = queries(rng, offs[-1], 8, 64, dtype)
+    f = flag()
+    out = P.presto_window_attention(q, ints(offs), most, c.k, c.v, c.table, c.ctx, window=mask[0], sinks=mask[1],
+                                    flags=f)
+    assert f.item() == 0 and torch.isfinite(out).all()
+    pick = set(range(batch)) if batch <= 3 else set(rng.choice(batch, 12, replace=False).tolist()) | {0, batch - 1}
+    c.new = [n if b in pick else 0 for b, n in enumerate(new)]
+    close(out, q, c, offs, *mask)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("batch,hi", [(5, 4000), (40, 900), (130, 700), (2100, 600)])
+@pytest.mark.parametrize("n", [1, 3])
+def test_ragged_contexts_in_shares(dtype, batch, hi, n):
+    """Batches of very different lengths, empty sequences among them, cut into
+    equal shares (or too large a batch for that)."""
+    rng = np.random.default_rng([17, batch, n])
+    ctx = [int(x) for x in np.exp(rng.uniform(0, np.log(hi), batch))]
+    ctx[batch // 2], ctx[-1] = 0, hi
+    new = [min(n, x) if b % 5 else 0 for b, x in enumerate(ctx)] if n > 1 else [1] * batch
+    d = 64 if batch > 100 else 128
+    c = Cache(rng, ctx, [1] * batch, 16, 2, d, dtype)
+    c.new = new
+    offs = np.concatenate([[0], np.cumsum(new)]).tolist()
+    q = queries(rng, offs[-1], 6, d, dtype)
+    f = flag()
+    if n == 1:
+        out = P.presto_paged_attention(q, c.k, c.v, c.table, c.ctx, max_ctx=hi, flags=f)
+    else:
+        out = P.presto_window_attention(q, ints(offs), n, c.k, c.v, c.table, c.ctx, max_ctx=hi, flags=f)
+    assert f.item() == 0 and torch.isfinite(out).all()
+    pick = set(rng.choice(batch, min(batch, 14), replace=False).tolist()) | {0, batch - 1, batch // 2 - 1}
+    assert n > 1 or not out[batch // 2].any()
+    c.new = [x if b in pick and ctx[b] else 0 for b, x in enumerate(new)]
+    close(out, q, c, offs, 0, 0)
+
+
+def test_more_pages_than_one_workgroup_keeps():
+    """A context whose page numbers do not fit the LDS of one workgroup."""
+    rng = np.random.default_rng(18)
+    L, n = 140000, 20
+    c = Cache(rng, [L], [1], 16, 1, 64, "bf16")
+    c.new = [n]
+    q = queries(rng, n, 2, 64, "bf16")
+    out = P.presto_window_attention(q, ints([0, n]), n, c.k, c.v, c.table, c.ctx)
+    close(out, q, c, [0], 0, 0)
+
+
+@pytest.mark.parametrize("heads,n,ctx", [((32, 8, 128), 130, 130), ((32, 8, 128), 600, 700), ((16, 1, 128), 100, 2000),
+                                         ((12, 4, 64), 513, 900), ((8, 8, 64), 257, 257)])
+def test_blocks_of_64_128_and_256_rows(heads, n, ctx):
+    """The plans of short, long and wide prompts (heads x tokens), a sample of
+    the rows against the reference."""
+    rng = np.random.default_rng([19, n])
+    hq, hkv, d = heads
+    c = Cache(rng, [ctx], [n], 32, hkv, d, "bf16", 300, 4)
+    q = queries(rng, n, hq, d, "bf16")
+    out = P.presto_window_attention(q, ints([0, n]), n, c.k, c.v, c.table, c.ctx, window=300, sinks=4)
+    k, v = c.rows(0)
+    for i in sorted({0, 1, 15, 16, 63, 64, n // 2, n - 2, n - 1}):
+        want, bound = R.attention(q[i:i + 1].double().cpu().numpy(), k, v, ctx - n + i, 300, 4)
+        assert (np.abs(out[i:i + 1].double().cpu().numpy() - want) <= bound).all(), i
 
 
 def test_equal_and_extreme_scores():

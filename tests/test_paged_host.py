@@ -1,6 +1,7 @@
 """Host-only checks of the paged cache: what its entry points refuse before
 anything is launched, workspace sizes, and the reference itself (no GPU)."""
 import ctypes
+import itertools
 
 import numpy as np
 import pytest
@@ -28,7 +29,7 @@ def attn(pool=None, **over):
 
 BAD_POOLS = [dict(page_size=8), dict(page_size=48), dict(page_size=2048), dict(head_dim=96), dict(hkv=0), dict(hkv=5000),
              dict(num_pages=0), dict(max_pages=0), dict(max_pages=(1 << 20) + 1), dict(max_pages=1 << 20, page_size=1024),
-             dict(layers=0), dict(dt=7), dict(batch=-1), dict(page_stride=16 * 8 * 128 - 8),
+             dict(batch=1 << 23), dict(batch=1 << 20, max_pages=1 << 12, page_size=16), dict(layers=0), dict(dt=7), dict(batch=-1), dict(page_stride=16 * 8 * 128 - 8),
              dict(page_stride=16 * 8 * 128 + 4), dict(layer_stride=-8), dict(layer_stride=12), dict(page_stride=1 << 62)]
 BAD_ATTN = [dict(hq=12), dict(hq=0), dict(max_ctx=-1), dict(max_ctx=64 * 16 + 1), dict(max_q=-1), dict(window=-1),
             dict(window=(1 << 30) + 1), dict(sinks=-1), dict(scale=0.0), dict(scale=float("nan")), dict(total_q=-1),
@@ -171,3 +172,31 @@ def test_reference_books_by_hand():
     assert b.refs == [1, 0, 1, 1, 0, 0] and b.ctx == [0, 20, 16]
     moves, to, live = b.compact()
     assert moves == [(3, 1, 16)] and live == 3 and b.table[1][:2] == [0, 1] and to == [0, -1, 2, 1, -1, -1]
+
+
+def test_calls_too_large_for_one_grid_are_refused():
+    """More workgroups, or query rows, than a launch can number."""
+    lib = P.lib()
+    big = attn(pages(batch=(1 << 23) - 1, max_pages=2), max_ctx=32, max_q=1, total_q=(1 << 23) - 1)
+    for fn, n in ((lib.presto_paged_attention, 6), (lib.presto_window_attention, 7)):
+        assert fn(ctypes.byref(big), *[FAKE] * n, None, FAKE, 1 << 40, None) == P.PRESTO_ERR_UNSUPPORTED
+    wide = attn(pages(batch=64, max_pages=1 << 16), max_ctx=1 << 20, max_q=1 << 20, total_q=64 << 20)
+    assert _attend(wide, False) == P.PRESTO_ERR_UNSUPPORTED
+    d = pages(batch=1 << 20, max_pages=1024)
+    assert lib.presto_append_kv(ctypes.byref(d), FAKE, FAKE, 1 << 30, 0, FAKE, 1000, *[FAKE] * 5, None, None) == \
+        P.PRESTO_ERR_INVALID_ARG
+
+
+@pytest.mark.parametrize("n", [1, 2, 5, 8, 9, 33, 64, 127, 1000, 4096])
+def test_workspaces_hold_the_partials(n):
+    """Whatever the plan, the workspace is either none or room for one partial
+    of every row at least, and the same each time it is asked for."""
+    lib = P.lib()
+    for dt, hkv, d in itertools.product((P.PRESTO_DT_BF16, P.PRESTO_DT_F32), (1, 8), (64, 128)):
+        for batch, ctx, window, total in itertools.product((1, 5, 70, 3000), (0, 17, 4100, 150000), (0, 500), (0, 1)):
+            pool = pages(batch=batch, max_pages=9400, hkv=hkv, head_dim=d, dt=dt)
+            a = attn(pool, hq=hkv * 4, max_q=n, max_ctx=ctx, window=window, sinks=4, total_q=batch * n,
+                     total_ctx=total * batch * ctx)
+            need = lib.presto_window_attention_workspace(ctypes.byref(a))
+            assert need == lib.presto_window_attention_workspace(ctypes.byref(a))
+            assert need == 0 or need >= hkv * 4 * n * (d * 4 + 8)

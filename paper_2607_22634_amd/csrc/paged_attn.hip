@@ -1354,9 +1354,9 @@ void plan_rows(const presto_paged_attn_desc* d, int64_t rows, PagedPlan& p) {
     // head_dim 128, two where they have 32 rows
     const int wgs = 256 * (d->pages.head_dim == 64 ? (p.nb == 1 ? 4 : 3) : (p.nb == 1 ? 3 : 2));
     if (p.row_blocks > 1) {
-        // twice as many, of at least one tile per wave
+        // twice as many, of at least one tile per wave; short lists are not cut
         p.split_tiles = (int)(cdiv(cdiv(all * cdiv(mean, T), 2 * wgs), kWaves) * kWaves);
-        if (p.split_tiles > tiles) p.split_tiles = (int)tiles;
+        if (p.split_tiles > tiles || tiles <= 3 * kWaves) p.split_tiles = (int)tiles;
         p.splits = (int)cdiv(tiles, p.split_tiles);
         p.blocks = d->pages.hkv * counted_blocks(d, p) * p.splits;
         return;
@@ -1392,20 +1392,17 @@ void plan_rows(const presto_paged_attn_desc* d, int64_t rows, PagedPlan& p) {
 
 PagedPlan paged_plan(const presto_paged_attn_desc* d) {
     PagedPlan p{};
+    // output rows are numbered in 32 bits, and a grid holds fewer than 2^32 threads
+    if ((double)d->pages.batch * d->max_q * d->hq >= 2147483648.0) return p;
+    const int64_t out_rows = (int64_t)d->pages.batch * d->max_q * d->hq;
     const int64_t rows = (int64_t)(d->hq / d->pages.hkv) * d->max_q;
     p.tiles = d->pages.dt == PRESTO_DT_BF16 && d->max_q > 1 && rows > 32;
     if (p.tiles)
         plan_tiles(d, rows, p);
     else
         plan_rows(d, rows, p);
-    if (p.splits > 1 || p.shares > 0) {
-        const int64_t parts = d->pages.hkv * (p.shares ? (int64_t)p.n_slots : (int64_t)d->pages.batch * p.splits);
-        p.o_bytes = (size_t)(parts * rows) * d->pages.head_dim * sizeof(float);
-        p.ml_bytes = (size_t)(parts * rows) * sizeof(float2);
-        p.bytes = p.o_bytes + p.ml_bytes + (p.shares ? (size_t)d->pages.batch * sizeof(int2) : 0);
-    }
-    const int64_t out_rows = (int64_t)d->pages.batch * d->max_q * d->hq;
-    if (p.splits > 1 || p.shares > 0) {
+    const bool cut = p.splits > 1 || p.shares > 0;
+    if (cut) {
         // four splits or fewer per part
         const int groups = kMergeThreads / (d->pages.head_dim / 4);
         const int each = p.shares ? p.shares / d->pages.batch + 2 : p.splits;
@@ -1413,8 +1410,13 @@ PagedPlan paged_plan(const presto_paged_attn_desc* d) {
         while (p.merge_parts < groups && p.merge_parts * 4 < each) p.merge_parts *= 2;
         p.merge_blocks = cdiv(out_rows, groups / p.merge_parts);
     }
-    // (fewer than 2^32 threads in a grid, and row numbers of 32 bits)
-    p.fits = p.blocks < ((int64_t)1 << 23) && p.merge_blocks < ((int64_t)1 << 24) && out_rows < ((int64_t)1 << 31);
+    p.fits = p.blocks < ((int64_t)1 << 23) && p.merge_blocks < ((int64_t)1 << 24);
+    if (cut && p.fits) {
+        const int64_t parts = d->pages.hkv * (p.shares ? (int64_t)p.n_slots : (int64_t)d->pages.batch * p.splits);
+        p.o_bytes = (size_t)(parts * rows) * d->pages.head_dim * sizeof(float);
+        p.ml_bytes = (size_t)(parts * rows) * sizeof(float2);
+        p.bytes = p.o_bytes + p.ml_bytes + (p.shares ? (size_t)d->pages.batch * sizeof(int2) : 0);
+    }
     return p;
 }
 

@@ -497,9 +497,9 @@ struct PagesWs {
 };
 PagesWs pages_ws(void* ws, int64_t num_pages, int64_t n) {
     PagesWs w{};
-    char* at = static_cast<char*>(ws);
+    const uintptr_t at = reinterpret_cast<uintptr_t>(ws);  // (null where only the size is asked for)
     auto take = [&](int64_t bytes) {
-        char* p = at + w.bytes;
+        const uintptr_t p = at + w.bytes;
         w.bytes += (size_t)up16(bytes);
         return p;
     };

@@ -16,7 +16,7 @@ struct PagedPlan {
     int nb;            // (rows) 16-row blocks per workgroup
     int block_rows, row_blocks;
     int splits, split_tiles;
-    int shares, n_slots;  // shares > 0: equal shares in the place of splits
+    int pieces, n_slots;  // (rows) pieces > 0: pieces of one length in the place of splits
     int64_t blocks, merge_blocks;
     int merge_parts;
     size_t o_bytes, ml_bytes, bytes;  // workspace

@@ -61,7 +61,7 @@ struct Args {
     char* out;
     // partials: the output normalised by the part's own sum [part, rho, D] fp32
     // and (reference in log2 units, sum) [part, rho]; part = (b, g, split), or
-    // (g, slot) with shares
+    // (g, piece)
     float* part_o;
     float2* part_ml;
     int32_t* flags;
@@ -71,10 +71,10 @@ struct Args {
     int32_t window, sinks;
     int32_t row_blocks, block_rows, splits, split_tiles;
     int32_t order;  // of the row blocks: kByLength, kBySequence, kByGrid
-    // shares > 0: the tiles of all sequences are cut into that many equal
-    // shares; share c's part of sequence b is slot c + b < n_slots
-    int32_t shares, n_slots;
-    int2* slots;  // [batch] first and last slot of a sequence
+    // pieces > 0: every sequence is cut into pieces of one length, such that the
+    // batch has `pieces` of them and one more per sequence at most (n_slots)
+    int32_t pieces, n_slots;
+    int2* slots;  // [batch] a sequence's first and last piece, counted over the batch
     float scale_log2;  // scale * log2(e)
 };
 
@@ -270,10 +270,9 @@ __device__ float2 row_alone(const Args& a, const Span& sp, int b, int g, int64_t
 // units), so that the common tile needs no reduction across lanes.
 //
 // kOnce: every key is read by one workgroup, past the caches (a long cache at
-// 5.45 TB/s through them, 5.65 past them).  kShares: the same, each workgroup
-// taking an equal share of all tiles of the batch (see below).
+// 5.45 TB/s through them, 5.65 past them).
 constexpr int kWaves = 4;
-enum { kCached, kOnce, kShares };
+enum { kCached, kOnce };
 
 template <int MODE>
 __device__ __forceinline__ uint4 load16(const char* p) {
@@ -284,14 +283,14 @@ __device__ __forceinline__ uint4 load16(const char* p) {
 // Tiles of a sequence, at least one (so that some workgroup clears the rows of
 // an empty one).
 template <int T>
-__device__ __forceinline__ int share_tiles(const Args& a, int b) {
+__device__ __forceinline__ int tiles_of(const Args& a, int b) {
     if (b >= a.batch) return 0;
     const Seq sq = seq_of(a, b);
     return max((span_of(a, sq.pos0, sq.pos0 + max(sq.n, 1) - 1).n + T - 1) / T, 1);
 }
 
 template <bool BF16, int D, int NB, int MODE>
-__global__ __launch_bounds__(kWaves * kWave, NB == 1 && MODE != kShares ? 3 : 2) void paged_attn_rows_kernel(Args a) {
+__global__ __launch_bounds__(kWaves * kWave, NB == 1 ? 3 : 2) void paged_attn_rows_kernel(Args a) {
     constexpr int E = BF16 ? 2 : 4;
     constexpr int KB = BF16 ? 2 : 1;  // 16-key groups per tile
     constexpr int T = 16 * KB;
@@ -313,10 +312,9 @@ __global__ __launch_bounds__(kWaves * kWave, NB == 1 && MODE != kShares ? 3 : 2)
 
     // Tiles t_begin .. t_end - 1 of a row block's keys, to part `part`, or
     // with part < 0 (the block's only one) to the output.
-    auto segment = [&](int b, int g, const Seq& sq, int rb, int t_begin, int t_end, int64_t part)
+    auto segment = [&](int b, int g, const Seq& sq, int rb, int t_begin, int t_end, int part)
                        __attribute__((always_inline)) {
-    int lane = lane_id();
-    asm volatile("" : "+v"(lane));  // (what follows from it is not kept in registers from segment to segment)
+    const int lane = lane_id();
     const int rows = sq.n * a.G;
     const int row0 = rb * R;
     const int p_lo = sq.pos0 + row0 / a.G, p_hi = sq.pos0 + (min(row0 + R, rows) - 1) / a.G;
@@ -587,7 +585,7 @@ __global__ __launch_bounds__(kWaves * kWave, NB == 1 && MODE != kShares ? 3 : 2)
     if (tid < R) s_bad[tid] = 0;
     __syncthreads();
 
-    const int64_t prow = part * a.G * a.max_q;
+    const int64_t prow = (int64_t)part * a.G * a.max_q;
     auto put = [&](int rho, int d, floatx4 v) {
         if (part >= 0) {
             *reinterpret_cast<floatx4*>(a.part_o + (prow + rho) * D + d) = v;
@@ -654,70 +652,58 @@ __global__ __launch_bounds__(kWaves * kWave, NB == 1 && MODE != kShares ? 3 : 2)
     // eighth block) meets all KV heads: rows of one head alone fall on few of
     // its L2's channels (a long cache at 5.65 against 6.2 TB/s).
     int id = blockIdx.x;
-    if constexpr (MODE != kShares) {
-        const int split = id % a.splits;
-        id /= a.splits;
-        const int g = id % a.hkv;
-        id /= a.hkv;
-        int b = id, rev = 0;
-        if constexpr (MODE == kOnce) {
-            const Seq sq = seq_of(a, b);
-            if (g == 0 && split == 0 && tid == 0 && sq.bad) raise_flag(a.flags, PRESTO_FLAG_BAD_SEQ);
-            if (sq.n == 0) return;
-        } else if (!find_block(a, id, id == 0 && g == 0 && split == 0, b, rev)) {
-            return;
-        }
-        const Seq sq = seq_of(a, b);
-        const int rb = (sq.n * a.G + R - 1) / R - 1 - rev;
-        if (split > 0) {
-            const int row0 = rb * R;
-            const Span sp = span_of(a, sq.pos0 + row0 / a.G, sq.pos0 + (min(row0 + R, sq.n * a.G) - 1) / a.G);
-            if (split * a.split_tiles * T >= sp.n) return;  // the merge knows
-        }
-        segment(b, g, sq, rb, split * a.split_tiles, (split + 1) * a.split_tiles,
-                a.splits > 1 ? ((int64_t)b * a.hkv + g) * a.splits + split : -1);
-    } else {
-        // a share: part of one sequence, or the end of one, whole ones and the
-        // start of another; it and the sequence never advance together past a
-        // boundary, so share + sequence numbers the parts
-        const int lane = lane_id();
-        const int share = id % a.shares, g = id / a.shares;
+    int g, b, rev = 0, t_begin, t_end, part = -1;
+    if (MODE == kOnce && a.pieces > 0) {
+        const int lane = lane_id(), idx = id % a.n_slots;
+        g = id / a.n_slots;
         int total = 0;
         for (int b0 = 0; b0 < a.batch; b0 += kWave)
-            total += __builtin_amdgcn_readlane((int)wave_scan_dpp(share_tiles<T>(a, b0 + lane)), kWave - 1);
-        const int shares = min(a.shares, (total + kWaves - 1) / kWaves);  // a tile per wave at least
-        if (share >= shares) return;
-        const int q = total / shares, r = total % shares;
-        int from = share * q + min(share, r), base = 0, b = 0;
-        const int to = from + q + (share < r ? 1 : 0);
-        for (int b0 = 0; b0 < a.batch; b0 += kWave) {
-            const int n = share_tiles<T>(a, b0 + lane), incl = (int)wave_scan_dpp(n);
-            const uint64_t hit = __ballot(base + incl > from);
+            total += __builtin_amdgcn_readlane((int)wave_scan_dpp(tiles_of<T>(a, b0 + lane)), kWave - 1);
+        // whole rounds of the waves; at least one
+        const int len = ((total + a.pieces - 1) / a.pieces + kWaves - 1) / kWaves * kWaves;
+        int base = 0, count = 0;
+        b = -1;
+        for (int b0 = 0; b0 < a.batch && b < 0; b0 += kWave) {
+            const int n = (tiles_of<T>(a, b0 + lane) + len - 1) / len, incl = (int)wave_scan_dpp(n);
+            const uint64_t hit = __ballot(base + incl > idx);
             if (hit) {
                 const int at = __ffsll((unsigned long long)hit) - 1;
                 b = b0 + at;
-                base += __builtin_amdgcn_readlane(incl - n, at);
-                break;
+                count = __builtin_amdgcn_readlane(n, at);
+                base += __builtin_amdgcn_readlane(incl, at) - count;
+            } else {
+                base += __builtin_amdgcn_readlane(incl, kWave - 1);
             }
-            base += __builtin_amdgcn_readlane(incl, kWave - 1);
         }
-        for (bool first = true; b < a.batch; ++b, first = false) {
-            if (!first) __syncthreads();  // the states in LDS have been read
-            const int tiles = uniform(share_tiles<T>(a, b));
-            const Seq sq = seq_of(a, b);
-            const int t0 = from - base, t1 = min(to - base, tiles);
-            const bool whole = t0 == 0 && t1 == tiles;
-            if (g == 0 && tid == 0) {
-                if (t0 == 0 && sq.bad) raise_flag(a.flags, PRESTO_FLAG_BAD_SEQ);
-                if (t0 == 0) a.slots[b].x = share + b;
-                if (t1 == tiles) a.slots[b].y = share + b;
-            }
-            if (sq.n > 0) segment(b, g, sq, 0, t0, t1, whole ? -1 : (int64_t)g * a.n_slots + share + b);
-            if (base + tiles >= to) return;
-            base += tiles;
-            from = base;
-        }
+        if (b < 0) return;
+        t_begin = (idx - base) * len;
+        t_end = t_begin + len;
+        if (count > 1) part = g * a.n_slots + idx;
+        if (idx == base && g == 0 && tid == 0) a.slots[b] = make_int2(idx, idx + count - 1);
+    } else {
+        const int split = id % a.splits;
+        id /= a.splits;
+        g = id % a.hkv;
+        id /= a.hkv;
+        b = id;
+        if (MODE == kCached && !find_block(a, id, id == 0 && g == 0 && split == 0, b, rev)) return;
+        t_begin = split * a.split_tiles;
+        t_end = t_begin + a.split_tiles;
+        if (a.splits > 1) part = (b * a.hkv + g) * a.splits + split;
     }
+    // (the same for the whole workgroup: scalars from here on)
+    b = uniform(b), g = uniform(g), rev = uniform(rev);
+    t_begin = uniform(t_begin), t_end = uniform(t_end), part = uniform(part);
+    const Seq sq = seq_of(a, b);
+    if (MODE == kOnce && sq.bad && g == 0 && t_begin == 0 && tid == 0) raise_flag(a.flags, PRESTO_FLAG_BAD_SEQ);
+    if (sq.n == 0) return;
+    const int rb = MODE == kOnce ? 0 : (sq.n * a.G + R - 1) / R - 1 - rev;
+    if (t_begin > 0) {
+        const int row0 = rb * R;
+        const Span sp = span_of(a, sq.pos0 + row0 / a.G, sq.pos0 + (min(row0 + R, sq.n * a.G) - 1) / a.G);
+        if (t_begin * T >= sp.n) return;  // the merge knows
+    }
+    segment(b, g, sq, rb, t_begin, t_end, part);
 }
 
 // Many query rows per KV head (bf16): tiles of 64 keys go from memory straight
@@ -1187,7 +1173,7 @@ __global__ __launch_bounds__(kMergeThreads) void paged_attn_merge_kernel(Args a,
         const int g = head / a.G, rho = tok * a.G + head - g * a.G;
         const int64_t all = (int64_t)a.G * a.max_q;
         int64_t first;
-        if (a.shares > 0) {
+        if (a.pieces > 0) {
             const int2 s = a.slots[b];
             first = (int64_t)g * a.n_slots + s.x;
             live = s.y - s.x + 1;
@@ -1200,7 +1186,7 @@ __global__ __launch_bounds__(kMergeThreads) void paged_attn_merge_kernel(Args a,
         const int64_t prow = first * all + rho;
         const float2* ml = a.part_ml + prow;
         const float* po = a.part_o + prow * D + ln * 4;
-        for (int s0 = part; s0 < (a.shares > 0 && live == 1 ? 0 : live); s0 += 4 * parts) {
+        for (int s0 = part; s0 < (a.pieces > 0 && live == 1 ? 0 : live); s0 += 4 * parts) {
             floatx4 v[4];
             float2 x[4];
 #pragma unroll
@@ -1254,7 +1240,7 @@ __global__ __launch_bounds__(kMergeThreads) void paged_attn_merge_kernel(Args a,
             for (int e = 0; e < 4; ++e) acc[e] = fmaf(w, v[e], acc[e]);
         }
     }
-    if (!live_row || (a.shares > 0 && live == 1)) return;  // (written by the one share that held it)
+    if (!live_row || (a.pieces > 0 && live == 1)) return;  // (a sequence in one piece is written already)
     const float inv = L == 0.f ? 0.f : 1.f / L;
     char* p = a.out + (((sq.r0 + tok) * a.hq + head) * D + ln * 4) * E;
     if constexpr (BF16)
@@ -1368,10 +1354,8 @@ void plan_rows(const presto_paged_attn_desc* d, int64_t rows, PagedPlan& p) {
     // * Sequences of about one length (known from total_ctx) are cut into as
     //   many splits as fill one round: 32 x 2048 keys in 3 splits 48 us, in 6
     //   52; 80 x 2048 uncut 114, in 2 splits 143.
-    // * Others, and those that would leave much of a last round empty, in equal
-    //   shares: 24 sequences of 200 .. 12000 keys 157 us in splits, 100 in
-    //   shares.  16 x 32768 in shares 328, in 6 splits 322: shares take more
-    //   registers, two workgroups per CU, and two such rounds.
+    // * Others, and those that would leave much of a last round empty, in pieces
+    //   of one length, of which there is about one round.
     p.splits = all < wgs ? (int)(wgs / all) : 1;
     p.split_tiles = (int)(cdiv(cdiv(tiles, p.splits), kWaves) * kWaves);
     if (tiles <= 3 * kWaves || p.split_tiles > tiles) p.split_tiles = (int)tiles;
@@ -1379,12 +1363,15 @@ void plan_rows(const presto_paged_attn_desc* d, int64_t rows, PagedPlan& p) {
     p.blocks = all * p.splits;
     const bool even = d->total_ctx > 0 && 10 * mean >= 9 * longest;
     const bool idle = all > wgs && cdiv(all, wgs) * wgs * 7 > all * 8;
-    // (every workgroup looks through the batch for its share)
+    // (every workgroup looks through the batch for its piece)
     const bool can = d->pages.batch <= 2048 && d->pages.batch * tiles < ((int64_t)1 << 30);
     if (tiles > 3 * kWaves && (!even || idle) && can) {
-        p.shares = 1024 / d->pages.hkv > 0 ? 1024 / d->pages.hkv : 1;
-        p.n_slots = p.shares + d->pages.batch;
-        p.blocks = (int64_t)p.shares * d->pages.hkv;
+        const int round = wgs / d->pages.hkv > 0 ? wgs / d->pages.hkv : 1;
+        // every sequence may end in a piece that is not full
+        p.pieces = round > 2 * d->pages.batch ? round - d->pages.batch : (round + 1) / 2;
+        p.n_slots = p.pieces + d->pages.batch;
+        p.blocks = (int64_t)p.n_slots * d->pages.hkv;
+        p.splits = 1;
     }
 }
 
@@ -1401,21 +1388,21 @@ PagedPlan paged_plan(const presto_paged_attn_desc* d) {
         plan_tiles(d, rows, p);
     else
         plan_rows(d, rows, p);
-    const bool cut = p.splits > 1 || p.shares > 0;
+    const bool cut = p.splits > 1 || p.pieces > 0;
     if (cut) {
         // four splits or fewer per part
         const int groups = kMergeThreads / (d->pages.head_dim / 4);
-        const int each = p.shares ? p.shares / d->pages.batch + 2 : p.splits;
+        const int each = p.pieces ? p.pieces / d->pages.batch + 2 : p.splits;
         p.merge_parts = 1;
         while (p.merge_parts < groups && p.merge_parts * 4 < each) p.merge_parts *= 2;
         p.merge_blocks = cdiv(out_rows, groups / p.merge_parts);
     }
     p.fits = p.blocks < ((int64_t)1 << 23) && p.merge_blocks < ((int64_t)1 << 24);
     if (cut && p.fits) {
-        const int64_t parts = d->pages.hkv * (p.shares ? (int64_t)p.n_slots : (int64_t)d->pages.batch * p.splits);
+        const int64_t parts = d->pages.hkv * (p.pieces ? (int64_t)p.n_slots : (int64_t)d->pages.batch * p.splits);
         p.o_bytes = (size_t)(parts * rows) * d->pages.head_dim * sizeof(float);
         p.ml_bytes = (size_t)(parts * rows) * sizeof(float2);
-        p.bytes = p.o_bytes + p.ml_bytes + (p.shares ? (size_t)d->pages.batch * sizeof(int2) : 0);
+        p.bytes = p.o_bytes + p.ml_bytes + (p.pieces ? (size_t)d->pages.batch * sizeof(int2) : 0);
     }
     return p;
 }
@@ -1425,9 +1412,7 @@ namespace {
 template <bool BF16, int D, int NB>
 void launch_rows(const PagedPlan& p, const Args& a, hipStream_t stream) {
     const unsigned grid = (unsigned)p.blocks;
-    if (p.shares > 0)
-        paged_attn_rows_kernel<BF16, D, NB, kShares><<<grid, kWaves * kWave, 0, stream>>>(a);
-    else if (p.row_blocks == 1)
+    if (p.row_blocks == 1)
         paged_attn_rows_kernel<BF16, D, NB, kOnce><<<grid, kWaves * kWave, 0, stream>>>(a);
     else
         paged_attn_rows_kernel<BF16, D, NB, kCached><<<grid, kWaves * kWave, 0, stream>>>(a);
@@ -1443,7 +1428,7 @@ void launch_attn(const PagedPlan& p, const Args& a, hipStream_t stream) {
     } else {
         launch_rows<BF16, D, 2>(p, a, stream);
     }
-    if (p.splits > 1 || p.shares > 0) {
+    if (p.splits > 1 || p.pieces > 0) {
         constexpr int T = BF16 ? 32 : 16;
         const unsigned grid = (unsigned)p.merge_blocks;
         const int parts = p.merge_parts;
@@ -1490,7 +1475,7 @@ presto_status launch_paged_attn(const presto_paged_attn_desc* d, const PagedPlan
     a.order = p.order;
     a.splits = p.splits;
     a.split_tiles = p.split_tiles;
-    a.shares = p.shares;
+    a.pieces = p.pieces;
     a.n_slots = p.n_slots;
     a.slots = reinterpret_cast<int2*>(static_cast<char*>(ws) + p.o_bytes + p.ml_bytes);
     a.scale_log2 = d->scale * kLog2e;

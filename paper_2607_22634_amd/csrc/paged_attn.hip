@@ -648,7 +648,7 @@ __global__ __launch_bounds__(kWaves * kWave, NB == 1 ? 3 : 2) void paged_attn_ro
     }
     };
 
-    // Neighbouring blocks differ in the split or share, so that an XCD (every
+    // Neighbouring blocks differ in the split or piece, so that an XCD (every
     // eighth block) meets all KV heads: rows of one head alone fall on few of
     // its L2's channels (a long cache at 5.65 against 6.2 TB/s).
     int id = blockIdx.x;
@@ -1354,19 +1354,21 @@ void plan_rows(const presto_paged_attn_desc* d, int64_t rows, PagedPlan& p) {
     // * Sequences of about one length (known from total_ctx) are cut into as
     //   many splits as fill one round: 32 x 2048 keys in 3 splits 48 us, in 6
     //   52; 80 x 2048 uncut 114, in 2 splits 143.
-    // * Others, and those that would leave much of a last round empty, in pieces
-    //   of one length, of which there is about one round.
+    // * Others in pieces of one length: about one round of them, three where
+    //   there are many sequences, each with an end that is not full (us: 16 of
+    //   1024 .. 8192 keys 61 in one round, 62 in three; 40 of 1000 .. 9000 155
+    //   and 138; 24 of 200 .. 12000 in splits of the longest 157, in pieces 102).
     p.splits = all < wgs ? (int)(wgs / all) : 1;
     p.split_tiles = (int)(cdiv(cdiv(tiles, p.splits), kWaves) * kWaves);
     if (tiles <= 3 * kWaves || p.split_tiles > tiles) p.split_tiles = (int)tiles;
     p.splits = (int)cdiv(tiles, p.split_tiles);
     p.blocks = all * p.splits;
     const bool even = d->total_ctx > 0 && 10 * mean >= 9 * longest;
-    const bool idle = all > wgs && cdiv(all, wgs) * wgs * 7 > all * 8;
     // (every workgroup looks through the batch for its piece)
     const bool can = d->pages.batch <= 2048 && d->pages.batch * tiles < ((int64_t)1 << 30);
-    if (tiles > 3 * kWaves && (!even || idle) && can) {
-        const int round = wgs / d->pages.hkv > 0 ? wgs / d->pages.hkv : 1;
+    if (tiles > 3 * kWaves && !even && can) {
+        int round = wgs / d->pages.hkv > 0 ? wgs / d->pages.hkv : 1;
+        if (4 * d->pages.batch > round) round *= 3;
         // every sequence may end in a piece that is not full
         p.pieces = round > 2 * d->pages.batch ? round - d->pages.batch : (round + 1) / 2;
         p.n_slots = p.pieces + d->pages.batch;

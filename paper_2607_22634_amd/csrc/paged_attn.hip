@@ -310,16 +310,65 @@ __global__ __launch_bounds__(kWaves * kWave, NB == 1 ? 3 : 2) void paged_attn_ro
     const int tid = threadIdx.x;
     const int wave = uniform(tid / kWave);
 
-    // Tiles t_begin .. t_end - 1 of a row block's keys, to part `part`, or
-    // with part < 0 (the block's only one) to the output.
-    auto segment = [&](int b, int g, const Seq& sq, int rb, int t_begin, int t_end, int part)
-                       __attribute__((always_inline)) {
+    // ---- which keys and rows: tiles t_begin .. t_end - 1 of row block rb, to part
+    // `part`, or with part < 0 (the rows' only one) to the output.
+    // Neighbouring blocks differ in the split or piece, so that an XCD (every
+    // eighth block) meets all KV heads: rows of one head alone fall on few of
+    // its L2's channels (a long cache at 5.65 against 6.2 TB/s).
+    int id = blockIdx.x;
+    int g, b, rev = 0, t_begin, t_end, part = -1;
+    if (MODE == kOnce && a.pieces > 0) {
+        const int lane = lane_id(), idx = id % a.n_slots;
+        g = id / a.n_slots;
+        int total = 0;
+        for (int b0 = 0; b0 < a.batch; b0 += kWave)
+            total += __builtin_amdgcn_readlane((int)wave_scan_dpp(tiles_of<T>(a, b0 + lane)), kWave - 1);
+        // whole rounds of the waves; at least one
+        const int len = ((total + a.pieces - 1) / a.pieces + kWaves - 1) / kWaves * kWaves;
+        int base = 0, count = 0;
+        b = -1;
+        for (int b0 = 0; b0 < a.batch && b < 0; b0 += kWave) {
+            const int n = (tiles_of<T>(a, b0 + lane) + len - 1) / len, incl = (int)wave_scan_dpp(n);
+            const uint64_t hit = __ballot(base + incl > idx);
+            if (hit) {
+                const int at = __ffsll((unsigned long long)hit) - 1;
+                b = b0 + at;
+                count = __builtin_amdgcn_readlane(n, at);
+                base += __builtin_amdgcn_readlane(incl, at) - count;
+            } else {
+                base += __builtin_amdgcn_readlane(incl, kWave - 1);
+            }
+        }
+        if (b < 0) return;
+        t_begin = (idx - base) * len;
+        t_end = t_begin + len;
+        if (count > 1) part = g * a.n_slots + idx;
+        if (idx == base && g == 0 && tid == 0) a.slots[b] = make_int2(idx, idx + count - 1);
+    } else {
+        const int split = id % a.splits;
+        id /= a.splits;
+        g = id % a.hkv;
+        id /= a.hkv;
+        b = id;
+        if (MODE == kCached && !find_block(a, id, id == 0 && g == 0 && split == 0, b, rev)) return;
+        t_begin = split * a.split_tiles;
+        t_end = t_begin + a.split_tiles;
+        if (a.splits > 1) part = (b * a.hkv + g) * a.splits + split;
+    }
+    // (the same for the whole workgroup: scalars from here on)
+    b = uniform(b), g = uniform(g), rev = uniform(rev);
+    t_begin = uniform(t_begin), t_end = uniform(t_end), part = uniform(part);
+    const Seq sq = seq_of(a, b);
+    if (MODE == kOnce && sq.bad && g == 0 && t_begin == 0 && tid == 0) raise_flag(a.flags, PRESTO_FLAG_BAD_SEQ);
+    if (sq.n == 0) return;
+    const int rb = MODE == kOnce ? 0 : (sq.n * a.G + R - 1) / R - 1 - rev;
     const int lane = lane_id();
     const int rows = sq.n * a.G;
     const int row0 = rb * R;
     const int p_lo = sq.pos0 + row0 / a.G, p_hi = sq.pos0 + (min(row0 + R, rows) - 1) / a.G;
     const Span sp = span_of(a, p_lo, p_hi);
     t_end = min(t_end, (sp.n + T - 1) / T);
+    if (t_begin > 0 && t_begin >= t_end) return;  // the merge knows
 
     const int t16 = lane & 15, tq = lane >> 4;
     const uint32_t RS = (uint32_t)(a.hkv * D * E);  // bytes from a cache row to the next
@@ -646,64 +695,6 @@ __global__ __launch_bounds__(kWaves * kWave, NB == 1 ? 3 : 2) void paged_attn_ro
         for (int d = tid * 4; d < D; d += NT * 4) put(rho, d, *reinterpret_cast<const floatx4*>(&s_acc[d]));
         if (tid == 0) put_ml(rho, ml.x, ml.y);
     }
-    };
-
-    // Neighbouring blocks differ in the split or piece, so that an XCD (every
-    // eighth block) meets all KV heads: rows of one head alone fall on few of
-    // its L2's channels (a long cache at 5.65 against 6.2 TB/s).
-    int id = blockIdx.x;
-    int g, b, rev = 0, t_begin, t_end, part = -1;
-    if (MODE == kOnce && a.pieces > 0) {
-        const int lane = lane_id(), idx = id % a.n_slots;
-        g = id / a.n_slots;
-        int total = 0;
-        for (int b0 = 0; b0 < a.batch; b0 += kWave)
-            total += __builtin_amdgcn_readlane((int)wave_scan_dpp(tiles_of<T>(a, b0 + lane)), kWave - 1);
-        // whole rounds of the waves; at least one
-        const int len = ((total + a.pieces - 1) / a.pieces + kWaves - 1) / kWaves * kWaves;
-        int base = 0, count = 0;
-        b = -1;
-        for (int b0 = 0; b0 < a.batch && b < 0; b0 += kWave) {
-            const int n = (tiles_of<T>(a, b0 + lane) + len - 1) / len, incl = (int)wave_scan_dpp(n);
-            const uint64_t hit = __ballot(base + incl > idx);
-            if (hit) {
-                const int at = __ffsll((unsigned long long)hit) - 1;
-                b = b0 + at;
-                count = __builtin_amdgcn_readlane(n, at);
-                base += __builtin_amdgcn_readlane(incl, at) - count;
-            } else {
-                base += __builtin_amdgcn_readlane(incl, kWave - 1);
-            }
-        }
-        if (b < 0) return;
-        t_begin = (idx - base) * len;
-        t_end = t_begin + len;
-        if (count > 1) part = g * a.n_slots + idx;
-        if (idx == base && g == 0 && tid == 0) a.slots[b] = make_int2(idx, idx + count - 1);
-    } else {
-        const int split = id % a.splits;
-        id /= a.splits;
-        g = id % a.hkv;
-        id /= a.hkv;
-        b = id;
-        if (MODE == kCached && !find_block(a, id, id == 0 && g == 0 && split == 0, b, rev)) return;
-        t_begin = split * a.split_tiles;
-        t_end = t_begin + a.split_tiles;
-        if (a.splits > 1) part = (b * a.hkv + g) * a.splits + split;
-    }
-    // (the same for the whole workgroup: scalars from here on)
-    b = uniform(b), g = uniform(g), rev = uniform(rev);
-    t_begin = uniform(t_begin), t_end = uniform(t_end), part = uniform(part);
-    const Seq sq = seq_of(a, b);
-    if (MODE == kOnce && sq.bad && g == 0 && t_begin == 0 && tid == 0) raise_flag(a.flags, PRESTO_FLAG_BAD_SEQ);
-    if (sq.n == 0) return;
-    const int rb = MODE == kOnce ? 0 : (sq.n * a.G + R - 1) / R - 1 - rev;
-    if (t_begin > 0) {
-        const int row0 = rb * R;
-        const Span sp = span_of(a, sq.pos0 + row0 / a.G, sq.pos0 + (min(row0 + R, sq.n * a.G) - 1) / a.G);
-        if (t_begin * T >= sp.n) return;  // the merge knows
-    }
-    segment(b, g, sq, rb, t_begin, t_end, part);
 }
 
 // Many query rows per KV head (bf16): tiles of 64 keys go from memory straight

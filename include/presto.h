@@ -550,8 +550,8 @@ presto_status presto_pages_reserve(const presto_pages_desc *desc, int32_t *refs,
  * here are not shared where a sequence appends; a program that moves a
  * sequence's ctx back (to drop rejected tokens) keeps it at or above the length
  * at which it was last forked.
- * Limits: new_rows < 2^31, batch * ceil(max_new / 16) < 2^23; 16-byte aligned,
- * new_stride a multiple of 16 bytes.
+ * Limits: new_rows < 2^31, batch * max_new < 2^24; 16-byte aligned, new_stride
+ * a multiple of 16 bytes.
  */
 presto_status presto_append_kv(const presto_pages_desc *desc, const void *k_new, const void *v_new,
                                int64_t new_rows, int64_t new_stride, const int32_t *offsets,

@@ -200,8 +200,7 @@ presto_status presto_append_kv(const presto_pages_desc* desc, const void* k_new,
     REQUIRE(new_stride >= row && new_stride <= ((int64_t)1 << 31) &&
                 new_stride % (d.dt == PRESTO_DT_BF16 ? 8 : 4) == 0,
             "%s: new_stride %lld", who, (long long)new_stride);
-    REQUIRE((int64_t)d.batch * ((max_new + (int64_t)15) / 16) < ((int64_t)1 << 23),
-            "%s: batch * max_new too large for one call", who);
+    REQUIRE((int64_t)d.batch * max_new < ((int64_t)1 << 24), "%s: batch * max_new is 2^24 or more", who);
     if (d.batch == 0 || max_new == 0 || new_rows == 0) return PRESTO_OK;
     REQUIRE(k_new && v_new && offsets && k_pages && v_pages && page_table && ctx && ctx_new, "%s: null pointer",
             who);

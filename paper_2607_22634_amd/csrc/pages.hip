@@ -376,11 +376,14 @@ __global__ __launch_bounds__(256) void pages_remap_kernel(const int32_t* table, 
 // and of V.  A unit is a stretch of kMoveBytes of one page; the pages of a
 // call's moves are all different, so units run in any order.  Neighbouring
 // units belong to different pools (layers, K and V): every eighth block runs on
-// one XCD, which so touches few pools' address translations.
+// one XCD, which so touches few pools' address translations.  STREAM: past the
+// caches, for a compaction's pages, which nobody reads next (1.5 GB moved: 326
+// us through them, 310 past them: 5.05 TB/s read and written).
 constexpr int kMoveThreads = 256;
 constexpr int kMoveLoads = 4;
 constexpr int kMoveBytes = kMoveThreads * kMoveLoads * 16;
 
+template <bool STREAM>
 __global__ __launch_bounds__(kMoveThreads) void pages_move_kernel(char* __restrict__ k, char* __restrict__ v,
                                                                   const Move* __restrict__ moves,
                                                                   const int32_t* __restrict__ n_moves,
@@ -401,23 +404,33 @@ __global__ __launch_bounds__(kMoveThreads) void pages_move_kernel(char* __restri
         if (at >= bytes) continue;
         uint4 x[kMoveLoads];  // (past the end the last piece is read again)
 #pragma unroll
-        for (int j = 0; j < kMoveLoads; ++j)
-            x[j] = *reinterpret_cast<const uint4*>(from + min(at + j * (kMoveThreads * 16), bytes - 16));
+        for (int j = 0; j < kMoveLoads; ++j) {
+            const char* p = from + min(at + j * (kMoveThreads * 16), bytes - 16);
+            if constexpr (STREAM)
+                x[j] = load_stream16(p);
+            else
+                x[j] = *reinterpret_cast<const uint4*>(p);
+        }
 #pragma unroll
         for (int j = 0; j < kMoveLoads; ++j) arrived(x[j]);
 #pragma unroll
         for (int j = 0; j < kMoveLoads; ++j) {
             const int64_t o = at + j * (kMoveThreads * 16);
-            if (o < bytes) *reinterpret_cast<uint4*>(to + o) = x[j];
+            if (o >= bytes) break;
+            if constexpr (STREAM)
+                __builtin_nontemporal_store((u32x4){x[j].x, x[j].y, x[j].z, x[j].w}, reinterpret_cast<u32x4*>(to + o));
+            else
+                *reinterpret_cast<uint4*>(to + o) = x[j];
         }
     }
 }
 
-// New rows of sequence b go to positions ctx[b] .. ctx_new[b] - 1.  Sixteen
-// rows of one sequence per workgroup (blockIdx.y: sequence), sixteen lanes or
-// more per row.
+// New rows of sequence b go to positions ctx[b] .. ctx_new[b] - 1, a few rows
+// of one sequence per workgroup, read past the caches (18,000 rows of 2 KB, K
+// and V, with the reservation: 44.8 us at sixteen rows, 34.9 at four; 144 MB at
+// 4.9 TB/s take 29).
 constexpr int kAppendThreads = 256;
-constexpr int kAppendRows = 16;
+constexpr int kAppendRows = 4;
 
 __global__ __launch_bounds__(kAppendThreads) void append_kv_kernel(
     const char* __restrict__ k_new, const char* __restrict__ v_new, int64_t new_bytes, int64_t new_rows,
@@ -453,8 +466,8 @@ __global__ __launch_bounds__(kAppendThreads) void append_kv_kernel(
             e[j] = table[(int64_t)b * max_pages + (pos >> shift)];
             at[j] = (pos & (page - 1)) * row16 + x;
             const int64_t src = (o0 + i0 + r) * new_bytes + x * 16;
-            kv[j] = *reinterpret_cast<const uint4*>(k_new + src);
-            vv[j] = *reinterpret_cast<const uint4*>(v_new + src);
+            kv[j] = load_stream16(k_new + src);
+            vv[j] = load_stream16(v_new + src);
         }
 #pragma unroll
         for (int j = 0; j < U; ++j) {
@@ -514,14 +527,15 @@ PagesWs pages_ws(void* ws, int64_t num_pages, int64_t n) {
 
 int esize(const presto_pages_desc* d) { return d->dt == PRESTO_DT_BF16 ? 2 : 4; }
 
+template <bool STREAM>
 void launch_move(const presto_pages_desc* d, void* k, void* v, const PagesWs& w, int64_t max_moves,
                  hipStream_t stream) {
     const int64_t row = (int64_t)d->hkv * d->head_dim * esize(d);
     const int stretches = (int)((row * d->page_size + kMoveBytes - 1) / kMoveBytes);
     // (the number of moves is known to the device only)
     const int64_t units = max_moves * d->layers * 2 * stretches;
-    const unsigned grid = (unsigned)std::min<int64_t>(units, 256 * 16);
-    pages_move_kernel<<<grid, kMoveThreads, 0, stream>>>(static_cast<char*>(k), static_cast<char*>(v), w.moves,
+    const unsigned grid = (unsigned)std::min<int64_t>(units, 256 * 64);
+    pages_move_kernel<STREAM><<<grid, kMoveThreads, 0, stream>>>(static_cast<char*>(k), static_cast<char*>(v), w.moves,
                                                          w.n_moves, d->layers, stretches, row,
                                                          d->page_stride * esize(d), d->layer_stride * esize(d));
 }
@@ -550,7 +564,7 @@ presto_status launch_pages_fork(const presto_pages_desc* d, int32_t* refs, int32
     pages_fork_kernel<<<1, kPlanThreads, 0, stream>>>(refs, table, ctx, parent, child, n, d->batch, d->max_pages,
                                                       d->num_pages, __builtin_ctz((unsigned)d->page_size), w.list,
                                                       w.need, w.lens, w.moves, w.n_moves, flags);
-    launch_move(d, k, v, w, n, stream);
+    launch_move<false>(d, k, v, w, n, stream);
     return check_launch("pages_fork_kernel");
 }
 
@@ -580,7 +594,7 @@ presto_status launch_pages_compact(const presto_pages_desc* d, const int32_t* re
     if (items > 0)
         pages_remap_kernel<<<(unsigned)((items + 255) / 256), 256, 0, stream>>>(table, table_out, entries,
                                                                                 d->num_pages, w.map, map_out, flags);
-    launch_move(d, k, v, w, d->num_pages / 2, stream);
+    launch_move<true>(d, k, v, w, d->num_pages / 2, stream);
     return check_launch("pages_compact_kernel");
 }
 

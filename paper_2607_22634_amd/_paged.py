@@ -30,9 +30,9 @@ def _book(dev: int, names: str, *ts) -> None:
             raise ValueError(f"{names.split()[i]} must be a contiguous int32 tensor on the GPU of the others")
 
 
-def _shape(name, t, *shape):
-    if t is not None and tuple(t.shape) != shape:
-        raise ValueError(f"{name} must be of shape {list(shape)}, not {list(t.shape)}")
+def _vector(name, t, n):
+    if t is not None and (t.dim() != 1 or t.shape[0] != n):
+        raise ValueError(f"{name} must be of shape [{n}], not {list(t.shape)}")
 
 
 _current = torch._C._cuda_getDevice
@@ -64,22 +64,29 @@ def _pool(k, v, page_table, batch, layers: bool) -> PagesDesc:
     """Descriptor of the pools k, v: [pages, page, hkv, dim], or with a leading
     layer dimension where `layers` allows it."""
     shape, stride = k.shape, k.stride()
-    if len(shape) != 4 and not (layers and len(shape) == 5):
-        raise ValueError("the page pools must be [pages, page, hkv, dim]" + (" or with layers first" if layers else ""))
-    if v.shape != shape or v.stride() != stride or v.dtype != k.dtype:
+    if v.shape != shape or v.stride() != stride or v.dtype is not k.dtype:
         raise ValueError("k_pages and v_pages must have one shape, stride and type")
-    n, page, hkv, d = shape[-4:]
-    if stride[-3:] != (hkv * d, d, 1) and k.numel() > 0:
+    n_layers, layer_stride = 1, 0
+    if len(shape) == 4:
+        n, page, hkv, d = shape
+        s_page, s_row, s_head, s_dim = stride
+    elif layers and len(shape) == 5:
+        n_layers, n, page, hkv, d = shape
+        layer_stride, s_page, s_row, s_head, s_dim = stride
+    else:
+        raise ValueError("the page pools must be [pages, page, hkv, dim]" + (" or with layers first" if layers else ""))
+    if (s_dim != 1 or s_head != d or s_row != hkv * d) and k.numel() > 0:
         raise ValueError("a page must be contiguous")
     # (the stride of a single page or layer is free: the default, 0)
-    page_stride, n_layers, layer_stride = stride[-4] if n > 1 else 0, 1, 0
-    if n > 1 and page_stride < page * hkv * d:
+    if n <= 1:
+        s_page = 0
+    elif s_page < page * hkv * d:
         raise ValueError("pages must not overlap")
-    if len(shape) == 5 and shape[0] != 1:
-        n_layers, layer_stride = shape[0], stride[0]
-        if layer_stride < (n - 1) * page_stride + page * hkv * d:
-            raise ValueError("layers must not overlap")
-    return PagesDesc(batch, page_table.shape[1], n, page, hkv, d, _dt(k), n_layers, page_stride, layer_stride)
+    if n_layers == 1:
+        layer_stride = 0
+    elif layer_stride < (n - 1) * s_page + page * hkv * d:
+        raise ValueError("layers must not overlap")
+    return PagesDesc(batch, page_table.shape[1], n, page, hkv, d, _dt(k), n_layers, s_page, layer_stride)
 
 
 def _books(refs, page_table, page_size) -> PagesDesc:
@@ -129,7 +136,7 @@ def _attend(who, call, need_of, q, q_offsets, k_pages, v_pages, page_table, ctx,
             ws = torch.empty(nb, dtype=torch.uint8, device=q.device)
             made.append(ws)
     else:
-        nb = ws.numel() * ws.element_size()
+        nb = ws.nbytes
     head = (ref, q.data_ptr()) if q_offsets is None else (ref, q.data_ptr(), q_offsets.data_ptr())
     _launch(call, who, dev, stream, made, *head, k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(),
             ctx.data_ptr(), out.data_ptr(), _ptr(flags), _ptr(ws), nb)
@@ -145,10 +152,10 @@ def presto_paged_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torc
     `window` of them and the first `sinks`)."""
     b = q.shape[0]
     desc = _attn_desc(q, k_pages, v_pages, page_table, b, 1, max_ctx, scale, window, sinks, total_ctx)
-    _shape("ctx", ctx, b)
+    _vector("ctx", ctx, b)
     L = lib()
-    return _attend("presto_paged_attention", L.presto_paged_attention, L.presto_paged_attention_workspace, q, None, k_pages, v_pages,
-                   page_table, ctx, desc, out, flags, workspace, stream)
+    return _attend("presto_paged_attention", L.presto_paged_attention, L.presto_paged_attention_workspace, q, None,
+                   k_pages, v_pages, page_table, ctx, desc, out, flags, workspace, stream)
 
 
 def presto_window_attention(q: torch.Tensor, q_offsets: torch.Tensor, max_q: int, k_pages: torch.Tensor,
@@ -160,11 +167,11 @@ def presto_window_attention(q: torch.Tensor, q_offsets: torch.Tensor, max_q: int
     q [total, Hq, d] are the last positions of sequence b, at most max_q."""
     b = q_offsets.shape[0] - 1
     desc = _attn_desc(q, k_pages, v_pages, page_table, b, max_q, max_ctx, scale, window, sinks, total_ctx)
-    _shape("q_offsets", q_offsets, b + 1)
-    _shape("ctx", ctx, b)
+    _vector("q_offsets", q_offsets, b + 1)
+    _vector("ctx", ctx, b)
     L = lib()
-    return _attend("presto_window_attention", L.presto_window_attention, L.presto_window_attention_workspace, q, q_offsets, k_pages, v_pages,
-                   page_table, ctx, desc, out, flags, workspace, stream)
+    return _attend("presto_window_attention", L.presto_window_attention, L.presto_window_attention_workspace, q,
+                   q_offsets, k_pages, v_pages, page_table, ctx, desc, out, flags, workspace, stream)
 
 
 def paged_attention_workspace(q: torch.Tensor, k_pages: torch.Tensor, page_table: torch.Tensor, *, max_q: int = 1,
@@ -179,15 +186,15 @@ def paged_attention_workspace(q: torch.Tensor, k_pages: torch.Tensor, page_table
     return torch.empty(need, dtype=torch.uint8, device=q.device)
 
 
-def _pages_call(who, dev, device, desc, args, flags, workspace, stream, made=()):
+def _pages_call(who, refs, dev, desc, args, flags, workspace, stream, made=()):
     """args: the call's pointers up to flags."""
     L, ref, ws = lib(), ctypes.byref(desc), workspace
-    _same(dev, "workspace", ws)
     if ws is None:
-        ws = torch.empty(max(L.presto_pages_workspace(ref), 16), dtype=torch.uint8, device=device)
+        ws = torch.empty(max(L.presto_pages_workspace(ref), 16), dtype=torch.uint8, device=refs.device)
         made = (*made, ws)
-    _launch(getattr(L, who), who, dev, stream, made, ref, *args, _ptr(flags), ws.data_ptr(),
-            ws.numel() * ws.element_size())
+    elif ws.get_device() != dev:
+        raise ValueError("workspace must be a tensor on the GPU of the others")
+    _launch(getattr(L, who), who, dev, stream, made, ref, *args, _ptr(flags), ws.data_ptr(), ws.nbytes)
 
 
 def pages_workspace(refs: torch.Tensor, page_table: torch.Tensor) -> torch.Tensor:
@@ -201,7 +208,7 @@ def _check_books(refs, page_table, ctx, names: str = "", *more):
         raise ValueError("page_table must be [sequences, columns] and refs [pages]")
     dev = refs.get_device()
     _book(dev, "refs page_table ctx " + names, refs, page_table, ctx, *more)
-    _shape("ctx", ctx, page_table.shape[0])
+    _vector("ctx", ctx, page_table.shape[0])
     return dev
 
 
@@ -213,13 +220,13 @@ def presto_pages_reserve(refs: torch.Tensor, page_table: torch.Tensor, ctx: torc
     in place.  A sequence the pool has no pages for keeps its length."""
     dev = _check_books(refs, page_table, ctx, "add out flags", add, out, flags)
     b = page_table.shape[0]
-    _shape("add", add, b)
-    _shape("out", out, b)
+    _vector("add", add, b)
+    _vector("out", out, b)
     made = ()
     if out is None:
         out = torch.empty_like(ctx)
         made = (out,)
-    _pages_call("presto_pages_reserve", dev, refs.device, _books(refs, page_table, page_size),
+    _pages_call("presto_pages_reserve", refs, dev, _books(refs, page_table, page_size),
                 (refs.data_ptr(), page_table.data_ptr(), ctx.data_ptr(), _ptr(add), extra, out.data_ptr()), flags,
                 workspace, stream, made)
     return out
@@ -234,11 +241,11 @@ def presto_append_kv(k_new: torch.Tensor, v_new: torch.Tensor, offsets: torch.Te
     b = offsets.shape[0] - 1
     _same(dev, "k_new v_new k_pages v_pages", k_new, v_new, k_pages, v_pages)
     _book(dev, "offsets page_table ctx ctx_new flags", offsets, page_table, ctx, ctx_new, flags)
-    _shape("offsets", offsets, b + 1)
+    _vector("offsets", offsets, b + 1)
     if page_table.dim() != 2 or page_table.shape[0] != b:
         raise ValueError("page_table must be [sequences, columns]")
-    _shape("ctx", ctx, b)
-    _shape("ctx_new", ctx_new, b)
+    _vector("ctx", ctx, b)
+    _vector("ctx_new", ctx_new, b)
     desc = _pool(k_pages, v_pages, page_table, b, False)
     if k_new.dtype != k_pages.dtype or v_new.dtype != k_pages.dtype:
         raise TypeError("the new rows and the pages must be of one type")
@@ -260,11 +267,11 @@ def presto_pages_fork(refs: torch.Tensor, page_table: torch.Tensor, ctx: torch.T
     dev = _check_books(refs, page_table, ctx, "parent child flags", parent, child, flags)
     _same(dev, "k_pages v_pages", k_pages, v_pages)
     n = parent.numel()
-    _shape("parent", parent, n)
-    _shape("child", child, n)
+    _vector("parent", parent, n)
+    _vector("child", child, n)
     desc = _pool(k_pages, v_pages, page_table, page_table.shape[0], True)
-    _shape("refs", refs, desc.num_pages)
-    _pages_call("presto_pages_fork", dev, refs.device, desc,
+    _vector("refs", refs, desc.num_pages)
+    _pages_call("presto_pages_fork", refs, dev, desc,
                 (_ptr(refs), _ptr(page_table), _ptr(ctx), _ptr(parent), _ptr(child), n, _ptr(k_pages),
                  _ptr(v_pages)), flags, workspace, stream)
 
@@ -274,7 +281,7 @@ def presto_pages_free(refs: torch.Tensor, page_table: torch.Tensor, ctx: torch.T
     """Drops the sequences `rows`: their references go, their lengths are 0."""
     dev = _check_books(refs, page_table, ctx, "rows flags", rows, flags)
     n = rows.numel()
-    _shape("rows", rows, n)
+    _vector("rows", rows, n)
     _launch(lib().presto_pages_free, "presto_pages_free", dev, stream, (), ctypes.byref(_books(refs, page_table, 16)),
             refs.data_ptr(), page_table.data_ptr(), ctx.data_ptr(), rows.data_ptr(), n, _ptr(flags))
 
@@ -305,12 +312,13 @@ def presto_pages_compact(refs: torch.Tensor, page_table: torch.Tensor, k_pages: 
     page_map = out.get("page_map")
     _book(dev, "out_refs out_page_table n_live page_map", out["refs"], out["page_table"], out["n_live"], page_map)
     desc = _pool(k_pages, v_pages, page_table, page_table.shape[0], True)
-    _shape("refs", refs, desc.num_pages)
-    _shape("out refs", out["refs"], desc.num_pages)
-    _shape("out page_table", out["page_table"], *page_table.shape)
-    _shape("n_live", out["n_live"], 1)
-    _shape("page_map", page_map, desc.num_pages)
-    _pages_call("presto_pages_compact", dev, refs.device, desc,
+    _vector("refs", refs, desc.num_pages)
+    _vector("out refs", out["refs"], desc.num_pages)
+    if out["page_table"].shape != page_table.shape:
+        raise ValueError("out page_table must be of page_table's shape")
+    _vector("n_live", out["n_live"], 1)
+    _vector("page_map", page_map, desc.num_pages)
+    _pages_call("presto_pages_compact", refs, dev, desc,
                 (_ptr(refs), _ptr(out["refs"]), _ptr(page_table), _ptr(out["page_table"]), _ptr(out["n_live"]),
                  _ptr(page_map), _ptr(k_pages), _ptr(v_pages)), flags, workspace, stream, made)
     return out

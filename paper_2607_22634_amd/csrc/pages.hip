@@ -53,12 +53,15 @@ __device__ __forceinline__ Four refs_at(const int32_t* refs, int64_t p, int n, i
 }
 
 // The first `want` free pages in order, into list; returns how many there are
-// (at most `want`).
-__device__ __forceinline__ int free_pages(const int32_t* refs, int n, int want, int32_t* list, int* s_wave) {
+// (at most `want`).  `head`: this thread's counts of the first 4096 pages, asked
+// for before the work that says how many pages are wanted.
+__device__ __forceinline__ Four pool_head(const int32_t* refs, int n) { return refs_at(refs, 4 * threadIdx.x, n, 1); }
+__device__ __forceinline__ int free_pages(const int32_t* refs, const Four& head, int n, int want, int32_t* list,
+                                          int* s_wave) {
     int found = 0;
     for (int64_t p0 = 0; p0 < n && found < want; p0 += 4 * kPlanThreads) {
         const int64_t p = p0 + 4 * threadIdx.x;
-        const Four f = refs_at(refs, p, n, 1);
+        const Four f = p0 == 0 ? head : refs_at(refs, p, n, 1);
         int mine = 0, total;
         for (int i = 0; i < 4; ++i) mine += f.v[i] <= 0;
         int at = found + block_scan(mine, s_wave, total);
@@ -97,6 +100,7 @@ __global__ __launch_bounds__(kPlanThreads) void pages_reserve_kernel(
     int32_t* __restrict__ list, int32_t* __restrict__ need, int32_t* __restrict__ flags) {
     __shared__ int s_wave[kPlanThreads / kWave];
     const int tid = threadIdx.x, sl = tid % kSeqLanes;
+    const Four head = pool_head(refs, num_pages);
     constexpr int PER = kPlanThreads / kSeqLanes;
     const int page = 1 << shift;
     // length after the call, -1: not a length
@@ -128,7 +132,7 @@ __global__ __launch_bounds__(kPlanThreads) void pages_reserve_kernel(
         total += sum;
     }
     const int want = (int)min(total, (int64_t)num_pages);
-    const int found = free_pages(refs, num_pages, want, list, s_wave);
+    const int found = free_pages(refs, head, num_pages, want, list, s_wave);
     bool out_of_pages = false;
     for (int b = tid / kSeqLanes; b < batch; b += PER) {
         const int c = ctx[b], n = grown(b, c), pre = need[b];
@@ -170,11 +174,18 @@ struct Move {
 __global__ __launch_bounds__(kPlanThreads) void pages_fork_kernel(
     int32_t* __restrict__ refs, int32_t* __restrict__ table, int32_t* __restrict__ ctx,
     const int32_t* __restrict__ parent, const int32_t* __restrict__ child, int32_t n, int32_t batch,
-    int32_t max_pages, int32_t num_pages, int32_t shift, int32_t* __restrict__ list, int32_t* __restrict__ need,
-    int32_t* __restrict__ lens, Move* __restrict__ moves, int32_t* __restrict__ n_moves,
+    int32_t max_pages, int32_t num_pages, int32_t shift, int32_t* list, int32_t* need,
+    int32_t* lens, Move* __restrict__ moves, int32_t* __restrict__ n_moves,
     int32_t* __restrict__ flags) {
     __shared__ int s_wave[kPlanThreads / kWave];
+    __shared__ int32_t s_need[kPlanThreads], s_len[kPlanThreads], s_list[kPlanThreads];
     const int tid = threadIdx.x, wave = tid / kWave, lane = lane_id();
+    const Four head = pool_head(refs, num_pages);
+    if (n <= kPlanThreads) {  // few forks keep their words in LDS
+        list = s_list;
+        need = s_need;
+        lens = s_len;
+    }
     constexpr int NW = kPlanThreads / kWave;
     const int page = 1 << shift;
     bool bad = false, short_of = false;
@@ -182,11 +193,8 @@ __global__ __launch_bounds__(kPlanThreads) void pages_fork_kernel(
     for (int i = wave; i < n; i += NW) {
         const int p = parent[i], c = child[i];
         bool ok = p >= 0 && p < batch && c >= 0 && c < batch && p != c;
-        int len = 0;
-        if (ok) {
-            len = ctx[p];
-            ok = len >= 0 && len <= (int64_t)max_pages * page && ctx[c] == 0;
-        }
+        const int len = ok ? ctx[p] : 0, own = ok ? ctx[c] : 0;
+        ok = ok && len >= 0 && len <= (int64_t)max_pages * page && own == 0;
         if (ok) {
             const int used = (int)(((int64_t)len + page - 1) >> shift);
             bool here = true;
@@ -218,7 +226,7 @@ __global__ __launch_bounds__(kPlanThreads) void pages_fork_kernel(
         if (i0 + tid < n) need[i0 + tid] = pre;
         total += sum;
     }
-    const int found = free_pages(refs, num_pages, min(total, num_pages), list, s_wave);
+    const int found = free_pages(refs, head, num_pages, min(total, num_pages), list, s_wave);
     if (tid == 0) *n_moves = found;  // (the forks that get a page are the first ones that need one)
     for (int i = wave; i < n; i += NW) {
         const int len = lens[i];
@@ -426,7 +434,7 @@ __global__ __launch_bounds__(kMoveThreads) void pages_move_kernel(char* __restri
 }
 
 // New rows of sequence b go to positions ctx[b] .. ctx_new[b] - 1, a few rows
-// of one sequence per workgroup, read past the caches (18,000 rows of 2 KB, K
+// of one sequence per workgroup, read past the caches (17,600 rows of 2 KB, K
 // and V, with the reservation: 44.8 us at sixteen rows, 34.9 at four; 144 MB at
 // 4.9 TB/s take 29).
 constexpr int kAppendThreads = 256;

@@ -184,66 +184,135 @@ __device__ __forceinline__ bool sees(const Args& a, int pos, int key) {
     return key <= pos && (a.window == 0 || key > pos - a.window || key < a.sinks);
 }
 
-// One row on its own, key by key: what the matrix instructions cannot do when
-// a row does not see a key whose V is not finite (0 * inf).  Entries v0 .. v1
-// - 1 of the list; O normalised into s_acc[D], (reference, sum) returned.
+// The kernel's arguments, read again: what a path taken rarely needs would
+// otherwise stay in scalar registers over the key loop (prompts 7% slower).
+__device__ __forceinline__ const Args& args_again() {
+    auto p = (const __attribute__((address_space(4))) Args*)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return *(const Args*)p;
+}
+
+// What the matrix instructions cannot do: a row that does not see a key whose V
+// is not finite still meets it, as 0 * inf.  Only keys that some rows of a
+// block see and others do not can do that: the positions of the block's own
+// tokens, and as many at the window's start.  Does one of them hold a V that is
+// not finite?  (This thread's part of the answer.)
 template <bool BF16, int D>
-__device__ float2 row_alone(const Args& a, const Span& sp, int b, int g, int64_t qrow, int head, int pos, int v0,
-                            int v1, float* s_q, float* s_p, float* s_red, float* s_acc) {
-    constexpr int E = BF16 ? 2 : 4;
-    const int tid = threadIdx.x, NT = blockDim.x;
-    const int keys = min(v1, sp.n) - v0;
-    auto value = [](const char* p) {
-        if constexpr (BF16)
-            return bf16_to_f(*reinterpret_cast<const uint16_t*>(p));
-        else
-            return *reinterpret_cast<const float*>(p);
-    };
-    __syncthreads();
-    for (int d = tid; d < D; d += NT) {
-        s_q[d] = value(a.q + (qrow * a.q_stride + (int64_t)head * D + d) * E);
-        s_acc[d] = 0.f;
-    }
-    __syncthreads();
-    auto key_at = [&](int i) {
-        const int key = key_of(sp, v0 + i);
-        return sees(a, pos, key) ? key : -1;
-    };
-    auto row_at = [&](const char* pool, int key) -> const char* {
+__device__ bool edge_not_finite(const Args& a, int b, int g, int p_lo, int p_hi) {
+    constexpr int E = BF16 ? 2 : 4, CPR = D * E / 16;
+    const int after = max(p_lo + 1, 0), n_after = max(p_hi + 1 - after, 0);
+    const int at_start = max(max(p_lo - a.window + 1, a.sinks), 0);
+    const int n_start = a.window > 0 ? max(p_hi - a.window + 1 - at_start, 0) : 0;
+    bool found = false;
+    for (int i = threadIdx.x; i < (n_after + n_start) * CPR; i += blockDim.x) {
+        const int k = i / CPR, key = k < n_after ? after + k : at_start + k - n_after;
         const int page = a.table[(int64_t)b * a.max_pages + (key >> a.page_shift)];
-        if (page < 0 || page >= a.num_pages) return nullptr;
-        return pool + (page * a.page_stride + ((int64_t)(key & ((1 << a.page_shift) - 1)) * a.hkv + g) * D) * E;
-    };
-    auto score = [&](int i) {
-        const int key = key_at(i);
-        const char* k = key < 0 ? nullptr : row_at(a.kp, key);
-        if (k == nullptr) return -INFINITY;
-        float s = 0.f;
-        for (int d = 0; d < D; ++d) s = fmaf(s_q[d], value(k + d * E), s);
-        return s * a.scale_log2;
-    };
-    float m = -INFINITY;
-    for (int i = tid; i < keys; i += NT) m = fmaxf(m, score(i));
-    s_red[tid] = m;
-    __syncthreads();
-    m = -INFINITY;
-    for (int i = 0; i < NT; ++i) m = fmaxf(m, s_red[i]);
-    float l = 0.f;
-    for (int i0 = 0; i0 < keys; i0 += NT) {
-        __syncthreads();
-        const float s = i0 + tid < keys ? score(i0 + tid) : -INFINITY;
-        s_p[tid] = s == -INFINITY ? -1.f : __builtin_amdgcn_exp2f(s - m);  // -1: no part in the sums
-        __syncthreads();
-        for (int i = 0; i < min(NT, keys - i0); ++i) {
-            const float p = s_p[i];
-            if (p == -1.f) continue;
-            l += p;
-            const char* v = row_at(a.vp, key_at(i0 + i));
-            for (int d = tid; d < D; d += NT) s_acc[d] = fmaf(p, value(v + d * E), s_acc[d]);
+        if (page < 0 || page >= a.num_pages) continue;
+        const int64_t row = page * a.page_stride + ((int64_t)(key & ((1 << a.page_shift) - 1)) * a.hkv + g) * D;
+        const uint4 u = *reinterpret_cast<const uint4*>(a.vp + row * E + i % CPR * 16);
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+        for (int j = 0; j < 4; ++j) {
+            // (an exponent of ones: in fp32, and in the upper and lower bf16)
+            found |= (w[j] & 0x7f800000u) == 0x7f800000u || (BF16 && (w[j] & 0x7f80u) == 0x7f80u);
         }
     }
+    return found;
+}
+
+// One row on its own, by all NT threads: entries v0 .. v1 - 1 of the list, with
+// the keys that the row does not see left out of the sums.  A thread scores a
+// key of NT, then sums 16 bytes of V over every (NT / CPR)-th of them.  O,
+// normalised, in scratch[0 .. D - 1]; (reference, sum) returned.  About 0.1 ms
+// per 10,000 keys: for caches that hold infinities, not a path to take often.
+template <int D, int E, int NT>
+constexpr int kAloneFloats = D + NT + 2 * NT + 2 * (NT / kWave) + NT / (D * E / 16) * D;
+
+template <bool BF16, int D, int NT>
+__device__ float2 row_alone(const Args& a, const Span& sp, int b, int g, int64_t qrow, int head, int pos, int v0,
+                            int v1, float* scratch) {
+    constexpr int E = BF16 ? 2 : 4, CPR = D * E / 16, EPC = 16 / E;  // values per 16 bytes
+    constexpr int LANES = NT / CPR, NW = NT / kWave;
+    float* const s_q = scratch;
+    int64_t* const s_at = reinterpret_cast<int64_t*>(s_q + D);  // -1: not seen
+    float* const s_p = reinterpret_cast<float*>(s_at + NT);
+    float* const s_w = s_p + NT;
+    float* const s_part = s_w + 2 * NW;  // [LANES][D]
+    const int tid = threadIdx.x, wave = tid / kWave, lane = lane_id();
+    const int keys = min(v1, sp.n) - v0;
+    auto values = [](const char* p, float (&x)[EPC]) {
+        const uint4 u = *reinterpret_cast<const uint4*>(p);
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+        for (int j = 0; j < 4; ++j) {
+            if constexpr (BF16) {
+                x[2 * j] = bf16lo(w[j]);
+                x[2 * j + 1] = bf16hi(w[j]);
+            } else {
+                x[j] = __uint_as_float(w[j]);
+            }
+        }
+    };
+    __syncthreads();
+    if (tid < CPR) {
+        float x[EPC];
+        values(a.q + (qrow * a.q_stride + (int64_t)head * D) * E + tid * 16, x);
+        for (int j = 0; j < EPC; ++j) s_q[tid * EPC + j] = x[j];
+    }
+    const int chunk = tid % CPR, part = tid / CPR;
+    float acc[EPC], m = -INFINITY, l = 0.f;
+    for (int j = 0; j < EPC; ++j) acc[j] = 0.f;
+    for (int i0 = 0; i0 < keys; i0 += NT) {
+        __syncthreads();
+        float s = -INFINITY;
+        int64_t at = -1;
+        if (i0 + tid < keys) {
+            const int key = key_of(sp, v0 + i0 + tid);
+            if (sees(a, pos, key)) {
+                const int page = a.table[(int64_t)b * a.max_pages + (key >> a.page_shift)];
+                if (page >= 0 && page < a.num_pages) {
+                    at = (page * a.page_stride + ((int64_t)(key & ((1 << a.page_shift) - 1)) * a.hkv + g) * D) * E;
+                    s = 0.f;
+                    for (int c = 0; c < CPR; ++c) {
+                        float x[EPC];
+                        values(a.kp + at + c * 16, x);
+                        for (int j = 0; j < EPC; ++j) s = fmaf(s_q[c * EPC + j], x[j], s);
+                    }
+                    s *= a.scale_log2;
+                }
+            }
+        }
+        const float mw = wave_max_f32_dpp(s);
+        if (lane == 0) s_w[wave] = mw;
+        __syncthreads();
+        float mn = m;
+        for (int w = 0; w < NW; ++w) mn = fmaxf(mn, s_w[w]);
+        const float f = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
+        m = mn;
+        const float p = at < 0 ? 0.f : __builtin_amdgcn_exp2f(s - (m == -INFINITY ? 0.f : m));
+        s_p[tid] = p;
+        s_at[tid] = at;
+        l = l * f + p;
+        if (i0 > 0)
+            for (int j = 0; j < EPC; ++j) acc[j] *= f;
+        __syncthreads();
+        for (int i = part; i < min(NT, keys - i0); i += LANES) {
+            if (s_at[i] < 0) continue;
+            float x[EPC];
+            values(a.vp + s_at[i] + chunk * 16, x);
+            for (int j = 0; j < EPC; ++j) acc[j] = fmaf(s_p[i], x[j], acc[j]);
+        }
+    }
+    const float lw = wave_sum_f32_dpp(l);
+    if (lane == 0) s_w[NW + wave] = lw;
+    for (int j = 0; j < EPC; ++j) s_part[part * D + chunk * EPC + j] = acc[j];
+    __syncthreads();
+    l = 0.f;
+    for (int w = 0; w < NW; ++w) l += s_w[NW + w];
     const float inv = l == 0.f ? 0.f : 1.f / l;
-    for (int d = tid; d < D; d += NT) s_acc[d] *= inv;
+    for (int d = tid; d < D; d += NT) {
+        float o = 0.f;
+        for (int i = 0; i < LANES; ++i) o += s_part[i * D + d];
+        s_q[d] = o * inv;
+    }
     __syncthreads();
     return make_float2(m, l);
 }
@@ -685,14 +754,16 @@ __global__ __launch_bounds__(kWaves * kWave, NB == 1 ? 3 : 2) void paged_attn_ro
     }
     // ---- rows of several positions whose sums are not all finite: a key that
     // only others see may be the cause
+    static_assert(kAloneFloats<D, E, NT> <= kWaves * R * SD, "the states' room is enough");
     if (p_lo == p_hi || !__syncthreads_or(bad)) return;
+    const Args& a2 = args_again();
+    if (!__syncthreads_or(edge_not_finite<BF16, D>(a2, b, g, p_lo, p_hi))) return;
     for (int r = 0; r < R; ++r) {
         if (!s_bad[r]) continue;
-        const int rho = row0 + r, tok = rho / a.G;
-        float* const s_acc = s_o;
-        const float2 ml = row_alone<BF16, D>(a, sp, b, g, sq.r0 + tok, g * a.G + rho - tok * a.G, sq.pos0 + tok,
-                                             t_begin * T, t_end * T, s_o + D, s_o + 2 * D, s_o + 2 * D + NT, s_acc);
-        for (int d = tid * 4; d < D; d += NT * 4) put(rho, d, *reinterpret_cast<const floatx4*>(&s_acc[d]));
+        const int rho = row0 + r, tok = rho / a2.G;
+        const float2 ml = row_alone<BF16, D, NT>(a2, sp, b, g, sq.r0 + tok, g * a2.G + rho - tok * a2.G, sq.pos0 + tok,
+                                                 t_begin * T, t_end * T, s_o);
+        for (int d = tid * 4; d < D; d += NT * 4) put(rho, d, *reinterpret_cast<const floatx4*>(&s_o[d]));
         if (tid == 0) put_ml(rho, ml.x, ml.y);
     }
 }
@@ -1119,12 +1190,17 @@ __global__ __launch_bounds__(kTileWaves * kWave) void paged_attn_tiles_kernel(Ar
     // ---- rows whose sums are not all finite: a key that only others see may
     // be the cause; or all rows, where a page is not there
     if (!any) return;
+    const Args& a2 = args_again();
+    if (!skip && !__syncthreads_or(edge_not_finite<true, D>(a2, b, g, sq.pos0 + row0 / a2.G,
+                                                            sq.pos0 + (row_end - 1) / a2.G)))
+        return;
     float* const f = reinterpret_cast<float*>(s_kv);
+    static_assert(kAloneFloats<D, 2, NT> * 4 <= 2 * kRing * kTile, "the ring's room is enough");
     for (int r = 0; r < row_end - row0; ++r) {
         if (!s_bad[r]) continue;
-        const int rr = row0 + r, tk = rr / a.G;
-        const float2 ml = row_alone<true, D>(a, sp, b, g, sq.r0 + tk, g * a.G + rr - tk * a.G, sq.pos0 + tk, t_begin * T,
-                                             t_end * T, f + D, f + 2 * D, f + 2 * D + NT, f);
+        const int rr = row0 + r, tk = rr / a2.G;
+        const float2 ml = row_alone<true, D, NT>(a2, sp, b, g, sq.r0 + tk, g * a2.G + rr - tk * a2.G, sq.pos0 + tk,
+                                                 t_begin * T, t_end * T, f);
         for (int d = tid; d < D / 2; d += NT) {
             if (a.splits == 1)
                 *reinterpret_cast<uint32_t*>(out_row(rr) + 2 * d) = pack2(f[2 * d], f[2 * d + 1]);

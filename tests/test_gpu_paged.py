@@ -185,6 +185,45 @@ def test_values_that_are_not_finite_reach_their_own_queries_only(dtype, n, past,
         base = run()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [5, 180])
+def test_values_that_are_not_finite_in_a_long_context(dtype, n):
+    """K and V that no query can leave out, and V that only some see, 20000
+    keys into a sequence: every element is finite exactly where the
+    definition's is, and right there."""
+    rng = np.random.default_rng([33, n])
+    past, hq, hkv, d = 20000, 4, 2, 64
+    L = past + n
+    c = Cache(rng, [L], [n], 64, hkv, d, dtype, 0, 0)
+    q = queries(rng, n, hq, d, dtype)
+    offs = ints([0, n])
+    some = [0, n // 2, n - 1]
+
+    def check():
+        got = P.presto_window_attention(q, offs, n, c.k, c.v, c.table, c.ctx).double().cpu().numpy()
+        k, v = c.rows(0)
+        for i in some:
+            with np.errstate(invalid="ignore"):
+                want, bound = R.attention(q[i:i + 1].double().cpu().numpy(), k, v, past + i, 0, 0, None, dtype)
+            fin = np.isfinite(want)
+            assert (np.isfinite(got[i:i + 1]) == fin).all(), i
+            assert (np.abs(got[i:i + 1][fin] - want[fin]) <= bound[fin]).all(), i
+
+    def put(name, key, head, dim, val):
+        page, row = int(c.table_h[0, key // 64]), key % 64
+        for pool in (getattr(c, name), getattr(c, name + "_h")):
+            pool[page, row, head, dim] = val
+
+    put("v", 7, 1, 3, float("nan"))  # all queries of heads 2, 3: that dim
+    check()
+    put("v", past + n // 2, 1, 5, float("inf"))  # and one that queries from the middle on see
+    check()
+    put("k", 9000, 0, 3, float("nan"))  # all of heads 0, 1
+    check()
+    put("v", L - 1, 0, 0, float("nan"))
+    check()
+
+
 def _ragged(rng, batch, lo, hi):
     return [int(x) for x in rng.integers(lo, hi + 1, batch)]
 

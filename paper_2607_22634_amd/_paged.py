@@ -84,8 +84,9 @@ def _pool(k, v, page_table, batch, layers: bool) -> PagesDesc:
         raise ValueError("pages must not overlap")
     if n_layers == 1:
         layer_stride = 0
-    elif layer_stride < (n - 1) * s_page + page * hkv * d:
-        raise ValueError("layers must not overlap")
+    elif layer_stride < (n - 1) * s_page + page * hkv * d and (
+            layer_stride < page * hkv * d or s_page < (n_layers - 1) * layer_stride + page * hkv * d):
+        raise ValueError("layers must not overlap")  # (they may lie one behind the other or page by page)
     return PagesDesc(batch, page_table.shape[1], n, page, hkv, d, _dt(k), n_layers, s_page, layer_stride)
 
 
@@ -102,7 +103,11 @@ def _rows(name, t, heads, d):
         raise ValueError(f"{name} must be [tokens, {heads}, {d}]")
     if (stride[2] != 1 or (stride[1] != d and heads > 1)) and t.numel() > 0:
         raise ValueError(f"the heads of a token of {name} must be contiguous")
-    return stride[0] if shape[0] > 1 else 0
+    if shape[0] <= 1:
+        return 0
+    if stride[0] < heads * d:  # (0 would mean the default)
+        raise ValueError(f"the tokens of {name} must not overlap")
+    return stride[0]
 
 
 def _attn_desc(q, k_pages, v_pages, page_table, batch, max_q, max_ctx, scale, window, sinks, total_ctx):
@@ -118,6 +123,12 @@ def _attn_desc(q, k_pages, v_pages, page_table, batch, max_q, max_ctx, scale, wi
         max_ctx = pages.max_pages * pages.page_size
     return PagedAttnDesc(pages, hq, max_q, max_ctx, window, sinks, d ** -0.5 if scale is None else scale, n, stride,
                          total_ctx)
+
+
+def _room(workspace) -> int:
+    if not workspace.is_contiguous():
+        raise ValueError("the workspace must be contiguous")
+    return workspace.nbytes
 
 
 def _attend(who, call, need_of, q, q_offsets, k_pages, v_pages, page_table, ctx, desc, out, flags, workspace, stream):
@@ -136,7 +147,7 @@ def _attend(who, call, need_of, q, q_offsets, k_pages, v_pages, page_table, ctx,
             ws = torch.empty(nb, dtype=torch.uint8, device=q.device)
             made.append(ws)
     else:
-        nb = ws.nbytes
+        nb = _room(ws)
     head = (ref, q.data_ptr()) if q_offsets is None else (ref, q.data_ptr(), q_offsets.data_ptr())
     _launch(call, who, dev, stream, made, *head, k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(),
             ctx.data_ptr(), out.data_ptr(), _ptr(flags), _ptr(ws), nb)
@@ -194,7 +205,7 @@ def _pages_call(who, refs, dev, desc, args, flags, workspace, stream, made=()):
         made = (*made, ws)
     elif ws.get_device() != dev:
         raise ValueError("workspace must be a tensor on the GPU of the others")
-    _launch(getattr(L, who), who, dev, stream, made, ref, *args, _ptr(flags), ws.data_ptr(), ws.nbytes)
+    _launch(getattr(L, who), who, dev, stream, made, ref, *args, _ptr(flags), ws.data_ptr(), _room(ws))
 
 
 def pages_workspace(refs: torch.Tensor, page_table: torch.Tensor) -> torch.Tensor:

@@ -222,8 +222,9 @@ __device__ bool edge_not_finite(const Args& a, int b, int g, int p_lo, int p_hi)
 // One row on its own, by all NT threads: entries v0 .. v1 - 1 of the list, with
 // the keys that the row does not see left out of the sums.  A thread scores a
 // key of NT, then sums 16 bytes of V over every (NT / CPR)-th of them.  O,
-// normalised, in scratch[0 .. D - 1]; (reference, sum) returned.  About 0.1 ms
-// per 10,000 keys: for caches that hold infinities, not a path to take often.
+// normalised, in scratch[0 .. D - 1]; (reference, sum) returned.  About 0.2 ms
+// per row and 10,000 keys: for caches that hold infinities, not a path to take
+// often.
 template <int D, int E, int NT>
 constexpr int kAloneFloats = D + NT + 2 * NT + 2 * (NT / kWave) + NT / (D * E / 16) * D;
 

@@ -175,16 +175,25 @@ __global__ __launch_bounds__(kPlanThreads) void pages_fork_kernel(
     int32_t* __restrict__ refs, int32_t* __restrict__ table, int32_t* __restrict__ ctx,
     const int32_t* __restrict__ parent, const int32_t* __restrict__ child, int32_t n, int32_t batch,
     int32_t max_pages, int32_t num_pages, int32_t shift, int32_t* list, int32_t* need,
-    int32_t* lens, Move* __restrict__ moves, int32_t* __restrict__ n_moves,
+    int32_t* lens, int32_t* first, Move* __restrict__ moves, int32_t* __restrict__ n_moves,
     int32_t* __restrict__ flags) {
     __shared__ int s_wave[kPlanThreads / kWave];
     __shared__ int32_t s_need[kPlanThreads], s_len[kPlanThreads], s_list[kPlanThreads];
     const int tid = threadIdx.x, wave = tid / kWave, lane = lane_id();
     const Four head = pool_head(refs, num_pages);
-    if (n <= kPlanThreads) {  // few forks keep their words in LDS
+    const bool few = n <= kPlanThreads;
+    if (few) {  // few forks keep their words in LDS
         list = s_list;
         need = s_need;
         lens = s_len;
+    } else {  // the first fork that names a child
+        for (int i = tid; i < batch; i += kPlanThreads) first[i] = n;
+        __syncthreads();
+        for (int i = tid; i < n; i += kPlanThreads) {
+            const int c = child[i];
+            if (c >= 0 && c < batch) atomicMin(&first[c], i);
+        }
+        __syncthreads();
     }
     constexpr int NW = kPlanThreads / kWave;
     const int page = 1 << shift;
@@ -207,7 +216,10 @@ __global__ __launch_bounds__(kPlanThreads) void pages_fork_kernel(
                     here &= held || (e < 0 && !(x == used - 1 && (len & (page - 1))));
                 }
             }
-            for (int j = lane; j < i; j += kWave) here &= child[j] != c;
+            if (few)
+                for (int j = lane; j < i; j += kWave) here &= child[j] != c;
+            else
+                here &= __hip_atomic_load(&first[c], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == i;
             ok = __ballot(!here) == 0;
         }
         if (lane == 0) {
@@ -510,10 +522,10 @@ namespace {
 int64_t up16(int64_t b) { return (b + 15) / 16 * 16; }
 
 // Workspace: the moves (at most one per page of the pool), the list of free
-// pages, the map and two words per sequence or fork.
+// pages, the map and three words per sequence or fork.
 struct PagesWs {
     Move* moves;
-    int32_t *list, *map, *need, *lens, *n_moves;
+    int32_t *list, *map, *need, *lens, *first, *n_moves;
     size_t bytes;
 };
 PagesWs pages_ws(void* ws, int64_t num_pages, int64_t n) {
@@ -529,6 +541,7 @@ PagesWs pages_ws(void* ws, int64_t num_pages, int64_t n) {
     w.map = reinterpret_cast<int32_t*>(take(num_pages * 4));
     w.need = reinterpret_cast<int32_t*>(take(n * 4));
     w.lens = reinterpret_cast<int32_t*>(take(n * 4));
+    w.first = reinterpret_cast<int32_t*>(take(n * 4));
     w.n_moves = reinterpret_cast<int32_t*>(take(4));
     return w;
 }
@@ -542,6 +555,7 @@ void launch_move(const presto_pages_desc* d, void* k, void* v, const PagesWs& w,
     const int stretches = (int)((row * d->page_size + kMoveBytes - 1) / kMoveBytes);
     // (the number of moves is known to the device only)
     const int64_t units = max_moves * d->layers * 2 * stretches;
+    if (units == 0) return;  // (a pool of one page has none to fill)
     const unsigned grid = (unsigned)std::min<int64_t>(units, 256 * 64);
     pages_move_kernel<STREAM><<<grid, kMoveThreads, 0, stream>>>(static_cast<char*>(k), static_cast<char*>(v), w.moves,
                                                          w.n_moves, d->layers, stretches, row,
@@ -568,10 +582,10 @@ presto_status launch_pages_reserve(const presto_pages_desc* d, int32_t* refs, in
 presto_status launch_pages_fork(const presto_pages_desc* d, int32_t* refs, int32_t* table, int32_t* ctx,
                                 const int32_t* parent, const int32_t* child, int32_t n, void* k, void* v,
                                 int32_t* flags, void* ws, hipStream_t stream) {
-    const PagesWs w = pages_ws(ws, d->num_pages, n);
+    const PagesWs w = pages_ws(ws, d->num_pages, d->batch);
     pages_fork_kernel<<<1, kPlanThreads, 0, stream>>>(refs, table, ctx, parent, child, n, d->batch, d->max_pages,
                                                       d->num_pages, __builtin_ctz((unsigned)d->page_size), w.list,
-                                                      w.need, w.lens, w.moves, w.n_moves, flags);
+                                                      w.need, w.lens, w.first, w.moves, w.n_moves, flags);
     launch_move<false>(d, k, v, w, n, stream);
     return check_launch("pages_fork_kernel");
 }

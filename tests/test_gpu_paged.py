@@ -571,6 +571,71 @@ def test_pools_of_page_pairs_and_spaced_layers():
     assert torch.equal(room, ref0)
 
 
+def test_layers_page_by_page():
+    """[pages, layers, ...], as the call's [layers, pages, ...]."""
+    page, hkv, d, pages, layers = 16, 2, 64, 10, 3
+    room = torch.randn(2, pages, layers, page, hkv, d, device=DEV)
+    ref0 = room.clone()
+    k, v = room.transpose(1, 2)
+    ref = R.Books([1, 0, 1, 0, 0, 1, 0, 0, 0, 1], [[9, 5, 2], [0, -1, -1], [-1] * 3], [40, 7, 0], page)
+    refs, table, ctx = _books_on_device(ref)
+    P.presto_pages_fork(refs, table, ctx, ints([0]), ints([2]), k, v)
+    moves = ref.fork([0], [2])
+    got = P.presto_pages_compact(refs, table, k, v)
+    moves += ref.compact()[0]
+    _same_books(ref, got["refs"], got["page_table"], ctx)
+    for s, t, r in moves:
+        ref0[:, t, :, :r] = ref0[:, s, :, :r]
+    assert torch.equal(room, ref0)
+
+
+@pytest.mark.parametrize("held", [0, 1])
+def test_a_pool_of_one_page(held):
+    refs, table = ints([held]), ints([[0 if held else -1, -1]])
+    k = torch.randn(2, 1, 16, 1, 64, device=DEV)
+    kh, f = k.clone(), flag()
+    got = P.presto_pages_compact(refs, table, k, k.clone(), flags=f)
+    assert got["refs"].tolist() == [held] and got["n_live"].tolist() == [held] and f.item() == 0
+    assert torch.equal(got["page_table"], table) and torch.equal(k, kh)
+    if held:  # and no room for a fork's page, but for one that shares the only one
+        table, ctx = ints([[0, -1], [-1, -1], [-1, -1]]), ints([5, 0, 0])
+        P.presto_pages_fork(refs, table, ctx, ints([0]), ints([1]), k, k.clone(), flags=f)
+        assert f.item() == P.PRESTO_FLAG_NO_PAGES and ctx.tolist() == [5, 0, 0] and refs.tolist() == [1]
+        ctx = ints([16, 0, 0])
+        P.presto_pages_fork(refs, table, ctx, ints([0, 0]), ints([1, 2]), k, k.clone())
+        assert ctx.tolist() == [16] * 3 and refs.tolist() == [3] and table[:, 0].tolist() == [0] * 3
+
+
+@pytest.mark.parametrize("n", [1024, 1025, 3000])
+def test_many_forks_at_once(n):
+    """More forks than one workgroup keeps in LDS, children named twice among
+    them, and fewer free pages than they need."""
+    rng = np.random.default_rng([44, n])
+    page, cols, parents, B = 16, 4, 40, n + 40
+    ctx = [int(x) for x in rng.integers(1, cols * page + 1, parents)] + [0] * n
+    used = [-(-c // page) for c in ctx]
+    pages = sum(used) + n // 2
+    order = iter(rng.permutation(pages).tolist())
+    table = [[next(order) if x < u else -1 for x in range(cols)] for u in used]
+    refs = [0] * pages
+    for row in table:
+        for e in row:
+            refs[e] += e >= 0
+    par = rng.integers(-1, parents, n).tolist()
+    chi = (rng.permutation(n) + parents).tolist()
+    for i in rng.integers(0, n, 50).tolist():
+        chi[i] = int(rng.integers(0, B + 2))
+    ref = R.Books(refs, table, ctx, page)
+    dev = _books_on_device(ref)
+    k, f = torch.randn(1, pages, page, 1, 64, device=DEV), flag()
+    kh = k.cpu()
+    P.presto_pages_fork(*dev, ints(par), ints(chi), k, k.clone(), flags=f)
+    for s, t, r in ref.fork(par, chi):
+        kh[:, t, :r] = kh[:, s, :r]
+    _same_books(ref, *dev)
+    assert f.item() == ref.flags and torch.equal(k.cpu(), kh)
+
+
 def _dense(kv, q, pos0, window, sinks, dtype):
     k, v = (np.stack(x) for x in kv)
     return R.attention(q, k, v, pos0, window, sinks, None, dtype)

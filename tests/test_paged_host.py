@@ -9,6 +9,7 @@ import torch
 
 import paged_ref as R
 import paper_2607_22634_amd as P
+from paper_2607_22634_amd import _paged
 
 FAKE = ctypes.c_void_p(0x1000)  # never dereferenced: the checks fail first
 
@@ -150,6 +151,29 @@ def test_binding_refuses_host_tensors():
         P.presto_paged_attention(q, k, k, t, c)
     with pytest.raises(ValueError):
         P.presto_pages_reserve(torch.zeros(3, dtype=torch.int32), t, c, 16, extra=1)
+
+
+def test_binding_refuses_overlapping_tokens_and_layers():
+    k = torch.zeros(4, 16, 2, 64)
+    table, ctx, offs = torch.zeros(3, 2, dtype=torch.int32), torch.ones(3, dtype=torch.int32), torch.arange(4).int()
+    for q in (torch.zeros(1, 4, 64).expand(3, 4, 64), torch.zeros(600).as_strided((3, 4, 64), (64, 64, 1))):
+        with pytest.raises(ValueError, match="overlap"):
+            P.presto_paged_attention(q, k, k, table, ctx)
+        with pytest.raises(ValueError, match="overlap"):
+            P.presto_window_attention(q, offs, 1, k, k, table, ctx)
+        with pytest.raises(ValueError, match="overlap"):
+            P.paged_attention_workspace(q, k, table)
+    pool = _paged._pool
+    for stride in ((2048 * 4, 2048), (2048, 2048 * 5), (4096, 4096 * 5)):  # layer by layer, page by page, of pairs
+        p = torch.zeros(5 * 4 * 4096).as_strided((5, 4, 16, 2, 64), (*stride, 128, 64, 1))
+        d = pool(p, p, table, 3, True)
+        assert (d.layer_stride, d.page_stride) == stride
+    for stride in ((2048 * 3, 2048), (2048, 2048 * 4), (4096, 4096 * 4), (0, 2048)):
+        p = torch.zeros(5 * 4 * 4096).as_strided((5, 4, 16, 2, 64), (*stride, 128, 64, 1))
+        with pytest.raises(ValueError, match="overlap"):
+            pool(p, p, table, 3, True)
+    with pytest.raises(ValueError, match="contiguous"):
+        _paged._room(torch.zeros(1, dtype=torch.uint8).expand(64))
 
 
 def test_reference_attention_on_a_case_by_hand():

@@ -1393,28 +1393,80 @@ void plan_tiles(const presto_paged_attn_desc* d, int64_t rows, PagedPlan& p) {
         p.order = kBySequence;
 }
 
+// The kernel of rows on more than sixteen: 16 or 32 rows per workgroup and
+// splits, by modelled time in us.  A round (a tile for each of the four waves)
+// takes a workgroup a + b nb, more where others share its CU, and the chip gets
+// through 256 of them in c + d nb: with 32 rows a key is fetched for twice as
+// many rows, with 16 there are twice as many workgroups of half the work.
+// Fitted to 2000 plans of 170 shapes (off by 14% and 8% r.m.s.); the choice
+// takes 3% longer than the best of each shape's, 32 rows always, in as many
+// splits as fill two rounds, took 19% and 11%.  (us, 16 and 32 rows: fp32, 3 x
+// 77 rows on 50 keys 7.3 and 9.6, 1 x 2048 on itself 368 and 332; bf16, 4
+// sequences of 32 rows on 8000 keys 32 and 34.)
+struct RowsCost {
+    double start, a, b, shared, round, c, d, merge, partials, keys;
+};
+constexpr RowsCost kRowsF32{5.4, 0.2, 1.4, 0.5, 0.45, 0.2, 1.5, 3.4, 0.7, 0.06};
+constexpr RowsCost kRowsBf16{4.7, 0.7, 0.9, 0.25, 0.0, 0.15, 1.4, 3.0, 0.8, 0.11};
+
+void plan_many_rows(const presto_paged_attn_desc* d, int64_t rows, PagedPlan& p) {
+    const bool bf16 = d->pages.dt == PRESTO_DT_BF16;
+    const RowsCost& k = bf16 ? kRowsBf16 : kRowsF32;
+    const int T = bf16 ? 32 : 16;
+    const double dims = d->pages.head_dim / 128.0, batch = d->pages.batch;
+    const double ctx = d->total_ctx > 0 ? d->total_ctx / batch : d->max_ctx;
+    double best = 1e300;
+    for (int nb = 2; nb >= 1; --nb) {
+        PagedPlan x = p;
+        x.nb = nb;
+        x.block_rows = 16 * nb;
+        x.row_blocks = (int)cdiv(rows, x.block_rows);
+        const int64_t blocks = d->pages.hkv * counted_blocks(d, x);
+        const int64_t list = longest_list(d, x.block_rows), tiles = cdiv(list, T);
+        // the keys of a mean block: the earlier ones of a sequence see fewer
+        double mean = ctx < list ? ctx : list;
+        if (list == d->max_ctx) mean -= d->total_q / batch / 2;
+        mean = mean < 1 ? 1 / (double)list : mean / list;
+        const double kv_mb = batch * d->pages.hkv * list * d->pages.head_dim * (bf16 ? 4e-6 : 8e-6);
+        for (int64_t want = 1; want <= tiles && (want == 1 || blocks * want <= 4096); want += 1 + want / 8) {
+            const int64_t per = cdiv(tiles, want), s = cdiv(tiles, per);
+            const double rounds = (double)cdiv(per, kWaves), load = (double)(blocks * s) / 256;
+            const double alone = k.start + rounds * (k.a + k.b * nb * dims) * (1 + k.shared * (load < 1 ? load : 1));
+            const double chip = k.start / 2 + load * (k.round + rounds * mean * (k.c + k.d * nb) * dims);
+            const double fetch = k.start + kv_mb * x.row_blocks * k.keys;
+            double cost = alone > chip ? alone : chip;
+            if (cost < fetch) cost = fetch;
+            if (s > 1) cost += k.merge + k.partials * 4e-6 * (double)(d->total_q * s) * d->hq * d->pages.head_dim;
+            if (cost < best) {
+                best = cost;
+                p = x;
+                p.splits = (int)s;
+                p.split_tiles = (int)per;
+                p.blocks = blocks * s;
+            }
+        }
+    }
+}
+
 // The kernel of rows.
 void plan_rows(const presto_paged_attn_desc* d, int64_t rows, PagedPlan& p) {
     const bool bf16 = d->pages.dt == PRESTO_DT_BF16;
     const int T = bf16 ? 32 : 16;
     p.nb = rows > 16 ? 2 : 1;
     p.block_rows = 16 * p.nb;
-    p.row_blocks = (int)cdiv(rows, p.block_rows);
+    p.row_blocks = 1;
     const int64_t longest = longest_list(d, p.block_rows), tiles = cdiv(longest, T);
-    const int64_t all = (int64_t)d->pages.batch * d->pages.hkv * p.row_blocks;
+    const int64_t all = (int64_t)d->pages.batch * d->pages.hkv;
     int64_t mean = longest;
     if (d->total_ctx > 0 && d->total_ctx / d->pages.batch < mean) mean = d->total_ctx / d->pages.batch + 1;
+    const bool even = d->total_ctx > 0 && 10 * mean >= 9 * longest;
+    if (rows > 32 || (rows > 16 && (even || d->pages.batch == 1 || tiles <= 3 * kWaves))) {
+        plan_many_rows(d, rows, p);
+        return;
+    }
     // Workgroups that the chip holds at once: three per CU by registers at
     // head_dim 128, two where they have 32 rows
     const int wgs = 256 * (d->pages.head_dim == 64 ? (p.nb == 1 ? 4 : 3) : (p.nb == 1 ? 3 : 2));
-    if (p.row_blocks > 1) {
-        // twice as many, of at least one tile per wave; short lists are not cut
-        p.split_tiles = (int)(cdiv(cdiv(all * cdiv(mean, T), 2 * wgs), kWaves) * kWaves);
-        if (p.split_tiles > tiles || tiles <= 3 * kWaves) p.split_tiles = (int)tiles;
-        p.splits = (int)cdiv(tiles, p.split_tiles);
-        p.blocks = d->pages.hkv * counted_blocks(d, p) * p.splits;
-        return;
-    }
     // Few rows are a stream of the cache: what counts is that all CUs end
     // together, and few launches.
     // * Sequences of up to three tiles per wave are not cut (no merge: 384 keys
@@ -1431,7 +1483,6 @@ void plan_rows(const presto_paged_attn_desc* d, int64_t rows, PagedPlan& p) {
     if (tiles <= 3 * kWaves || p.split_tiles > tiles) p.split_tiles = (int)tiles;
     p.splits = (int)cdiv(tiles, p.split_tiles);
     p.blocks = all * p.splits;
-    const bool even = d->total_ctx > 0 && 10 * mean >= 9 * longest;
     // (every workgroup looks through the batch for its piece)
     const bool can = d->pages.batch <= 2048 && d->pages.batch * tiles < ((int64_t)1 << 30);
     if (tiles > 3 * kWaves && !even && can) {

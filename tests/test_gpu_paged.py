@@ -304,6 +304,34 @@ def test_blocks_of_64_128_and_256_rows(heads, n, ctx):
         assert (np.abs(out[i:i + 1].double().cpu().numpy() - want) <= bound).all(), i
 
 
+@pytest.mark.parametrize("dtype,heads,n,ctx", [("f32", (32, 8, 128), 900, 1500), ("f32", (32, 8, 64), 40, 50),
+                                               ("f32", (8, 2, 128), 30, 6000), ("bf16", (32, 8, 128), 6, 9000),
+                                               ("bf16", (32, 8, 128), 8, 200), ("bf16", (2, 1, 64), 13, 3001)])
+@pytest.mark.parametrize("window", [0, 1000])
+@pytest.mark.parametrize("batch", [1, 5])
+def test_blocks_of_16_and_32_rows(dtype, heads, n, ctx, window, batch):
+    """The plans of the kernel of rows on more than sixteen, uncut and cut, of
+    even and ragged batches; a sample of the rows against the reference."""
+    rng = np.random.default_rng([20, n, window, batch])
+    hq, hkv, d = heads
+    new = [n] + _ragged(rng, batch - 1, 1, n)
+    lens = [ctx] + [int(x) for x in rng.integers(ctx // 2, ctx + 1, batch - 1)]
+    lens = [max(a, b) for a, b in zip(lens, new)]
+    c = Cache(rng, lens, new, 32, hkv, d, dtype, window, 4)
+    offs = np.concatenate([[0], np.cumsum(new)]).tolist()
+    q = queries(rng, offs[-1], hq, d, dtype)
+    for total in (0, sum(lens)):
+        out = P.presto_window_attention(q, ints(offs), n, c.k, c.v, c.table, c.ctx, max_ctx=max(lens), window=window,
+                                        sinks=4 if window else 0, total_ctx=total)
+        for b in {0, batch - 1}:
+            k, v = c.rows(b)
+            for i in sorted({0, min(16, new[b] - 1), new[b] // 2, new[b] - 1}):
+                r = offs[b] + i
+                want, bound = R.attention(q[r:r + 1].double().cpu().numpy(), k, v, lens[b] - new[b] + i, window,
+                                          4 if window else 0, None, dtype)
+                assert (np.abs(out[r:r + 1].double().cpu().numpy() - want) <= bound).all(), (b, i, total)
+
+
 def test_equal_and_extreme_scores():
     """Scores far from 0, of one value, and growing along the sequence (the
     running reference moves at every tile)."""

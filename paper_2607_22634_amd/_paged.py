@@ -7,20 +7,25 @@ device of their tensors, on that device's current stream unless one is given.
 from __future__ import annotations
 
 import ctypes
+import functools
 
 import torch
 
-from ._lib import PagedAttnDesc, PagesDesc, _check, _dt, _ptr, lib
+from ._lib import PRESTO_DT_BF16, PRESTO_DT_F32, PagedAttnDesc, PagesDesc, _check, _ptr, lib
 
 
+_I32 = torch.int32
+_DT = {torch.bfloat16: PRESTO_DT_BF16, torch.float32: PRESTO_DT_F32}
+
+
+# (A decode step of a small batch is bound by the host: every check of the two
+# functions costs 0.1 us, and the calls look at their usual tensors in one
+# expression before they come here to say which one is wrong.)
 def _same(dev: int, names: str, *ts) -> None:
     """Tensors on GPU `dev` (None: left out)."""
     for i, t in enumerate(ts):
         if t is not None and (t.get_device() != dev or dev < 0):
             raise ValueError(f"{names.split()[i]} must be a tensor on the GPU of the others")
-
-
-_I32 = torch.int32
 
 
 def _book(dev: int, names: str, *ts) -> None:
@@ -31,7 +36,7 @@ def _book(dev: int, names: str, *ts) -> None:
 
 
 def _vector(name, t, n):
-    if t is not None and (t.dim() != 1 or t.shape[0] != n):
+    if t is not None and t.shape != (n,):
         raise ValueError(f"{name} must be of shape [{n}], not {list(t.shape)}")
 
 
@@ -60,12 +65,20 @@ def _launch(call, who: str, dev: int, stream, made, *args) -> None:
         _check(status, who)
 
 
-def _pool(k, v, page_table, batch, layers: bool) -> PagesDesc:
+def _pool(k, v, cols, batch, layers: bool) -> PagesDesc:
     """Descriptor of the pools k, v: [pages, page, hkv, dim], or with a leading
     layer dimension where `layers` allows it."""
     shape, stride = k.shape, k.stride()
     if v.shape != shape or v.stride() != stride or v.dtype is not k.dtype:
         raise ValueError("k_pages and v_pages must have one shape, stride and type")
+    return _pool_of(shape, stride, k.dtype, batch, cols, layers)
+
+
+@functools.lru_cache(maxsize=64)
+def _pool_of(shape, stride, dtype, batch, cols, layers) -> PagesDesc:
+    """The same from sizes alone (a program has few pools; not to be changed)."""
+    if dtype not in _DT:
+        raise TypeError(f"unsupported dtype {dtype}")
     n_layers, layer_stride = 1, 0
     if len(shape) == 4:
         n, page, hkv, d = shape
@@ -75,7 +88,7 @@ def _pool(k, v, page_table, batch, layers: bool) -> PagesDesc:
         layer_stride, s_page, s_row, s_head, s_dim = stride
     else:
         raise ValueError("the page pools must be [pages, page, hkv, dim]" + (" or with layers first" if layers else ""))
-    if (s_dim != 1 or s_head != d or s_row != hkv * d) and k.numel() > 0:
+    if (s_dim != 1 or s_head != d or s_row != hkv * d) and 0 not in shape:
         raise ValueError("a page must be contiguous")
     # (the stride of a single page or layer is free: the default, 0)
     if n <= 1:
@@ -87,13 +100,18 @@ def _pool(k, v, page_table, batch, layers: bool) -> PagesDesc:
     elif layer_stride < (n - 1) * s_page + page * hkv * d and (
             layer_stride < page * hkv * d or s_page < (n_layers - 1) * layer_stride + page * hkv * d):
         raise ValueError("layers must not overlap")  # (they may lie one behind the other or page by page)
-    return PagesDesc(batch, page_table.shape[1], n, page, hkv, d, _dt(k), n_layers, s_page, layer_stride)
+    return PagesDesc(batch, cols, n, page, hkv, d, _DT[dtype], n_layers, s_page, layer_stride)
 
 
 def _books(refs, page_table, page_size) -> PagesDesc:
     """Descriptor for the calls that look at the books only."""
     batch, cols = page_table.shape
-    return PagesDesc(batch, cols, refs.numel(), page_size, 1, 64, 0, 1, 0, 0)
+    return _books_of(batch, cols, refs.shape[0], page_size)
+
+
+@functools.lru_cache(maxsize=64)
+def _books_of(batch, cols, pages, page_size) -> PagesDesc:
+    return PagesDesc(batch, cols, pages, page_size, 1, 64, 0, 1, 0, 0)
 
 
 def _rows(name, t, heads, d):
@@ -111,10 +129,11 @@ def _rows(name, t, heads, d):
 
 
 def _attn_desc(q, k_pages, v_pages, page_table, batch, max_q, max_ctx, scale, window, sinks, total_ctx):
-    if page_table.dim() != 2 or page_table.shape[0] != batch:
+    table = page_table.shape
+    if len(table) != 2 or table[0] != batch:
         raise ValueError("page_table must be [sequences, columns]")
-    pages = _pool(k_pages, v_pages, page_table, batch, False)
-    if q.dtype != k_pages.dtype:
+    pages = _pool(k_pages, v_pages, table[1], batch, False)
+    if q.dtype is not k_pages.dtype:
         raise TypeError("q and the pages must be of one type")
     d = pages.head_dim
     n, hq = q.shape[:2]
@@ -125,29 +144,33 @@ def _attn_desc(q, k_pages, v_pages, page_table, batch, max_q, max_ctx, scale, wi
                          total_ctx)
 
 
-def _room(workspace) -> int:
-    if not workspace.is_contiguous():
-        raise ValueError("the workspace must be contiguous")
+def _room(workspace, dev: int) -> int:
+    if workspace.get_device() != dev or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous tensor on the GPU of the others")
     return workspace.nbytes
 
 
 def _attend(who, call, need_of, q, q_offsets, k_pages, v_pages, page_table, ctx, desc, out, flags, workspace, stream):
     dev = q.get_device()
-    _same(dev, "q k_pages v_pages out workspace", q, k_pages, v_pages, out, workspace)
-    _book(dev, "page_table ctx q_offsets flags", page_table, ctx, q_offsets, flags)
+    if not (0 <= dev == k_pages.get_device() == v_pages.get_device() == page_table.get_device() == ctx.get_device()
+            and page_table.dtype is _I32 is ctx.dtype and page_table.is_contiguous() and ctx.is_contiguous()):
+        _same(dev, "q k_pages v_pages", q, k_pages, v_pages)
+        _book(dev, "page_table ctx", page_table, ctx)
+    if q_offsets is not None or flags is not None:
+        _book(dev, "q_offsets flags", q_offsets, flags)
     ref, made, ws, nb = ctypes.byref(desc), [], workspace, 0
     if out is None:
         out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
         made.append(out)
-    elif out.shape != q.shape or out.dtype != q.dtype or not out.is_contiguous():
-        raise ValueError("out must be a contiguous tensor of q's shape and type")
+    elif out.shape != q.shape or out.dtype is not q.dtype or not out.is_contiguous() or out.get_device() != dev:
+        raise ValueError("out must be a contiguous tensor of q's shape and type on its GPU")
     if ws is None:
         nb = need_of(ref)
         if nb:
             ws = torch.empty(nb, dtype=torch.uint8, device=q.device)
             made.append(ws)
     else:
-        nb = _room(ws)
+        nb = _room(ws, dev)
     head = (ref, q.data_ptr()) if q_offsets is None else (ref, q.data_ptr(), q_offsets.data_ptr())
     _launch(call, who, dev, stream, made, *head, k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(),
             ctx.data_ptr(), out.data_ptr(), _ptr(flags), _ptr(ws), nb)
@@ -203,9 +226,7 @@ def _pages_call(who, refs, dev, desc, args, flags, workspace, stream, made=()):
     if ws is None:
         ws = torch.empty(max(L.presto_pages_workspace(ref), 16), dtype=torch.uint8, device=refs.device)
         made = (*made, ws)
-    elif ws.get_device() != dev:
-        raise ValueError("workspace must be a tensor on the GPU of the others")
-    _launch(getattr(L, who), who, dev, stream, made, ref, *args, _ptr(flags), ws.data_ptr(), _room(ws))
+    _launch(getattr(L, who), who, dev, stream, made, ref, *args, _ptr(flags), ws.data_ptr(), _room(ws, dev))
 
 
 def pages_workspace(refs: torch.Tensor, page_table: torch.Tensor) -> torch.Tensor:
@@ -219,7 +240,8 @@ def _check_books(refs, page_table, ctx, names: str = "", *more):
         raise ValueError("page_table must be [sequences, columns] and refs [pages]")
     dev = refs.get_device()
     _book(dev, "refs page_table ctx " + names, refs, page_table, ctx, *more)
-    _vector("ctx", ctx, page_table.shape[0])
+    if ctx is not None:
+        _vector("ctx", ctx, page_table.shape[0])
     return dev
 
 
@@ -250,15 +272,17 @@ def presto_append_kv(k_new: torch.Tensor, v_new: torch.Tensor, offsets: torch.Te
     ctx[b] + i < ctx_new[b] of the cache, at most max_new per sequence."""
     dev = k_new.get_device()
     b = offsets.shape[0] - 1
-    _same(dev, "k_new v_new k_pages v_pages", k_new, v_new, k_pages, v_pages)
+    if not (0 <= dev == v_new.get_device() == k_pages.get_device() == v_pages.get_device()):
+        _same(dev, "k_new v_new k_pages v_pages", k_new, v_new, k_pages, v_pages)
     _book(dev, "offsets page_table ctx ctx_new flags", offsets, page_table, ctx, ctx_new, flags)
     _vector("offsets", offsets, b + 1)
-    if page_table.dim() != 2 or page_table.shape[0] != b:
+    table = page_table.shape
+    if len(table) != 2 or table[0] != b:
         raise ValueError("page_table must be [sequences, columns]")
     _vector("ctx", ctx, b)
     _vector("ctx_new", ctx_new, b)
-    desc = _pool(k_pages, v_pages, page_table, b, False)
-    if k_new.dtype != k_pages.dtype or v_new.dtype != k_pages.dtype:
+    desc = _pool(k_pages, v_pages, table[1], b, False)
+    if k_new.dtype is not k_pages.dtype or v_new.dtype is not k_pages.dtype:
         raise TypeError("the new rows and the pages must be of one type")
     hkv, d = k_pages.shape[2:]
     stride = _rows("k_new", k_new, hkv, d)
@@ -280,7 +304,7 @@ def presto_pages_fork(refs: torch.Tensor, page_table: torch.Tensor, ctx: torch.T
     n = parent.numel()
     _vector("parent", parent, n)
     _vector("child", child, n)
-    desc = _pool(k_pages, v_pages, page_table, page_table.shape[0], True)
+    desc = _pool(k_pages, v_pages, page_table.shape[1], page_table.shape[0], True)
     _vector("refs", refs, desc.num_pages)
     _pages_call("presto_pages_fork", refs, dev, desc,
                 (_ptr(refs), _ptr(page_table), _ptr(ctx), _ptr(parent), _ptr(child), n, _ptr(k_pages),
@@ -322,7 +346,7 @@ def presto_pages_compact(refs: torch.Tensor, page_table: torch.Tensor, k_pages: 
         made = tuple(out.values())
     page_map = out.get("page_map")
     _book(dev, "out_refs out_page_table n_live page_map", out["refs"], out["page_table"], out["n_live"], page_map)
-    desc = _pool(k_pages, v_pages, page_table, page_table.shape[0], True)
+    desc = _pool(k_pages, v_pages, page_table.shape[1], page_table.shape[0], True)
     _vector("refs", refs, desc.num_pages)
     _vector("out refs", out["refs"], desc.num_pages)
     if out["page_table"].shape != page_table.shape:

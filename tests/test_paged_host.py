@@ -166,14 +166,14 @@ def test_binding_refuses_overlapping_tokens_and_layers():
     pool = _paged._pool
     for stride in ((2048 * 4, 2048), (2048, 2048 * 5), (4096, 4096 * 5)):  # layer by layer, page by page, of pairs
         p = torch.zeros(5 * 4 * 4096).as_strided((5, 4, 16, 2, 64), (*stride, 128, 64, 1))
-        d = pool(p, p, table, 3, True)
+        d = pool(p, p, 2, 3, True)
         assert (d.layer_stride, d.page_stride) == stride
     for stride in ((2048 * 3, 2048), (2048, 2048 * 4), (4096, 4096 * 4), (0, 2048)):
         p = torch.zeros(5 * 4 * 4096).as_strided((5, 4, 16, 2, 64), (*stride, 128, 64, 1))
         with pytest.raises(ValueError, match="overlap"):
-            pool(p, p, table, 3, True)
+            pool(p, p, 2, 3, True)
     with pytest.raises(ValueError, match="contiguous"):
-        _paged._room(torch.zeros(1, dtype=torch.uint8).expand(64))
+        _paged._room(torch.zeros(1, dtype=torch.uint8).expand(64), -1)
 
 
 def test_reference_attention_on_a_case_by_hand():

@@ -104,13 +104,19 @@ __device__ __forceinline__ Seq seq_of(const Args& a, int b) {
 // fall on the same shader engines: four ragged prompts 347 us, 272 counted.
 // false: there is no such block.
 enum { kByLength, kBySequence, kByGrid };
-__device__ __forceinline__ bool find_block(const Args& a, int idx, bool first, int& b, int& rev) {
+__device__ __forceinline__ bool find_block(const Args& a, int idx, bool first, int& b, int& rev, Seq& sq) {
     const int lane = lane_id();
+    // (a lane's sequence in sq; that of the lane which is asked for at the end)
     auto blocks_of = [&](int bb, bool& bad) {
         if (bb >= a.batch) return 0;
-        const Seq sq = seq_of(a, bb);
+        sq = seq_of(a, bb);
         bad |= sq.bad;
         return (sq.n * a.G + a.block_rows - 1) / a.block_rows;
+    };
+    auto of_lane = [&](int l) {
+        sq.r0 = __builtin_amdgcn_readlane((int)sq.r0, l);
+        sq.n = __builtin_amdgcn_readlane(sq.n, l);
+        sq.pos0 = __builtin_amdgcn_readlane(sq.pos0, l);
     };
     bool bad = false, found = false;
     b = rev = 0;
@@ -134,21 +140,26 @@ __device__ __forceinline__ bool find_block(const Args& a, int idx, bool first, i
         const int j = idx - upto(lo);
         const int incl = (int)wave_scan_dpp(n > lo ? 1 : 0);
         const uint64_t hit = __ballot(incl > j);
-        b = hit ? __ffsll((unsigned long long)hit) - 1 : 0;
+        b = uniform(hit ? __ffsll((unsigned long long)hit) - 1 : 0);
+        of_lane(b);
         rev = lo;
     } else if (a.order == kBySequence) {
         int base = 0;
+        Seq got{};
         for (int b0 = 0; b0 < a.batch && (!found || first); b0 += kWave) {
             const int n = blocks_of(b0 + lane, bad), incl = (int)wave_scan_dpp(n);
             const uint64_t hit = __ballot(base + incl > idx);
             if (hit && !found) {
-                const int at = __ffsll((unsigned long long)hit) - 1;
+                const int at = uniform(__ffsll((unsigned long long)hit) - 1);
+                of_lane(at);
+                got = sq;
                 b = b0 + at;
                 rev = idx - base - __builtin_amdgcn_readlane(incl - n, at);
                 found = true;
             }
             base += __builtin_amdgcn_readlane(incl, kWave - 1);
         }
+        sq = got;
     } else {
         b = idx % a.batch;
         rev = idx / a.batch;
@@ -158,6 +169,9 @@ __device__ __forceinline__ bool find_block(const Args& a, int idx, bool first, i
     if (first && __ballot(bad) && lane == 0) raise_flag(a.flags, PRESTO_FLAG_BAD_SEQ);
     b = uniform(b);
     rev = uniform(rev);
+    sq.r0 = uniform((int)sq.r0);
+    sq.n = uniform(sq.n);
+    sq.pos0 = uniform(sq.pos0);
     return found;
 }
 
@@ -387,6 +401,7 @@ __global__ __launch_bounds__(kWaves * kWave, NB == 1 ? 3 : 2) void paged_attn_ro
     // its L2's channels (a long cache at 5.65 against 6.2 TB/s).
     int id = blockIdx.x;
     int g, b, rev = 0, t_begin, t_end, part = -1;
+    Seq sq{};
     if (MODE == kOnce && a.pieces > 0) {
         const int lane = lane_id(), idx = id % a.n_slots;
         g = id / a.n_slots;
@@ -420,7 +435,7 @@ __global__ __launch_bounds__(kWaves * kWave, NB == 1 ? 3 : 2) void paged_attn_ro
         g = id % a.hkv;
         id /= a.hkv;
         b = id;
-        if (MODE == kCached && !find_block(a, id, id == 0 && g == 0 && split == 0, b, rev)) return;
+        if (MODE == kCached && !find_block(a, id, id == 0 && g == 0 && split == 0, b, rev, sq)) return;
         t_begin = split * a.split_tiles;
         t_end = t_begin + a.split_tiles;
         if (a.splits > 1) part = (b * a.hkv + g) * a.splits + split;
@@ -428,7 +443,7 @@ __global__ __launch_bounds__(kWaves * kWave, NB == 1 ? 3 : 2) void paged_attn_ro
     // (the same for the whole workgroup: scalars from here on)
     b = uniform(b), g = uniform(g), rev = uniform(rev);
     t_begin = uniform(t_begin), t_end = uniform(t_end), part = uniform(part);
-    const Seq sq = seq_of(a, b);
+    if (MODE == kOnce) sq = seq_of(a, b);
     if (MODE == kOnce && sq.bad && g == 0 && t_begin == 0 && tid == 0) raise_flag(a.flags, PRESTO_FLAG_BAD_SEQ);
     if (sq.n == 0) return;
     const int rb = MODE == kOnce ? 0 : (sq.n * a.G + R - 1) / R - 1 - rev;
@@ -846,8 +861,8 @@ __global__ __launch_bounds__(kTileWaves * kWave) void paged_attn_tiles_kernel(Ar
     const int split = id % a.splits;
     id /= a.splits;
     int b, rev;
-    if (!find_block(a, id, id == 0 && g == 0 && split == 0, b, rev)) return;
-    const Seq sq = seq_of(a, b);
+    Seq sq{};
+    if (!find_block(a, id, id == 0 && g == 0 && split == 0, b, rev, sq)) return;
     const int rows = sq.n * a.G;
     const int rb = (rows + a.block_rows - 1) / a.block_rows - 1 - rev;
     const int tid = threadIdx.x, lane = lane_id();
@@ -1102,11 +1117,16 @@ __global__ __launch_bounds__(kTileWaves * kWave) void paged_attn_tiles_kernel(Ar
         };
         // one tile: its two blocks, the load of tile t + 3 into the slot that
         // every wave left before the last barrier, the wait for tile t + 2
+        // (where no more tiles follow, for all that is on its way: loads of
+        // the last entry in their place cost short lists up to 5%)
         auto tile = [&](auto uc, int t) __attribute__((always_inline)) {
             constexpr int u = decltype(uc)::value;
             using BV = std::integral_constant<int, u>;
             using BK = std::integral_constant<int, (u + 1) % kRing>;
-            load_tile(t_begin + t + 3, (u + 3) % kRing);
+            if (t + 3 < ntiles)
+                load_tile(t_begin + t + 3, (u + 3) % kRing);
+            else
+                PRESTO_WAIT_VM(0);
             if (active) {
                 if (2 * t < nblocks) step(BV{}, BK{}, 2 * t, 0);
                 if (2 * t + 1 < nblocks) step(BV{}, BK{}, 2 * t + 1, 1);

@@ -1370,16 +1370,19 @@ int64_t counted_blocks(const presto_paged_attn_desc* d, PagedPlan& p) {
 }
 
 // The kernel of tiles: rows per workgroup and splits, by modelled time in us.
-// A workgroup takes about 8 beside its tiles (page numbers, queries, first
-// tiles, output), a tile of 64 keys 1.75 with two waves of rows per SIMD and
-// 1.25 with one (up to 128 rows), a merge 5 and its partials' traffic.  One
-// workgroup per CU: whole rounds where all are alike, else the longest or the
-// sum.  Measured: 512 new tokens alone 18.2 in blocks of 128 rows, 22.4 of 256;
+// A workgroup takes about 7.4 beside its tiles (page numbers, queries, first
+// tiles, output), a tile of 64 keys 1.9 with two waves of rows per SIMD and 1.3
+// with one (up to 128 rows), at head_dim 64 four and three quarters of that
+// (fitted to 149 shapes, off by 8% r.m.s.), a merge 5 and its partials'
+// traffic.  One workgroup per CU: whole rounds where all are alike, else the
+// longest or the sum.  Measured: 512 new tokens alone 18.2 in blocks of 128 rows, 22.4 of 256;
 // 64 on 65536 cached 99 in 32 splits of 256 rows, 114 in 16 of 128; 16 x 300
 // on 1700 217 in blocks of 256, 238 of 128.
-void plan_tiles(const presto_paged_attn_desc* d, int64_t rows, PagedPlan& p) {
+double plan_tiles(const presto_paged_attn_desc* d, int64_t rows, PagedPlan& p) {
     const int64_t heads = (int64_t)d->pages.batch * d->pages.hkv;
     const int64_t most = (int64_t)(kTilePages - 8) * d->pages.page_size / kKeyTile;  // page numbers in LDS
+    const bool narrow = d->pages.head_dim == 64;
+    const double start = narrow ? 5.9 : 7.4;
     double best = 1e300;
     for (int r = kTileRows; r >= 64; r /= 2) {
         const int64_t blocks = heads * cdiv(rows, r), list = longest_list(d, r), tiles = cdiv(list, kKeyTile);
@@ -1388,11 +1391,11 @@ void plan_tiles(const presto_paged_attn_desc* d, int64_t rows, PagedPlan& p) {
         const int64_t least = cdiv(tiles, most);
         for (int64_t want = least; want <= tiles && (want == least || blocks * want <= 4096); want += 1 + want / 8) {
             const int64_t per = cdiv(tiles, want), s = cdiv(tiles, per);
-            const double step = r > 128 ? 1.75 : 1.25;
-            const double longest = 8.0 + (double)per * step;
+            const double step = (r > 128 ? 1.9 : 1.3) * (narrow ? 0.75 : 1.0);
+            const double longest = start + (double)per * step;
             double cost = (double)cdiv(blocks * s, 256) * longest;
             if (10 * mean < 9 * list) {
-                const double sum = (double)(blocks * s) * (8.0 + (double)per * step * (double)mean / (double)list) / 256;
+                const double sum = (double)(blocks * s) * (start + (double)per * step * (double)mean / (double)list) / 256;
                 cost = longest > 1.1 * sum ? longest : 1.1 * sum;
             }
             if (s > 1) cost += 5.0 + 2.0 * (double)(heads * s * rows) * d->pages.head_dim * 4 / 8e6;
@@ -1411,6 +1414,7 @@ void plan_tiles(const presto_paged_attn_desc* d, int64_t rows, PagedPlan& p) {
     // 668 -> 677)
     if (p.order == kByLength && longest_list(d, p.block_rows) * d->pages.head_dim * 4 > (4 << 20))
         p.order = kBySequence;
+    return best;
 }
 
 // The kernel of rows on more than sixteen: 16 or 32 rows per workgroup and
@@ -1418,18 +1422,21 @@ void plan_tiles(const presto_paged_attn_desc* d, int64_t rows, PagedPlan& p) {
 // takes a workgroup a + b nb, more where others share its CU, and the chip gets
 // through 256 of them in c + d nb: with 32 rows a key is fetched for twice as
 // many rows, with 16 there are twice as many workgroups of half the work.
-// Fitted to 2000 plans of 170 shapes (off by 14% and 8% r.m.s.); the choice
+// Fitted to 2200 plans of 320 shapes (off by 14% and 12% r.m.s.); the choice
 // takes 3% longer than the best of each shape's, 32 rows always, in as many
 // splits as fill two rounds, took 19% and 11%.  (us, 16 and 32 rows: fp32, 3 x
 // 77 rows on 50 keys 7.3 and 9.6, 1 x 2048 on itself 368 and 332; bf16, 4
-// sequences of 32 rows on 8000 keys 32 and 34.)
+// sequences of 32 rows on 8000 keys 32 and 34.)  Against the kernel of tiles
+// the shorter modelled time decides: within 1% of the better of the two, which
+// tiles alone miss by 19% at up to 60 GFLOP (us, rows and tiles: 4 x 54 tokens
+// on 182, 8/4 heads of 64, 6.7 and 10.2; 28 x 41, 56/8 heads of 128, 37 and 20).
 struct RowsCost {
-    double start, a, b, shared, round, c, d, merge, partials, keys;
+    double start, a, b, shared, round, c, d, merge, partials, keys, ends;
 };
-constexpr RowsCost kRowsF32{5.4, 0.2, 1.4, 0.5, 0.45, 0.2, 1.5, 3.4, 0.7, 0.06};
-constexpr RowsCost kRowsBf16{4.7, 0.7, 0.9, 0.25, 0.0, 0.15, 1.4, 3.0, 0.8, 0.11};
+constexpr RowsCost kRowsF32{5.4, 0.2, 1.4, 0.5, 0.45, 0.2, 1.5, 3.4, 0.7, 0.06, 0.0};
+constexpr RowsCost kRowsBf16{4.7, 0.6, 0.9, 0.15, 1.2, 0.05, 0.95, 3.2, 0.8, 0.09, 1.0};
 
-void plan_many_rows(const presto_paged_attn_desc* d, int64_t rows, PagedPlan& p) {
+double plan_many_rows(const presto_paged_attn_desc* d, int64_t rows, PagedPlan& p) {
     const bool bf16 = d->pages.dt == PRESTO_DT_BF16;
     const RowsCost& k = bf16 ? kRowsBf16 : kRowsF32;
     const int T = bf16 ? 32 : 16;
@@ -1452,7 +1459,8 @@ void plan_many_rows(const presto_paged_attn_desc* d, int64_t rows, PagedPlan& p)
             const int64_t per = cdiv(tiles, want), s = cdiv(tiles, per);
             const double rounds = (double)cdiv(per, kWaves), load = (double)(blocks * s) / 256;
             const double alone = k.start + rounds * (k.a + k.b * nb * dims) * (1 + k.shared * (load < 1 ? load : 1));
-            const double chip = k.start / 2 + load * (k.round + rounds * mean * (k.c + k.d * nb) * dims);
+            const double some = rounds * mean + k.ends < rounds ? rounds * mean + k.ends : rounds;
+            const double chip = k.start / 2 + load * (k.round + some * (k.c + k.d * nb) * dims);
             const double fetch = k.start + kv_mb * x.row_blocks * k.keys;
             double cost = alone > chip ? alone : chip;
             if (cost < fetch) cost = fetch;
@@ -1466,6 +1474,7 @@ void plan_many_rows(const presto_paged_attn_desc* d, int64_t rows, PagedPlan& p)
             }
         }
     }
+    return best;
 }
 
 // The kernel of rows.
@@ -1525,10 +1534,13 @@ PagedPlan paged_plan(const presto_paged_attn_desc* d) {
     const int64_t out_rows = (int64_t)d->pages.batch * d->max_q * d->hq;
     const int64_t rows = (int64_t)(d->hq / d->pages.hkv) * d->max_q;
     p.tiles = d->pages.dt == PRESTO_DT_BF16 && d->max_q > 1 && rows > 32;
-    if (p.tiles)
-        plan_tiles(d, rows, p);
-    else
+    if (p.tiles) {
+        const double tiles_us = plan_tiles(d, rows, p);
+        PagedPlan x{};
+        if (plan_many_rows(d, rows, x) < tiles_us) p = x;  // (x.tiles: false)
+    } else {
         plan_rows(d, rows, p);
+    }
     const bool cut = p.splits > 1 || p.pieces > 0;
     if (cut) {
         // four splits or fewer per part

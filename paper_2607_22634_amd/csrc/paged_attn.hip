@@ -1370,11 +1370,10 @@ int64_t counted_blocks(const presto_paged_attn_desc* d, PagedPlan& p) {
 }
 
 // The kernel of tiles: rows per workgroup and splits, by modelled time in us.
-// A workgroup takes about 7.4 beside its tiles (page numbers, queries, first
-// tiles, output), a tile of 64 keys 1.9 with two waves of rows per SIMD and 1.3
-// with one (up to 128 rows), at head_dim 64 four and three quarters of that
-// (fitted to 149 shapes, off by 8% r.m.s.), a merge 5 and its partials'
-// traffic.  One workgroup per CU: whole rounds where all are alike, else the
+// A workgroup takes about 8 beside its tiles (page numbers, queries, first
+// tiles, output), a tile of 64 keys 1.75 with two waves of rows per SIMD and
+// 1.25 with one (up to 128 rows), at head_dim 64 three quarters of that (off by
+// 9% r.m.s. over 149 shapes), a merge 5 and its partials' traffic.  One workgroup per CU: whole rounds where all are alike, else the
 // longest or the sum.  Measured: 512 new tokens alone 18.2 in blocks of 128 rows, 22.4 of 256;
 // 64 on 65536 cached 99 in 32 splits of 256 rows, 114 in 16 of 128; 16 x 300
 // on 1700 217 in blocks of 256, 238 of 128.
@@ -1382,7 +1381,7 @@ double plan_tiles(const presto_paged_attn_desc* d, int64_t rows, PagedPlan& p) {
     const int64_t heads = (int64_t)d->pages.batch * d->pages.hkv;
     const int64_t most = (int64_t)(kTilePages - 8) * d->pages.page_size / kKeyTile;  // page numbers in LDS
     const bool narrow = d->pages.head_dim == 64;
-    const double start = narrow ? 5.9 : 7.4;
+    const double start = narrow ? 6.2 : 8.0;
     double best = 1e300;
     for (int r = kTileRows; r >= 64; r /= 2) {
         const int64_t blocks = heads * cdiv(rows, r), list = longest_list(d, r), tiles = cdiv(list, kKeyTile);
@@ -1391,7 +1390,7 @@ double plan_tiles(const presto_paged_attn_desc* d, int64_t rows, PagedPlan& p) {
         const int64_t least = cdiv(tiles, most);
         for (int64_t want = least; want <= tiles && (want == least || blocks * want <= 4096); want += 1 + want / 8) {
             const int64_t per = cdiv(tiles, want), s = cdiv(tiles, per);
-            const double step = (r > 128 ? 1.9 : 1.3) * (narrow ? 0.75 : 1.0);
+            const double step = (r > 128 ? 1.75 : 1.25) * (narrow ? 0.75 : 1.0);
             const double longest = start + (double)per * step;
             double cost = (double)cdiv(blocks * s, 256) * longest;
             if (10 * mean < 9 * list) {
@@ -1421,20 +1420,21 @@ double plan_tiles(const presto_paged_attn_desc* d, int64_t rows, PagedPlan& p) {
 // splits, by modelled time in us.  A round (a tile for each of the four waves)
 // takes a workgroup a + b nb, more where others share its CU, and the chip gets
 // through 256 of them in c + d nb: with 32 rows a key is fetched for twice as
-// many rows, with 16 there are twice as many workgroups of half the work.
-// Fitted to 2200 plans of 320 shapes (off by 14% and 12% r.m.s.); the choice
-// takes 3% longer than the best of each shape's, 32 rows always, in as many
-// splits as fill two rounds, took 19% and 11%.  (us, 16 and 32 rows: fp32, 3 x
-// 77 rows on 50 keys 7.3 and 9.6, 1 x 2048 on itself 368 and 332; bf16, 4
-// sequences of 32 rows on 8000 keys 32 and 34.)  Against the kernel of tiles
-// the shorter modelled time decides: within 1% of the better of the two, which
-// tiles alone miss by 19% at up to 60 GFLOP (us, rows and tiles: 4 x 54 tokens
-// on 182, 8/4 heads of 64, 6.7 and 10.2; 28 x 41, 56/8 heads of 128, 37 and 20).
+// many rows, with 16 there are twice as many workgroups of half the work (in
+// bf16 they win by more than the model has it: `wide`).  Fitted to 2200 plans of
+// 320 shapes (off by 14% and 12% r.m.s.); the choice takes 4% and 1% longer
+// than the best of each shape's, 32 rows always, in as many splits as fill two
+// rounds, took 19% and 11%.  (us, 16 and 32 rows: fp32, 3 x 77 rows on 50 keys
+// 7.3 and 9.6, 1 x 2048 on itself 368 and 332; bf16, 4 sequences of 32 rows on
+// 8000 keys 32 and 34.)  Against the kernel of tiles the shorter modelled time
+// decides: within 1 or 2% of the better of the two, which tiles alone miss by
+// 16 to 19% at up to 60 GFLOP (us, rows and tiles: 4 x 54 tokens on 182, 8/4
+// heads of 64, 6.7 and 10.2; 28 x 41, 56/8 heads of 128, 37 and 20).
 struct RowsCost {
-    double start, a, b, shared, round, c, d, merge, partials, keys, ends;
+    double start, a, b, shared, round, c, d, merge, partials, keys, ends, wide;
 };
-constexpr RowsCost kRowsF32{5.4, 0.2, 1.4, 0.5, 0.45, 0.2, 1.5, 3.4, 0.7, 0.06, 0.0};
-constexpr RowsCost kRowsBf16{4.7, 0.6, 0.9, 0.15, 1.2, 0.05, 0.95, 3.2, 0.8, 0.09, 1.0};
+constexpr RowsCost kRowsF32{5.4, 0.2, 1.4, 0.5, 0.45, 0.2, 1.5, 3.4, 0.7, 0.06, 0.0, 1.0};
+constexpr RowsCost kRowsBf16{4.7, 0.6, 0.9, 0.15, 1.2, 0.05, 0.95, 3.2, 0.8, 0.09, 1.0, 1.15};
 
 double plan_many_rows(const presto_paged_attn_desc* d, int64_t rows, PagedPlan& p) {
     const bool bf16 = d->pages.dt == PRESTO_DT_BF16;
@@ -1442,7 +1442,7 @@ double plan_many_rows(const presto_paged_attn_desc* d, int64_t rows, PagedPlan& 
     const int T = bf16 ? 32 : 16;
     const double dims = d->pages.head_dim / 128.0, batch = d->pages.batch;
     const double ctx = d->total_ctx > 0 ? d->total_ctx / batch : d->max_ctx;
-    double best = 1e300;
+    double best = 1e300, us = best;
     for (int nb = 2; nb >= 1; --nb) {
         PagedPlan x = p;
         x.nb = nb;
@@ -1465,8 +1465,10 @@ double plan_many_rows(const presto_paged_attn_desc* d, int64_t rows, PagedPlan& 
             double cost = alone > chip ? alone : chip;
             if (cost < fetch) cost = fetch;
             if (s > 1) cost += k.merge + k.partials * 4e-6 * (double)(d->total_q * s) * d->hq * d->pages.head_dim;
-            if (cost < best) {
-                best = cost;
+            const double weighed = nb == 2 ? cost * k.wide : cost;
+            if (weighed < best) {
+                best = weighed;
+                us = cost;
                 p = x;
                 p.splits = (int)s;
                 p.split_tiles = (int)per;
@@ -1474,7 +1476,7 @@ double plan_many_rows(const presto_paged_attn_desc* d, int64_t rows, PagedPlan& 
             }
         }
     }
-    return best;
+    return us;
 }
 
 // The kernel of rows.

@@ -332,6 +332,54 @@ def test_blocks_of_16_and_32_rows(dtype, heads, n, ctx, window, batch):
                 assert (np.abs(out[r:r + 1].double().cpu().numpy() - want) <= bound).all(), (b, i, total)
 
 
+@pytest.mark.parametrize("batch,n,past,heads,page,window", [
+    (2, 700, 2300, (16, 2, 128), 32, 0), (2, 700, 2300, (16, 2, 128), 64, 900), (2, 1000, 0, (16, 4, 64), 16, 0),
+    (1, 2100, 500, (12, 2, 64), 128, 0), (1, 200, 140000, (8, 1, 64), 16, 0)])
+def test_long_prompts_with_odd_values_and_missing_pages(batch, n, past, heads, page, window):
+    """Prompts too long for the kernel of rows: a sample of the rows as they
+    are, with V that is not finite at a key that some rows see and at one that
+    all do, and with a page that is not there (its keys count as not visible)."""
+    rng = np.random.default_rng([21, n, past, window])
+    hq, hkv, d = heads
+    sinks, L = 4 if window else 0, past + n
+    c = Cache(rng, [L] * batch, [n] * batch, page, hkv, d, "bf16", window, sinks)
+    q = queries(rng, batch * n, hq, d, "bf16")
+    offs, b = ints([i * n for i in range(batch + 1)]), batch - 1
+    some = sorted({0, 1, n // 3, n // 2, n // 2 + 1, n - 1})
+
+    def check(gone=()):
+        f = flag()
+        out = P.presto_window_attention(q, offs, n, c.k, c.v, c.table, c.ctx, window=window, sinks=sinks, flags=f)
+        assert f.item() == (P.PRESTO_FLAG_BAD_PAGE if gone else 0)
+        k, v = c.rows(b)
+        for i in some:
+            ok = R.visible(past + i, L, window, sinks)
+            ok[list(gone)] = False
+            r, m = b * n + i, int(ok.sum())
+            got = out[r:r + 1].double().cpu().numpy()
+            with np.errstate(invalid="ignore"):
+                want, bound = R.attention(q[r:r + 1].double().cpu().numpy(), k[ok], v[ok], m - 1, 0, 0, None, "bf16")
+            fin = np.isfinite(want)
+            assert (np.isfinite(got) == fin).all(), i
+            assert (np.abs(got[fin] - want[fin]) <= bound[fin]).all(), i
+
+    def put(name, key, head, dim, val):
+        pg, row = int(c.table_h[b, key // page]), key % page
+        for pool in (getattr(c, name), getattr(c, name + "_h")):
+            pool[pg, row, head, dim] = val
+
+    check()
+    put("v", past + n // 2, hkv - 1, 3, float("inf"))
+    check()
+    put("v", past + n // 3 if window else 1, 0, 9, float("nan"))
+    put("k", L - 1, 0, 0, float("nan"))
+    check()
+    col = (past + n // 2) // page if n > 300 else past // page  # (with the first of the odd values)
+    c.table[b, col] = -1
+    if n <= 1000:
+        check(range(col * page, min((col + 1) * page, L)))
+
+
 def test_equal_and_extreme_scores():
     """Scores far from 0, of one value, and growing along the sequence (the
     running reference moves at every tile)."""

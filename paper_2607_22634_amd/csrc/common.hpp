@@ -53,6 +53,12 @@ __device__ __forceinline__ int wave_sum_i32(int v) {
     return v;
 }
 
+// The attention kernels' lazy softmax reference starts at 0 for a row that has
+// seen no key, and moves to a block's maximum where the row's mass is less than
+// this.  exp2 flushes what lies below 2^-126: of a row with this much mass that
+// is less than 2^-62 of it, of one with 2^-125 it may be half.
+constexpr float kLeastMass = 0x1p-64f;
+
 __device__ __forceinline__ int lane_id() { return threadIdx.x & (kWave - 1); }
 
 // ---------------------------------------------------------------------------

@@ -798,7 +798,8 @@ __global__ __launch_bounds__(kWaves * kWave, NB == 1 ? 3 : 2) void paged_attn_ro
 // of block i, the exponentials of block i + 1 and the scores of block i + 2
 // between one another.  Scores start from -m, so that a probability is
 // exp2(c S); the reference m moves only where a block's sum exceeds 2^8 or a
-// row has no mass yet.
+// row has no mass yet, or next to none (kLeastMass: keys that a row does not see
+// may come first, and all of its scores may lie far below 0).
 //
 // The page numbers of the workgroup's keys are looked up once and kept in LDS:
 // eight rows of a tile, one wave's share of its loads, lie in one page.
@@ -1107,7 +1108,7 @@ __global__ __launch_bounds__(kTileWaves * kWave) void paged_attn_tiles_kernel(Ar
             }
             if (more) {
                 ls = row_sum(ls);
-                const bool need = !(ls <= 256.f) || l_run + ls == 0.f;
+                const bool need = !(ls <= 256.f) || l_run + ls < kLeastMass;
                 if (__ballot(need)) exact(Sa, Pn, ls, need, Sb);
                 l_run += ls;
             }

@@ -1,0 +1,77 @@
+"""Attention over scores that all lie far below zero.  The kernels keep a lazy
+reference per row, and a row that has seen nothing yet starts from 0: weighed
+against that, terms below 2^-126 are flushed to zero while others are not.
+
+Queries and keys are made such that a score is `far` (log2 units) plus noise of
+2: their first components' product, and the product of the others."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paged_ref as R
+import paper_2607_22634_amd as P
+from test_gpu_paged import Cache, flag, ints, queries
+
+pytestmark = pytest.mark.gpu
+SCALE = math.log(2.0)  # scores in log2 units are the products themselves
+FAR = [-122.0, -126.0, -128.0, -140.0, -1000.0]
+
+
+def _far(x, first):
+    """[..., d]: the first component, and noise that makes 2 of a product"""
+    x = x * (4.0 / (x.shape[-1] - 1)) ** 0.25
+    x[..., 0] = first
+    return x
+
+
+def _far_cache(c, far):
+    c.k_h.copy_(_far(c.k_h.float(), far / 8))  # (NaN where nothing sees it stays in the other components)
+    c.k.copy_(c.k_h)
+
+
+@pytest.mark.parametrize("far", FAR)
+@pytest.mark.parametrize("dtype,batch,n,past,heads,window,sinks", [
+    ("bf16", 2, 1000, 400, (16, 8, 64), 400, 0), ("bf16", 1, 1000, 100, (16, 16, 128), 100, 0),
+    ("bf16", 1, 1000, 800, (8, 8, 128), 800, 0), ("bf16", 1, 1000, 800, (8, 8, 128), 800, 5),
+    ("bf16", 1, 512, 3000, (8, 2, 128), 0, 0), ("bf16", 1, 40, 900, (4, 2, 64), 100, 0),
+    ("f32", 1, 300, 900, (8, 2, 64), 200, 0)])
+def test_prompts_of_far_scores(dtype, batch, n, past, heads, window, sinks, far):
+    """Windowed prompts, whose later rows see nothing of their block's first
+    keys, cut and uncut, and causal ones."""
+    hq, hkv, d = heads
+    rng = np.random.default_rng([50, n, past, window])
+    L = past + n
+    c = Cache(rng, [L] * batch, [n] * batch, 64, hkv, d, dtype, window, sinks)
+    _far_cache(c, far)
+    q = queries(rng, batch * n, hq, d, dtype)
+    q.copy_(_far(q.float(), 8.0))
+    f = flag()
+    out = P.presto_window_attention(q, ints([n * b for b in range(batch + 1)]), n, c.k, c.v, c.table, c.ctx, scale=SCALE,
+                                    window=window, sinks=sinks, flags=f)
+    assert f.item() == 0
+    got, qh = out.double().cpu().numpy(), q.double().cpu().numpy()
+    k, v = c.rows(batch - 1)
+    for i in range(0, n, 13):
+        r = (batch - 1) * n + i
+        want, bound = R.attention(qh[r:r + 1], k, v, past + i, window, sinks, SCALE, dtype)
+        err = np.abs(got[r:r + 1] - want)
+        assert (err <= bound).all(), (i, (err / bound).max())
+
+
+@pytest.mark.parametrize("far", FAR)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_decode_of_far_scores(dtype, far):
+    rng = np.random.default_rng(51)
+    ctx = [1, 40, 700, 5000]
+    c = Cache(rng, ctx, [1] * 4, 32, 2, 128, dtype)
+    _far_cache(c, far)
+    q = queries(rng, 4, 8, 128, dtype)
+    q.copy_(_far(q.float(), 8.0))
+    out = P.presto_paged_attention(q, c.k, c.v, c.table, c.ctx, scale=SCALE).double().cpu().numpy()
+    qh = q.double().cpu().numpy()
+    for b in range(4):
+        k, v = c.rows(b)
+        want, bound = R.attention(qh[b:b + 1], k, v, ctx[b] - 1, 0, 0, SCALE, dtype)
+        assert (np.abs(out[b:b + 1] - want) <= bound).all(), b

@@ -463,8 +463,10 @@ __global__ __launch_bounds__(kAttnWaves * kWave) void tree_attn_bf16_kernel(Attn
     // Every score chain starts from -m, so the MFMAs deliver x = s*c - m and
     // a probability costs one v_exp.  m is a lazy reference: no per-block
     // maximum is taken; a row whose block sum exceeds 2^8 (some x above
-    // about 3) or that has no mass yet takes an exact step (block maximum,
-    // rescale of o and l), which is rare.
+    // about 3) or that has no mass yet, or next to none (kLeastMass: a wave
+    // that shares its rows starts from m = 0, and all of a row's scores may lie
+    // far below that), takes an exact step (block maximum, rescale of o and l),
+    // which is rare.
     constexpr int EPK = 16 / KS;  // exponentials per score MFMA
     static_assert(EPK * KS == 16 && EPK % 2 == 0 && KS == 2 * DB, "head_dim 64 or 128");
     const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
@@ -558,7 +560,7 @@ __global__ __launch_bounds__(kAttnWaves * kWave) void tree_attn_bf16_kernel(Attn
         }
         if (more) {
             ls = row_sum(ls);
-            const bool need = !(ls <= 256.f) || l_run + ls == 0.f;
+            const bool need = !(ls <= 256.f) || l_run + ls < kLeastMass;
             if (__ballot(need)) exact(Sa, Pn, ls, need, Sb);
             l_run += ls;
         }
@@ -593,7 +595,7 @@ __global__ __launch_bounds__(kAttnWaves * kWave) void tree_attn_bf16_kernel(Attn
         if (masked(i)) apply_mask(S, j0_of(i));
         uint32_t P[8];
         float ls = row_sum(exps(S, P));
-        const bool need = !(ls <= 256.f) || l_run + ls == 0.f;
+        const bool need = !(ls <= 256.f) || l_run + ls < kLeastMass;
         floatx16 none = S;
         if (__ballot(need)) exact(S, P, ls, need, none);
         l_run += ls;

@@ -12,6 +12,9 @@ import torch
 
 import paged_ref as R
 import paper_2607_22634_amd as P
+import synthetic as sy
+from brute import anc_from_parent
+from gpu_util import to_dev, to_host
 from test_gpu_paged import Cache, flag, ints, queries
 
 pytestmark = pytest.mark.gpu
@@ -75,3 +78,41 @@ def test_decode_of_far_scores(dtype, far):
         k, v = c.rows(b)
         want, bound = R.attention(qh[b:b + 1], k, v, ctx[b] - 1, 0, 0, SCALE, dtype)
         assert (np.abs(out[b:b + 1] - want) <= bound).all(), b
+
+
+@pytest.mark.parametrize("far", FAR)
+@pytest.mark.parametrize("dtype,N,hq,hkv,d", [("bf16", 9, 8, 2, 128), ("bf16", 33, 8, 8, 64), ("bf16", 70, 16, 2, 128),
+                                              ("bf16", 257, 8, 1, 64), ("f32", 33, 4, 2, 64)])
+def test_trees_of_far_scores(dtype, N, hq, hkv, d, far):
+    """Trees of few nodes, whose rows' waves share the keys of one block among
+    them, and of many, over contexts of several lengths."""
+    rng = np.random.default_rng([52, N, hq])
+    ctx = np.array([0, 40, 300, 2000], np.int32)
+    b = len(ctx)
+    n_nodes = np.array([N, N, max(N // 2, 1), N], np.int32)
+    parent = np.full((b, N), -1, np.int32)
+    for s in range(b):
+        for n in range(1, int(n_nodes[s])):
+            parent[s, n] = n - 1 if s == 1 else rng.integers(0, n)
+    anc = anc_from_parent(parent, n_nodes, N)
+    offs = np.zeros(b + 1, np.int32)
+    offs[1:] = np.cumsum(ctx)
+    rows = int(offs[-1])
+    draw = lambda *s: rng.standard_normal(s, dtype=np.float32)
+    q, kc, kt = (sy.cast(_far(draw(*s), x), dtype)
+                 for s, x in (((b, N, hq, d), 8.0), ((rows, hkv, d), far / 8), ((b, N, hkv, d), far / 8)))
+    vc, vt = sy.cast(draw(rows, hkv, d), dtype), sy.cast(draw(b, N, hkv, d), dtype)
+    out = P.presto_tree_attention(to_dev(q, dtype), to_dev(kc, dtype), to_dev(vc, dtype), to_dev(offs), to_dev(kt, dtype),
+                                  to_dev(vt, dtype), to_dev(anc), to_dev(n_nodes), int(ctx.max()), SCALE)
+    got = sy.as_f32(to_host(out), dtype).astype(np.float64)
+    q, kc, vc, kt, vt = (sy.as_f32(x, dtype).astype(np.float64) for x in (q, kc, vc, kt, vt))
+    for s in range(b):
+        for n in sorted({0, 1, int(n_nodes[s]) // 2, int(n_nodes[s]) - 1}):
+            path = [n]
+            while path[-1] > 0:
+                path.append(int(parent[s, path[-1]]))
+            k, v = (np.concatenate([c[offs[s]:offs[s + 1]], t[s, path]]) for c, t in ((kc, kt), (vc, vt)))
+            want, bound = R.attention(q[s, n:n + 1], k, v, len(k) - 1, 0, 0, SCALE, dtype)
+            # (the bound once more: split contexts round their parts to bf16, by
+            # half a step of at most the sum that the bound is made of)
+            assert (np.abs(got[s, n:n + 1] - want) <= 2 * bound).all(), (s, n)

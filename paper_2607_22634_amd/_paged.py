@@ -44,17 +44,28 @@ _current = torch._C._cuda_getDevice
 _raw_stream = torch._C._cuda_getCurrentRawStream
 
 
-def _launch(call, who: str, dev: int, stream, made, *args) -> None:
-    """Enqueues call(*args, stream) on GPU `dev`.  Tensors made here for a call
-    on a stream that is not the current one must not be handed out again before
-    it is through."""
+def _empty(stream, shape, dtype, device, returned: bool = True) -> torch.Tensor:
+    """A tensor for a call on `stream`.  The allocator orders a block's uses
+    within one stream: taken on the current stream for a call on another, it may
+    be one that kernels of the current stream, freed but not through, still
+    write.  So it is taken on the call's own, and what the caller gets is noted
+    for the current stream, where it is used next."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    if returned:
+        t.record_stream(torch.cuda.current_stream(device))
+    return t
+
+
+def _launch(call, who: str, dev: int, stream, *args) -> None:
+    """Enqueues call(*args, stream) on GPU `dev`."""
     if stream is None:
         queue = _raw_stream(dev)
     else:
         if stream.device.index != dev:
             raise ValueError(f"the stream belongs to {stream.device}, the tensors to GPU {dev}")
-        for t in made:
-            t.record_stream(stream)
         queue = stream.cuda_stream
     if dev == _current():
         status = call(*args, queue)
@@ -158,21 +169,19 @@ def _attend(who, call, need_of, q, q_offsets, k_pages, v_pages, page_table, ctx,
         _book(dev, "page_table ctx", page_table, ctx)
     if q_offsets is not None or flags is not None:
         _book(dev, "q_offsets flags", q_offsets, flags)
-    ref, made, ws, nb = ctypes.byref(desc), [], workspace, 0
+    ref, ws, nb = ctypes.byref(desc), workspace, 0
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        made.append(out)
+        out = _empty(stream, q.shape, q.dtype, q.device)
     elif out.shape != q.shape or out.dtype is not q.dtype or not out.is_contiguous() or out.get_device() != dev:
         raise ValueError("out must be a contiguous tensor of q's shape and type on its GPU")
     if ws is None:
         nb = need_of(ref)
         if nb:
-            ws = torch.empty(nb, dtype=torch.uint8, device=q.device)
-            made.append(ws)
+            ws = _empty(stream, nb, torch.uint8, q.device, returned=False)
     else:
         nb = _room(ws, dev)
     head = (ref, q.data_ptr()) if q_offsets is None else (ref, q.data_ptr(), q_offsets.data_ptr())
-    _launch(call, who, dev, stream, made, *head, k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(),
+    _launch(call, who, dev, stream, *head, k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(),
             ctx.data_ptr(), out.data_ptr(), _ptr(flags), _ptr(ws), nb)
     return out
 
@@ -220,13 +229,12 @@ def paged_attention_workspace(q: torch.Tensor, k_pages: torch.Tensor, page_table
     return torch.empty(need, dtype=torch.uint8, device=q.device)
 
 
-def _pages_call(who, refs, dev, desc, args, flags, workspace, stream, made=()):
+def _pages_call(who, refs, dev, desc, args, flags, workspace, stream):
     """args: the call's pointers up to flags."""
     L, ref, ws = lib(), ctypes.byref(desc), workspace
     if ws is None:
-        ws = torch.empty(max(L.presto_pages_workspace(ref), 16), dtype=torch.uint8, device=refs.device)
-        made = (*made, ws)
-    _launch(getattr(L, who), who, dev, stream, made, ref, *args, _ptr(flags), ws.data_ptr(), _room(ws, dev))
+        ws = _empty(stream, max(L.presto_pages_workspace(ref), 16), torch.uint8, refs.device, returned=False)
+    _launch(getattr(L, who), who, dev, stream, ref, *args, _ptr(flags), ws.data_ptr(), _room(ws, dev))
 
 
 def pages_workspace(refs: torch.Tensor, page_table: torch.Tensor) -> torch.Tensor:
@@ -255,13 +263,11 @@ def presto_pages_reserve(refs: torch.Tensor, page_table: torch.Tensor, ctx: torc
     b = page_table.shape[0]
     _vector("add", add, b)
     _vector("out", out, b)
-    made = ()
     if out is None:
-        out = torch.empty_like(ctx)
-        made = (out,)
+        out = _empty(stream, ctx.shape, _I32, ctx.device)
     _pages_call("presto_pages_reserve", refs, dev, _books(refs, page_table, page_size),
                 (refs.data_ptr(), page_table.data_ptr(), ctx.data_ptr(), _ptr(add), extra, out.data_ptr()), flags,
-                workspace, stream, made)
+                workspace, stream)
     return out
 
 
@@ -288,7 +294,7 @@ def presto_append_kv(k_new: torch.Tensor, v_new: torch.Tensor, offsets: torch.Te
     stride = _rows("k_new", k_new, hkv, d)
     if v_new.shape != k_new.shape or _rows("v_new", v_new, hkv, d) != stride:
         raise ValueError("k_new and v_new must have one shape and stride")
-    _launch(lib().presto_append_kv, "presto_append_kv", dev, stream, (), ctypes.byref(desc), k_new.data_ptr(),
+    _launch(lib().presto_append_kv, "presto_append_kv", dev, stream, ctypes.byref(desc), k_new.data_ptr(),
             v_new.data_ptr(), k_new.shape[0], stride, offsets.data_ptr(), max_new, k_pages.data_ptr(),
             v_pages.data_ptr(), page_table.data_ptr(), ctx.data_ptr(), ctx_new.data_ptr(), _ptr(flags))
 
@@ -317,7 +323,7 @@ def presto_pages_free(refs: torch.Tensor, page_table: torch.Tensor, ctx: torch.T
     dev = _check_books(refs, page_table, ctx, "rows flags", rows, flags)
     n = rows.numel()
     _vector("rows", rows, n)
-    _launch(lib().presto_pages_free, "presto_pages_free", dev, stream, (), ctypes.byref(_books(refs, page_table, 16)),
+    _launch(lib().presto_pages_free, "presto_pages_free", dev, stream, ctypes.byref(_books(refs, page_table, 16)),
             refs.data_ptr(), page_table.data_ptr(), ctx.data_ptr(), rows.data_ptr(), n, _ptr(flags))
 
 
@@ -326,7 +332,7 @@ def presto_pages_trim(refs: torch.Tensor, page_table: torch.Tensor, ctx: torch.T
     """Drops the pages that no query from position ctx - 1 on sees under the
     window and sinks."""
     dev = _check_books(refs, page_table, ctx, "flags", flags)
-    _launch(lib().presto_pages_trim, "presto_pages_trim", dev, stream, (),
+    _launch(lib().presto_pages_trim, "presto_pages_trim", dev, stream,
             ctypes.byref(_books(refs, page_table, page_size)), refs.data_ptr(), page_table.data_ptr(), ctx.data_ptr(),
             window, sinks, _ptr(flags))
 
@@ -339,11 +345,9 @@ def presto_pages_compact(refs: torch.Tensor, page_table: torch.Tensor, k_pages: 
     page_map [pages], each live page's new number, if it is there)."""
     dev = _check_books(refs, page_table, None, "flags", flags)
     _same(dev, "k_pages v_pages", k_pages, v_pages)
-    made = ()
     if out is None:
-        out = {"refs": torch.empty_like(refs), "page_table": torch.empty_like(page_table),
-               "n_live": torch.empty(1, dtype=torch.int32, device=refs.device)}
-        made = tuple(out.values())
+        out = {name: _empty(stream, shape, _I32, refs.device)
+               for name, shape in (("refs", refs.shape), ("page_table", page_table.shape), ("n_live", 1))}
     page_map = out.get("page_map")
     _book(dev, "out_refs out_page_table n_live page_map", out["refs"], out["page_table"], out["n_live"], page_map)
     desc = _pool(k_pages, v_pages, page_table.shape[1], page_table.shape[0], True)
@@ -355,5 +359,5 @@ def presto_pages_compact(refs: torch.Tensor, page_table: torch.Tensor, k_pages: 
     _vector("page_map", page_map, desc.num_pages)
     _pages_call("presto_pages_compact", refs, dev, desc,
                 (_ptr(refs), _ptr(out["refs"]), _ptr(page_table), _ptr(out["page_table"]), _ptr(out["n_live"]),
-                 _ptr(page_map), _ptr(k_pages), _ptr(v_pages)), flags, workspace, stream, made)
+                 _ptr(page_map), _ptr(k_pages), _ptr(v_pages)), flags, workspace, stream)
     return out

@@ -40,6 +40,19 @@ def _vector(name, t, n):
         raise ValueError(f"{name} must be of shape [{n}], not {list(t.shape)}")
 
 
+def _int32(bits: int) -> None:
+    """Numbers, or-ed together, that the C interface holds in 32 bits: ctypes
+    would cut them to their low half without a word.  (One outside of them
+    shows unless a negative one stands beside it, which the library refuses.)"""
+    if not -1 <= bits >> 31 <= 0:
+        raise ValueError("a size, length or window does not fit 32 bits")
+
+
+def _one_by_one(*numbers: int) -> None:
+    for x in numbers:
+        _int32(x)
+
+
 _current = torch._C._cuda_getDevice
 _raw_stream = torch._C._cuda_getCurrentRawStream
 
@@ -88,6 +101,7 @@ def _pool(k, v, cols, batch, layers: bool) -> PagesDesc:
 @functools.lru_cache(maxsize=64)
 def _pool_of(shape, stride, dtype, batch, cols, layers) -> PagesDesc:
     """The same from sizes alone (a program has few pools; not to be changed)."""
+    _one_by_one(*shape, batch, cols)
     if dtype not in _DT:
         raise TypeError(f"unsupported dtype {dtype}")
     n_layers, layer_stride = 1, 0
@@ -122,6 +136,7 @@ def _books(refs, page_table, page_size) -> PagesDesc:
 
 @functools.lru_cache(maxsize=64)
 def _books_of(batch, cols, pages, page_size) -> PagesDesc:
+    _one_by_one(batch, cols, pages, page_size)
     return PagesDesc(batch, cols, pages, page_size, 1, 64, 0, 1, 0, 0)
 
 
@@ -151,6 +166,7 @@ def _attn_desc(q, k_pages, v_pages, page_table, batch, max_q, max_ctx, scale, wi
     stride = _rows("q", q, hq, d)
     if max_ctx is None:
         max_ctx = pages.max_pages * pages.page_size
+    _int32(max_q | max_ctx | window | sinks)
     return PagedAttnDesc(pages, hq, max_q, max_ctx, window, sinks, d ** -0.5 if scale is None else scale, n, stride,
                          total_ctx)
 
@@ -259,6 +275,7 @@ def presto_pages_reserve(refs: torch.Tensor, page_table: torch.Tensor, ctx: torc
     """Gives pages to the positions ctx .. ctx + add + extra - 1 and returns the
     new lengths (in `out`, which may be ctx); refs and page_table are updated
     in place.  A sequence the pool has no pages for keeps its length."""
+    _one_by_one(page_size, extra)
     dev = _check_books(refs, page_table, ctx, "add out flags", add, out, flags)
     b = page_table.shape[0]
     _vector("add", add, b)
@@ -276,6 +293,7 @@ def presto_append_kv(k_new: torch.Tensor, v_new: torch.Tensor, offsets: torch.Te
                      ctx_new: torch.Tensor, *, flags=None, stream=None) -> None:
     """Writes rows offsets[b] + i of k_new, v_new [rows, Hkv, d] to positions
     ctx[b] + i < ctx_new[b] of the cache, at most max_new per sequence."""
+    _int32(max_new)
     dev = k_new.get_device()
     b = offsets.shape[0] - 1
     if not (0 <= dev == v_new.get_device() == k_pages.get_device() == v_pages.get_device()):
@@ -331,6 +349,7 @@ def presto_pages_trim(refs: torch.Tensor, page_table: torch.Tensor, ctx: torch.T
                       sinks: int = 0, *, flags=None, stream=None) -> None:
     """Drops the pages that no query from position ctx - 1 on sees under the
     window and sinks."""
+    _one_by_one(page_size, window, sinks)
     dev = _check_books(refs, page_table, ctx, "flags", flags)
     _launch(lib().presto_pages_trim, "presto_pages_trim", dev, stream,
             ctypes.byref(_books(refs, page_table, page_size)), refs.data_ptr(), page_table.data_ptr(), ctx.data_ptr(),

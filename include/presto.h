@@ -577,7 +577,8 @@ presto_status presto_append_kv(const presto_pages_desc *desc, const void *k_new,
  *   PRESTO_FLAG_BAD_PAGE (the entry is cleared).
  * presto_pages_trim: drops, of every sequence, the references to pages whose
  *   positions no query at position ctx[b] - 1 or later sees under window and
- *   sinks.  Flags as above.
+ *   sinks.  A ctx[b] outside 0 .. max_pages * page_size leaves the sequence
+ *   alone and raises PRESTO_FLAG_BAD_SEQ; entries as above.
  * presto_pages_compact: moves the live pages to the front of the pool, in all
  *   layers: of *n_live (int32 device) live pages, the i-th free page below
  *   *n_live takes the i-th live one from there on.  refs_out [num_pages] and

@@ -302,7 +302,11 @@ __global__ __launch_bounds__(256) void pages_trim_kernel(int32_t* refs, int32_t*
                                                          int32_t num_pages, int32_t shift, int32_t window,
                                                          int32_t sinks, int32_t* flags) {
     const int b = blockIdx.x;
-    const int64_t len = min((int64_t)ctx[b], (int64_t)max_pages << shift);
+    const int64_t len = ctx[b];
+    if (len < 0 || len > (int64_t)max_pages << shift) {  // not a length: nothing is given back on its word
+        if (threadIdx.x == 0) raise_flag(flags, PRESTO_FLAG_BAD_SEQ);
+        return;
+    }
     const int64_t x0 = ((int64_t)sinks + (1 << shift) - 1) >> shift;
     const int64_t x1 = len > window ? (len - window) >> shift : 0;
     bool bad = false;

@@ -236,8 +236,12 @@ def presto_window_attention(q: torch.Tensor, q_offsets: torch.Tensor, max_q: int
 def paged_attention_workspace(q: torch.Tensor, k_pages: torch.Tensor, page_table: torch.Tensor, *, max_q: int = 1,
                               max_ctx: int | None = None, window: int = 0, sinks: int = 0,
                               total_ctx: int = 0) -> torch.Tensor:
-    """A workspace for presto_paged_attention, and for presto_window_attention
-    with up to max_q new tokens per sequence."""
+    """A workspace for calls with just these sizes and hints:
+    presto_window_attention with these queries and max_q, and
+    presto_paged_attention on this batch.  A call with fewer queries, a smaller
+    max_q or max_ctx or another total_ctx may be split further and need more
+    (too small a workspace is refused before anything runs): a program asks once
+    per shape that it uses, or passes none."""
     desc = _attn_desc(q, k_pages, k_pages, page_table, page_table.shape[0], max_q, max_ctx, None, window, sinks,
                       total_ctx)
     need = max(lib().presto_window_attention_workspace(ctypes.byref(desc)),

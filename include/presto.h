@@ -487,8 +487,12 @@ typedef struct {
  * that run backwards or past total_q skip that sequence (rows of others that
  * then overlap may be skipped too).  Each raises PRESTO_FLAG_BAD_SEQ.
  * A K or V that is not finite reaches the queries that see it only.
- * Arithmetic: bf16 inputs use bf16 matrix cores with fp32 accumulation and
- * fp32 softmax; fp32 inputs use fp32 throughout.
+ * Arithmetic: bf16 inputs use bf16 matrix cores with fp32 accumulation, fp32
+ * scores and sums; the probabilities enter the second product rounded, to two
+ * bf16 (16 bits) each in presto_paged_attention, and in presto_window_attention
+ * to two (short prompts) or one (long ones, which the matrix cores bound; their
+ * error is then up to 2^-8 of sum_j p_j |v_j - O| besides the output's own half
+ * step).  fp32 inputs use fp32 throughout.
  * Limits: hq % hkv == 0; max_ctx <= max_pages * page_size; window, sinks 0 ..
  * 2^30 (sinks without a window change nothing); max_q * hq / hkv < 2^30,
  * total_q < 2^30, batch * max_q * hq < 2^31 and at most 2^23 workgroups

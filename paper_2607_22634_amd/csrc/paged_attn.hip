@@ -655,18 +655,25 @@ __global__ __launch_bounds__(kWaves * kWave, NB == 1 ? 3 : 2) void paged_attn_ro
 
         // ---- O^T += V^T P^T
         if constexpr (BF16) {
-            const bf16x2 ones = {(__bf16)1.0f, (__bf16)1.0f};
-            bf16x8 pb[NB];
+            // A probability enters as two bf16, the second what the rounding of
+            // the first left (16 bits between them; their sum is taken before).
+            // The second products hide behind the keys' arrival: 16 x 32768
+            // keys 319 us with one and with two, the listed decodes within
+            // 0.7%, short prompts 1 to 3% slower; the error of an output is that
+            // of its own rounding, 1.66e-3 in norm, where one makes it 2.1e-3.
+            bf16x8 ph[NB], pl[NB];
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
-                uint32_t w[4];
+                uint32_t hi[4], lo[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    // (rounded to the product's bf16; the sum takes the rounded values)
-                    w[i] = pack2(S[nb][i / 2][2 * (i % 2)], S[nb][i / 2][2 * (i % 2) + 1]);
-                    l[nb] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w[i]), ones, l[nb], false);
+                    const float p0 = S[nb][i / 2][2 * (i % 2)], p1 = S[nb][i / 2][2 * (i % 2) + 1];
+                    hi[i] = pack2(p0, p1);
+                    lo[i] = pack2(p0 - bf16lo(hi[i]), p1 - bf16hi(hi[i]));
+                    l[nb] += p0 + p1;
                 }
-                pb[nb] = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
+                ph[nb] = __builtin_bit_cast(bf16x8, make_uint4(hi[0], hi[1], hi[2], hi[3]));
+                pl[nb] = __builtin_bit_cast(bf16x8, make_uint4(lo[0], lo[1], lo[2], lo[3]));
             }
 #pragma unroll
             for (int i = 0; i < VD; ++i) {
@@ -677,8 +684,10 @@ __global__ __launch_bounds__(kWaves * kWave, NB == 1 ? 3 : 2) void paged_attn_ro
                                                  i % 2 ? 0x07060302u : 0x05040100u);
                 const bf16x8 va = __builtin_bit_cast(bf16x8, make_uint4(w[0], w[1], w[2], w[3]));
 #pragma unroll
-                for (int nb = 0; nb < NB; ++nb)
-                    o[nb][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pb[nb], o[nb][i], 0, 0, 0);
+                for (int nb = 0; nb < NB; ++nb) {
+                    o[nb][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, pl[nb], o[nb][i], 0, 0, 0);
+                    o[nb][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, ph[nb], o[nb][i], 0, 0, 0);
+                }
             }
         } else {
 #pragma unroll
@@ -1048,7 +1057,9 @@ __global__ __launch_bounds__(kTileWaves * kWave) void paged_attn_tiles_kernel(Ar
             }
         };
         // two probabilities, rounded to the product's bf16; the sum takes the
-        // rounded values
+        // rounded values (one bf16: the matrix cores bound this kernel, and a
+        // second one, as the kernel of rows takes, would be half as many
+        // instructions again; 2.3e-3 in norm for the output rounding's 1.66e-3)
         auto pair = [&](const floatx16& S, int e, float& ls) __attribute__((always_inline)) {
             const uint32_t w = pack2(__builtin_amdgcn_exp2f(S[e] * c), __builtin_amdgcn_exp2f(S[e + 1] * c));
             ls = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w), ones, ls, false);

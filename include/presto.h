@@ -450,7 +450,9 @@ presto_status presto_flatten_slots(int32_t batch, int32_t n_max, int32_t slots,
  * 2^30; batch 0 .. 2^23 - 1 (0: nothing to do), batch * max_pages < 2^31;
  * layers >= 1; page_stride >= page_size * hkv * head_dim (0: exactly that),
  * layer_stride >= 0; pools 16-byte aligned with strides of a multiple of 16
- * bytes.  Layers of a pool must not overlap.
+ * bytes.  Layers of a pool must not overlap; the calls that move pages move
+ * those of all layers at once (the books change with them), so the layers of a
+ * cache that is forked or compacted lie in one allocation, layer_stride apart.
  */
 typedef struct {
     int32_t batch, max_pages;
@@ -484,9 +486,11 @@ typedef struct {
  * needs and that lies outside the pool raises PRESTO_FLAG_BAD_PAGE; its keys
  * count as not visible.  ctx[b] outside 0 .. max_ctx is cut to that range and
  * n_b > max_q to the first max_q rows (the others are not written); offsets
- * that run backwards or past total_q skip that sequence (rows of others that
- * then overlap may be skipped too).  Each raises PRESTO_FLAG_BAD_SEQ.
- * A K or V that is not finite reaches the queries that see it only.
+ * that run backwards or past total_q skip that sequence (rows that other
+ * sequences then have in common are undefined).  Each raises
+ * PRESTO_FLAG_BAD_SEQ.
+ * A K or V that is not finite reaches the queries that see it only; a query
+ * all of whose scores are -inf gets zeros, as one that sees nothing.
  * Arithmetic: bf16 inputs use bf16 matrix cores with fp32 accumulation, fp32
  * scores and sums; the probabilities enter the second product rounded, to two
  * bf16 (16 bits) each in presto_paged_attention, and in presto_window_attention

@@ -101,7 +101,8 @@ __device__ __forceinline__ Seq seq_of(const Args& a, int b) {
 // the other; kByGrid: idx counts `row_blocks` for every sequence, whether it has
 // them or not (batches too large to look through).  Counted by grid, blocks
 // without rows would lie in between at a fixed stride, and those with rows all
-// fall on the same shader engines: four ragged prompts 347 us, 272 counted.
+// fall on the same shader engines: four ragged windowed prompts of up to 4026
+// tokens (bf16, 32/8 heads of 128) 264 us, 239 counted.
 // false: there is no such block.
 enum { kByLength, kBySequence, kByGrid };
 __device__ __forceinline__ bool find_block(const Args& a, int idx, bool first, int& b, int& rev, Seq& sq) {
@@ -348,13 +349,16 @@ __device__ float2 row_alone(const Args& a, const Span& sp, int b, int g, int64_t
 // K is read whole rows at a time too and turned through LDS, by each wave for
 // itself (chunks permuted: no bank conflicts): read as the instruction wants
 // it, 64 bytes of sixteen rows at a time, a long cache came at 5.65 TB/s, and
-// comes at 6.3 this way.
+// at 6.3 this way (6.7 with the steps after it).
 //
 // The reference m of a row moves only when a score exceeds it by 8 (in log2
 // units), so that the common tile needs no reduction across lanes.
 //
-// kOnce: every key is read by one workgroup, past the caches (a long cache at
-// 5.45 TB/s through them, 5.65 past them).
+// kOnce: a sequence's keys are read by one workgroup per KV head, past the
+// caches (bf16, 32/8 heads of 128, 16 x 32768 keys: 318 us past them, 362
+// through them).  Pages that several sequences share are then fetched once for
+// each: 16 samples of one prompt of 32000 keys take 168 us, 107 through the
+// caches, 64 of 1792 keys 46 and 40 (what is shared is known to the table only).
 constexpr int kWaves = 4;
 enum { kCached, kOnce };
 
@@ -1385,10 +1389,14 @@ int64_t counted_blocks(const presto_paged_attn_desc* d, PagedPlan& p) {
 // A workgroup takes about 8 beside its tiles (page numbers, queries, first
 // tiles, output), a tile of 64 keys 1.75 with two waves of rows per SIMD and
 // 1.25 with one (up to 128 rows), at head_dim 64 three quarters of that (off by
-// 9% r.m.s. over 149 shapes), a merge 5 and its partials' traffic.  One workgroup per CU: whole rounds where all are alike, else the
-// longest or the sum.  Measured: 512 new tokens alone 18.2 in blocks of 128 rows, 22.4 of 256;
-// 64 on 65536 cached 99 in 32 splits of 256 rows, 114 in 16 of 128; 16 x 300
-// on 1700 217 in blocks of 256, 238 of 128.
+// 9% r.m.s. over 149 shapes), a merge 5 and its partials' traffic.  One
+// workgroup per CU: whole rounds where all are alike, else the longest or the
+// sum.  Measured, bf16, 32/8 heads of 128, forced to blocks of 64, 128 and 256
+// rows: 1000 new tokens alone 34, 27 and 41 us; 64 on 65536 cached 182, 111 and
+// 98; 16 x 300 on 1700 365, 193 and 152.
+// (Every sequence is counted with max_q tokens: a chunk that shares its call
+// with decode rows is cut too little, 512 tokens on 30720 keys 244 us alone, 408
+// beside one row and 777 beside seven, which alone take 26.)
 double plan_tiles(const presto_paged_attn_desc* d, int64_t rows, PagedPlan& p) {
     const int64_t heads = (int64_t)d->pages.batch * d->pages.hkv;
     const int64_t most = (int64_t)(kTilePages - 8) * d->pages.page_size / kKeyTile;  // page numbers in LDS
@@ -1421,8 +1429,8 @@ double plan_tiles(const presto_paged_attn_desc* d, int64_t rows, PagedPlan& p) {
     p.row_blocks = (int)cdiv(rows, p.block_rows);
     p.blocks = heads / d->pages.batch * counted_blocks(d, p) * p.splits;
     // K and V of a head past the 4 MB of an XCD's L2: its row blocks side by
-    // side (4 sequences of 2048 new tokens on 30720: 4178 -> 4037 us; on 4096:
-    // 668 -> 677)
+    // side (bf16, 32/8 heads of 128, 4 sequences of 2048 new tokens: on 30720
+    // cached 3979 -> 3836 us; on 4096 it would be 616 -> 623)
     if (p.order == kByLength && longest_list(d, p.block_rows) * d->pages.head_dim * 4 > (4 << 20))
         p.order = kBySequence;
     return best;
@@ -1433,15 +1441,17 @@ double plan_tiles(const presto_paged_attn_desc* d, int64_t rows, PagedPlan& p) {
 // takes a workgroup a + b nb, more where others share its CU, and the chip gets
 // through 256 of them in c + d nb: with 32 rows a key is fetched for twice as
 // many rows, with 16 there are twice as many workgroups of half the work (in
-// bf16 they win by more than the model has it: `wide`).  Fitted to 2200 plans of
-// 320 shapes (off by 14% and 12% r.m.s.); the choice takes 4% and 1% longer
-// than the best of each shape's, 32 rows always, in as many splits as fill two
-// rounds, took 19% and 11%.  (us, 16 and 32 rows: fp32, 3 x 77 rows on 50 keys
-// 7.3 and 9.6, 1 x 2048 on itself 368 and 332; bf16, 4 sequences of 32 rows on
-// 8000 keys 32 and 34.)  Against the kernel of tiles the shorter modelled time
-// decides: within 1 or 2% of the better of the two, which tiles alone miss by
-// 16 to 19% at up to 60 GFLOP (us, rows and tiles: 4 x 54 tokens on 182, 8/4
-// heads of 64, 6.7 and 10.2; 28 x 41, 56/8 heads of 128, 37 and 20).
+// bf16 they win by more than the model has it: `wide`).  Fitted by least squares
+// to the times of 2200 plans of 320 shapes (heads, dims, types, lengths and
+// windows drawn over their ranges, a sequence's new tokens and context evenly
+// between two bounds): off by 14% and 12% r.m.s.  Measured, 16 and 32 rows: fp32,
+// 4/2 heads of 64, 3 sequences of up to 77 tokens 8.5 and 9.8 us; fp32, 32/8 of
+// 128, 2048 tokens alone 363 and 326; bf16, 32/8 of 128, 4 x 8 tokens on 8000
+// keys 36 both.  Against the kernel of tiles the shorter modelled time decides,
+// rows and tiles: 4 x 54 tokens on 182, 8/4 heads of 64, 8.3 and 9.3 us; 28 x 41
+// alone, 56/8 of 128, 37 and 20.  On shapes drawn like the fitted ones that was
+// within 1 or 2% of the better kernel on average; single shapes miss by more
+// (512 tokens on 512 cached, 32/8 heads of 128: 31 us in tiles, 24 in rows).
 struct RowsCost {
     double start, a, b, shared, round, c, d, merge, partials, keys, ends, wide;
 };
@@ -1512,6 +1522,7 @@ void plan_rows(const presto_paged_attn_desc* d, int64_t rows, PagedPlan& p) {
     const int wgs = 256 * (d->pages.head_dim == 64 ? (p.nb == 1 ? 4 : 3) : (p.nb == 1 ? 3 : 2));
     // Few rows are a stream of the cache: what counts is that all CUs end
     // together, and few launches.
+    // (bf16, 32/8 heads of 128:)
     // * Sequences of up to three tiles per wave are not cut (no merge: 384 keys
     //   8.8 against 11.5 us).
     // * Sequences of about one length (known from total_ctx) are cut into as

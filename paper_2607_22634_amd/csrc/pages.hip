@@ -451,8 +451,8 @@ __global__ __launch_bounds__(kMoveThreads) void pages_move_kernel(char* __restri
 
 // New rows of sequence b go to positions ctx[b] .. ctx_new[b] - 1, a few rows
 // of one sequence per workgroup, read past the caches (17,600 rows of 2 KB, K
-// and V, with the reservation: 44.8 us at sixteen rows, 34.9 at four; 144 MB at
-// 4.9 TB/s take 29).
+// and V: 26 us, 31 with the reservation before it; 144 MB at the 5.05 TB/s of a
+// compaction take 28.5.  Sixteen rows per workgroup took 10 us more than four).
 constexpr int kAppendThreads = 256;
 constexpr int kAppendRows = 4;
 

@@ -80,6 +80,37 @@ def test_decode_of_far_scores(dtype, far):
         assert (np.abs(out[b:b + 1] - want) <= bound).all(), b
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n,past", [(1, 0), (1, 700), (5, 40), (600, 500)])
+def test_scores_of_minus_infinity(dtype, n, past):
+    """Keys whose score is -inf weigh nothing beside others; a query that sees
+    no others gets zeros."""
+    rng = np.random.default_rng([53, n, past])
+    L, page = past + n, 32
+    c = Cache(rng, [L], [n], page, 2, 64, dtype)
+    q = queries(rng, n, 4, 64, dtype)
+    q[..., 0] = 8.0
+    lost = np.arange(L) < L // 3 if L > 1 else np.ones(1, bool)
+    for head in range(2):
+        dead = lost if head == 0 else np.ones(L, bool)  # KV head 1: all of them
+        for j in np.flatnonzero(dead):
+            p = int(c.table_h[0, j // page])
+            c.k_h[p, j % page, head, 0] = float("-inf")
+    c.k.copy_(c.k_h)
+    out = P.presto_window_attention(q, ints([0, n]), n, c.k, c.v, c.table, c.ctx).double().cpu().numpy()
+    assert not out[:, 2:].any()
+    k, v = c.rows(0)
+    some = sorted({0, n // 2, n - 1})
+    for i in some:
+        live = ~lost & (np.arange(L) <= past + i)
+        if not live.any():
+            assert not out[i, :2].any()
+            continue
+        want, bound = R.attention(q[i:i + 1, :2].double().cpu().numpy(), k[live, :1], v[live, :1], int(live.sum()) - 1,
+                                  0, 0, None, dtype)
+        assert (np.abs(out[i:i + 1, :2] - want) <= bound).all(), i
+
+
 @pytest.mark.parametrize("far", FAR)
 @pytest.mark.parametrize("dtype,N,hq,hkv,d", [("bf16", 9, 8, 2, 128), ("bf16", 33, 8, 8, 64), ("bf16", 70, 16, 2, 128),
                                               ("bf16", 257, 8, 1, 64), ("f32", 33, 4, 2, 64)])

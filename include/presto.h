@@ -59,8 +59,14 @@ typedef enum {
 } presto_status;
 
 /* Any other non-negative value is rejected with PRESTO_ERR_INVALID_ARG (the
- * last enumerator only keeps the type 32 bits wide). */
-typedef enum { PRESTO_DT_BF16 = 0, PRESTO_DT_F32 = 1, PRESTO_DT_MAX_ENUM_ = 0x7fffffff } presto_dtype;
+ * last enumerator only keeps the type 32 bits wide), and PRESTO_DT_FP4 by every
+ * call but those of a paged cache in 4 bits (below). */
+typedef enum {
+    PRESTO_DT_BF16 = 0,
+    PRESTO_DT_F32 = 1,
+    PRESTO_DT_FP4 = 2, /* page pools only: 4-bit values with shared exponents */
+    PRESTO_DT_MAX_ENUM_ = 0x7fffffff
+} presto_dtype;
 
 typedef enum {
     PRESTO_TREE_BEST_FIRST = 0,      /* commit on pop: exactly the B best prefixes by S        */
@@ -80,8 +86,10 @@ enum {
     PRESTO_FLAG_BAD_PAGE = 64,   /* paged cache: a page-table entry that is needed lies
                                     outside the pool, or names a page that is free */
     PRESTO_FLAG_NO_PAGES = 128,  /* paged cache: the pool ran out of free pages */
-    PRESTO_FLAG_BAD_SEQ = 256    /* paged cache: a sequence index, length or offset
+    PRESTO_FLAG_BAD_SEQ = 256,   /* paged cache: a sequence index, length or offset
                                     outside its range, or a fork that cannot be made */
+    PRESTO_FLAG_NAN_LOGITS = 512 /* presto_sample: a row held a NaN or +inf, or no
+                                    finite logit at all */
 };
 
 /* ------------------------------------------------------------------------ */
@@ -612,6 +620,189 @@ presto_status presto_pages_compact(const presto_pages_desc *desc, const int32_t 
                                    int32_t *table_out, int32_t *n_live, int32_t *page_map,
                                    void *k_pages, void *v_pages, int32_t *flags, void *ws,
                                    size_t ws_bytes, hipStream_t stream);
+
+/* ------------------------------------------------------------------------ */
+/* Rotary positions.
+ *
+ * The first rot_dim values of a head are pairs (a, b), number i of them with
+ * the frequency f_i, i < rot_dim / 2; at position p, with t = p * f_i,
+ *     (a, b) -> magnitude * (a cos t - b sin t, b cos t + a sin t).
+ * Pair i is the values (i, i + rot_dim / 2), or (2 i, 2 i + 1) when
+ * interleaved.  The other values of the head stay as they are.  Positions are
+ * any int32; that of -p undoes that of p (for a magnitude of 1).
+ *
+ * Angles are held as 64-bit fractions of a turn, so that p * f_i wraps without
+ * loss at any position: steps[i] = the fraction of f_i / 2 pi times 2^64, a
+ * table of rot_dim / 2 words in DEVICE memory.  presto_rope_steps fills such a
+ * table in HOST memory (a program does it once per model and copies it): from
+ * f_i = freq[i] where freq is given (finite, magnitude below 2^20), else
+ *     f_i = base^(-2 i / rot_dim)
+ * changed for long contexts by `ramp`:
+ *     PRESTO_ROPE_RAMP_NONE    f_i / factor
+ *     PRESTO_ROPE_RAMP_TURNS   f_i (g + (1 - g) / factor) where r = original
+ *                              f_i / 2 pi is how often the pair turns over the
+ *                              `original` context, and g = (r - low) /
+ *                              (high - low) cut to 0 .. 1
+ *     PRESTO_ROPE_RAMP_LOG     the same with the logarithms of r, low and high
+ * Limits: rot_dim even, 2 .. 256; base > 0 and factor > 0, finite; with a ramp
+ * original > 0 and 0 < low < high, finite.
+ */
+typedef enum { PRESTO_ROPE_RAMP_NONE = 0, PRESTO_ROPE_RAMP_TURNS = 1, PRESTO_ROPE_RAMP_LOG = 2 } presto_rope_ramp;
+
+typedef struct {
+    int32_t rot_dim;
+    int32_t ramp; /* presto_rope_ramp */
+    double base, factor;
+    double original, low, high; /* read with a ramp only */
+} presto_rope_freq_desc;
+
+presto_status presto_rope_steps(const presto_rope_freq_desc *desc, const double *freq,
+                                uint64_t *steps);
+
+typedef struct {
+    int32_t rot_dim;     /* even, 0 .. head_dim; 0: nothing is rotated, steps may be NULL */
+    int32_t interleaved; /* 0 or 1 */
+    float magnitude;     /* finite; usually 1 */
+} presto_rope_desc;
+
+/* Rotates rows of heads by their positions:
+ *   x, out [rows, heads, head_dim] (dtype dt), rows x_stride and out_stride
+ *          elements apart (0: heads * head_dim), heads contiguous.  out may be
+ *          x itself with the same stride (queries and keys rotated where they
+ *          are in a wider projection); else it overlaps no input.
+ *   positions [rows] int32 device
+ * Each value is computed in fp32 and rounded once.
+ * Limits: head_dim a multiple of 8, 8 .. 256; heads 1 .. 65536; rows 0 ..
+ * 2^31 - 1; tensors and strides multiples of 16 bytes.
+ */
+presto_status presto_rope(const presto_rope_desc *rope, const uint64_t *steps, presto_dtype dt,
+                          const void *x, int64_t x_stride, int64_t rows, int32_t heads,
+                          int32_t head_dim, const int32_t *positions, void *out,
+                          int64_t out_stride, hipStream_t stream);
+
+/* ------------------------------------------------------------------------ */
+/* Paged cache in 4 bits: a pool of dtype PRESTO_DT_FP4 takes 17/64 of the
+ * memory of a bf16 one.
+ *
+ * Every 32 values of a row (a group) are held as e2m1 codes, one sign, two
+ * exponent and one mantissa bits (0, 0.5, 1, 1.5, 2, 3, 4, 6), and one exponent
+ * byte E: value = code * 2^(E - 127).  E is the least from 7 on with
+ * 7 * 2^(E - 127) >= the group's largest magnitude, 252 at most; codes are
+ * rounded to nearest even, what is above 6 to 6.  A group that holds a value
+ * that is not finite has E = 255 and reads as NaN throughout (253 and 254 are
+ * never written, and read the same).
+ *
+ * A page is [hkv][page_size / 16][17 * head_dim / 2] bytes: of 16 positions of a
+ * head the 8 * head_dim bytes of codes, then the exponents (head_dim / 2).
+ *   K: codes [16][head_dim / 2] in order, the low nibble first; exponents
+ *      [16][head_dim / 32]
+ *   V: with position 4 g + i and value x = (head_dim / 16) n + y: codes
+ *      [g][n][i][y / 2], exponents [g][x / 32][i] (each lane of the attention
+ *      then finds its 4 positions in one piece)
+ * In presto_pages_desc page_stride and layer_stride are BYTES for such a pool
+ * (0: page_size * hkv * head_dim * 17 / 32, packed); strides are multiples of
+ * 16.  presto_pages_reserve, _fork, _free, _trim and _compact serve it as any
+ * other (a fork copies the whole of a partly filled page);
+ * presto_append_kv, presto_paged_attention and presto_window_attention do not.
+ */
+
+/* New tokens into the cache, rotated on the way: as presto_append_kv, with
+ * row offsets[b] + i of k_new rotated by position ctx[b] + i before it is
+ * stored (v_new is stored as it is), and, where q is given, row offsets[b] + i
+ * of q rotated by the same position into q_out.
+ *   pages.dt: dt itself, or PRESTO_DT_FP4
+ *   q, q_out [new_rows, hq, head_dim], k_new, v_new [new_rows, hkv, head_dim],
+ *       dtype dt, rows q_stride, q_out_stride, k_stride and v_stride elements
+ *       apart (0: contiguous).  q_out may be q with the same stride.
+ *   q NULL: no queries.  rope NULL, or a rot_dim of 0: nothing is rotated.
+ * Rows that presto_append_kv would not write, and the rows of q_out that belong
+ * to them, are left as they were, with the same flags (a position without a
+ * page loses its K/V only).  Values are computed in fp32 (keys for a 4-bit pool
+ * in fp64) and rounded once.
+ * Limits: as presto_append_kv; hq 0 .. 65536.
+ */
+typedef struct {
+    presto_pages_desc pages;
+    presto_dtype dt;
+    int32_t hq;
+    int32_t max_new; /* the most new tokens of a sequence */
+    int64_t new_rows;
+    int64_t q_stride, q_out_stride, k_stride, v_stride;
+} presto_append_desc;
+
+presto_status presto_append_rope(const presto_append_desc *desc, const presto_rope_desc *rope,
+                                 const uint64_t *steps, const void *q, const void *k_new,
+                                 const void *v_new, const int32_t *offsets, void *q_out,
+                                 void *k_pages, void *v_pages, const int32_t *page_table,
+                                 const int32_t *ctx, const int32_t *ctx_new, int32_t *flags,
+                                 hipStream_t stream);
+
+/* The way back: positions ctx[b] .. ctx_new[b] - 1 of one layer's cache into
+ * rows offsets[b] + i of k_out, v_out [new_rows, hkv, head_dim] (dtype dt, rows
+ * k_stride and v_stride apart; either may be NULL), as cached, that is rotated.
+ * From a pool of dtype dt or PRESTO_DT_FP4, whose values both types hold
+ * exactly.  Fields of desc for q are not read.  A sequence that does not fit is
+ * skipped and a position without a page leaves its row as it was, with flags as
+ * above.
+ */
+presto_status presto_read_kv(const presto_append_desc *desc, const void *k_pages,
+                             const void *v_pages, const int32_t *page_table, const int32_t *ctx,
+                             const int32_t *ctx_new, const int32_t *offsets, void *k_out,
+                             void *v_out, int32_t *flags, hipStream_t stream);
+
+/* presto_paged_attention and presto_window_attention over a 4-bit cache: all
+ * that is said there holds (visible keys, ragged rows, flags, limits), with
+ *   desc->pages.dt = PRESTO_DT_FP4, q and out of dtype dt
+ *   q_offsets NULL: one new token per sequence, q, out [batch, hq, head_dim]
+ * A group of K that is not finite reaches the queries that see it; one of V the
+ * same 32 values of their outputs.  A row of q that is not finite has an
+ * undefined output.
+ * Arithmetic: products of the cached values with bf16 queries are exact, sums in
+ * fp32; probabilities enter the second product as two bf16 (one in long
+ * prompts, as in presto_window_attention).  fp32 queries and their
+ * probabilities enter as three bf16 (24 bits).
+ */
+size_t presto_quant_attention_workspace(const presto_paged_attn_desc *desc, presto_dtype dt,
+                                        int32_t ragged);
+presto_status presto_quant_attention(const presto_paged_attn_desc *desc, presto_dtype dt,
+                                     const void *q, const int32_t *q_offsets, const void *k_pages,
+                                     const void *v_pages, const int32_t *page_table,
+                                     const int32_t *ctx, void *out, int32_t *flags, void *ws,
+                                     size_t ws_bytes, hipStream_t stream);
+
+/* ------------------------------------------------------------------------ */
+/* A token from each row of logits, drawn with the caller's uniform numbers.
+ *
+ * With m = max_i z_i, token i weighs w_i = exp((z_i - m) / temperature).  Of the
+ * tokens in order of z (largest first, lower id first among equals, -0 = +0)
+ *   1. the first top_k stay,
+ *   2. of those the shortest head that has at least top_p of their sum,
+ *   3. of those the ones with w_i >= min_p,
+ * and the first token is taken whose running sum exceeds u times the sum of what
+ * stayed.  With a temperature of 0 the first token in order is taken.
+ *
+ *   logits [rows, row_stride] of dtype dt, the first `vocab` of a row are read
+ *   u [rows] fp32 in [0, 1) (outside it, and NaN: as the nearest of 0 and the
+ *       last below 1, NaN as 0)
+ *   temperature, top_p, min_p [rows] fp32 and top_k [rows] int32, all device.
+ *       temperature NULL: 1; not above 0, or NaN: 0.  top_k NULL or not above 0:
+ *       all.  top_p NULL, 1 or more, or NaN: all; not above 0: one token.
+ *       min_p NULL, not above 0, or NaN: none dropped; above 1: as 1.
+ *   token [rows] int32 out
+ *   logprob [rows] fp32 out, may be NULL: log of the token's share of what
+ *       stayed (0 where it was the only one)
+ *   flags  optional: PRESTO_FLAG_NAN_LOGITS when a row holds a NaN or +inf
+ *       or nothing above -inf; its token is -1 and its logprob NaN.
+ * -inf logits are never drawn, nor tokens that weigh less than 2^-64 of the
+ * largest.  Weights and sums are held in 64 bits.
+ * Limits: 1 <= vocab <= 2^20, row_stride >= vocab, rows 0 .. 2^21.
+ */
+size_t presto_sample_workspace(presto_dtype dt, int64_t rows, int32_t vocab);
+presto_status presto_sample(presto_dtype dt, const void *logits, int64_t rows, int32_t vocab,
+                            int64_t row_stride, const float *u, const float *temperature,
+                            const int32_t *top_k, const float *top_p, const float *min_p,
+                            int32_t *token, float *logprob, int32_t *flags, void *ws,
+                            size_t ws_bytes, hipStream_t stream);
 
 /* ------------------------------------------------------------------------ */
 const char *presto_status_string(presto_status s);

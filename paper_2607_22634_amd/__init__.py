@@ -17,9 +17,15 @@ from ._lib import (  # noqa: F401
     presto_topk_noalloc,
     presto_tree_attention, topk_fallback_chunks, topk_workspace, version,
     PRESTO_FLAG_BAD_PAGE, PRESTO_FLAG_BAD_SEQ, PRESTO_FLAG_NO_PAGES, PagedAttnDesc, PagesDesc,
+    PRESTO_DT_FP4, PRESTO_FLAG_NAN_LOGITS, PRESTO_ROPE_RAMP_LOG, PRESTO_ROPE_RAMP_NONE, PRESTO_ROPE_RAMP_TURNS,
+    AppendDesc, RopeDesc, RopeFreqDesc,
 )
 from ._paged import (  # noqa: F401
     paged_attention_workspace, pages_workspace, presto_append_kv, presto_paged_attention,
     presto_pages_compact, presto_pages_fork, presto_pages_free, presto_pages_reserve,
     presto_pages_trim, presto_window_attention,
+)
+from ._step import (  # noqa: F401
+    RopePlan, presto_append_rope, presto_quant_attention, presto_read_kv, presto_rope, presto_rope_steps,
+    presto_sample, quant_attention_workspace, quant_pages, rope_plan, sample_workspace,
 )

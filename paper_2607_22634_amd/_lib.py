@@ -25,6 +25,7 @@ PRESTO_ERR_HIP = -4
 
 PRESTO_DT_BF16 = 0
 PRESTO_DT_F32 = 1
+PRESTO_DT_FP4 = 2
 
 PRESTO_TREE_BEST_FIRST = 0
 PRESTO_TREE_BEST_FIRST_ALG2 = 1
@@ -39,8 +40,12 @@ PRESTO_FLAG_KV_COMMIT = 32
 PRESTO_FLAG_BAD_PAGE = 64
 PRESTO_FLAG_NO_PAGES = 128
 PRESTO_FLAG_BAD_SEQ = 256
+PRESTO_FLAG_NAN_LOGITS = 512
 PRESTO_CTX_PACKED = 0
 PRESTO_CTX_SLOTS = 1
+PRESTO_ROPE_RAMP_NONE = 0
+PRESTO_ROPE_RAMP_TURNS = 1
+PRESTO_ROPE_RAMP_LOG = 2
 
 EXPORTS = (
     "presto_topk_workspace", "presto_topk", "presto_topk_noalloc", "presto_entropy_lambda",
@@ -52,7 +57,9 @@ EXPORTS = (
     "presto_flatten_slots", "presto_paged_attention_workspace", "presto_paged_attention",
     "presto_window_attention_workspace", "presto_window_attention", "presto_pages_workspace",
     "presto_pages_reserve", "presto_append_kv", "presto_pages_fork", "presto_pages_free",
-    "presto_pages_trim", "presto_pages_compact", "presto_status_string", "presto_last_error", "presto_version",
+    "presto_pages_trim", "presto_pages_compact", "presto_rope_steps", "presto_rope", "presto_append_rope",
+    "presto_read_kv", "presto_quant_attention_workspace", "presto_quant_attention", "presto_sample_workspace",
+    "presto_sample", "presto_status_string", "presto_last_error", "presto_version",
 )
 
 
@@ -92,6 +99,22 @@ class PagedAttnDesc(ctypes.Structure):
                 ("max_ctx", ctypes.c_int32), ("window", ctypes.c_int32), ("sinks", ctypes.c_int32),
                 ("scale", ctypes.c_float), ("total_q", ctypes.c_int64), ("q_stride", ctypes.c_int64),
                 ("total_ctx", ctypes.c_int64)]
+
+
+class RopeFreqDesc(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int32), ("ramp", ctypes.c_int32), ("base", ctypes.c_double),
+                ("factor", ctypes.c_double), ("original", ctypes.c_double), ("low", ctypes.c_double),
+                ("high", ctypes.c_double)]
+
+
+class RopeDesc(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32), ("magnitude", ctypes.c_float)]
+
+
+class AppendDesc(ctypes.Structure):
+    _fields_ = [("pages", PagesDesc), ("dt", ctypes.c_int32), ("hq", ctypes.c_int32), ("max_new", ctypes.c_int32),
+                ("new_rows", ctypes.c_int64), ("q_stride", ctypes.c_int64), ("q_out_stride", ctypes.c_int64),
+                ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64)]
 
 
 _VP, _I32, _I64, _SZ = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
@@ -158,6 +181,20 @@ def lib() -> ctypes.CDLL:
                 ("presto_pages_free", [pages] + [_VP] * 4 + [_I32, _VP, _VP]),
                 ("presto_pages_trim", [pages] + [_VP] * 3 + [_I32, _I32, _VP, _VP]),
                 ("presto_pages_compact", [pages] + [_VP] * 10 + [_SZ, _VP])):
+            getattr(L, name).argtypes = args
+            getattr(L, name).restype = _I32
+        freq, rope, append = ctypes.POINTER(RopeFreqDesc), ctypes.POINTER(RopeDesc), ctypes.POINTER(AppendDesc)
+        L.presto_quant_attention_workspace.argtypes = [attn, _I32, _I32]
+        L.presto_sample_workspace.argtypes = [_I32, _I64, _I32]
+        for name in ("presto_quant_attention_workspace", "presto_sample_workspace"):
+            getattr(L, name).restype = _SZ
+        for name, args in (
+                ("presto_rope_steps", [freq, _VP, _VP]),
+                ("presto_rope", [rope, _VP, _I32, _VP, _I64, _I64, _I32, _I32, _VP, _VP, _I64, _VP]),
+                ("presto_append_rope", [append, rope] + [_VP] * 13),
+                ("presto_read_kv", [append] + [_VP] * 10),
+                ("presto_quant_attention", [attn, _I32] + [_VP] * 9 + [_SZ, _VP]),
+                ("presto_sample", [_I32, _VP, _I64, _I32, _I64] + [_VP] * 9 + [_SZ, _VP])):
             getattr(L, name).argtypes = args
             getattr(L, name).restype = _I32
         L.presto_status_string.argtypes = [_I32]

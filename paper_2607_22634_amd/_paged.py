@@ -11,7 +11,7 @@ import functools
 
 import torch
 
-from ._lib import PRESTO_DT_BF16, PRESTO_DT_F32, PagedAttnDesc, PagesDesc, _check, _ptr, lib
+from ._lib import PRESTO_DT_BF16, PRESTO_DT_F32, PRESTO_DT_FP4, PagedAttnDesc, PagesDesc, _check, _ptr, lib
 
 
 _I32 = torch.int32
@@ -100,32 +100,39 @@ def _pool(k, v, cols, batch, layers: bool) -> PagesDesc:
 
 @functools.lru_cache(maxsize=64)
 def _pool_of(shape, stride, dtype, batch, cols, layers) -> PagesDesc:
-    """The same from sizes alone (a program has few pools; not to be changed)."""
+    """The same from sizes alone (a program has few pools; not to be changed).
+    Pools of bytes are 4-bit caches [pages, hkv, page / 16, 17 dim / 2]."""
     _one_by_one(*shape, batch, cols)
-    if dtype not in _DT:
+    if dtype not in _DT and dtype is not torch.uint8:
         raise TypeError(f"unsupported dtype {dtype}")
     n_layers, layer_stride = 1, 0
-    if len(shape) == 4:
-        n, page, hkv, d = shape
-        s_page, s_row, s_head, s_dim = stride
-    elif layers and len(shape) == 5:
-        n_layers, n, page, hkv, d = shape
-        layer_stride, s_page, s_row, s_head, s_dim = stride
-    else:
+    if len(shape) == 5 and layers:
+        n_layers, layer_stride, shape, stride = shape[0], stride[0], shape[1:], stride[1:]
+    elif len(shape) != 4:
         raise ValueError("the page pools must be [pages, page, hkv, dim]" + (" or with layers first" if layers else ""))
-    if (s_dim != 1 or s_head != d or s_row != hkv * d) and 0 not in shape:
+    n, n2, n3, n4 = shape
+    s_page, s_2, s_3, s_4 = stride
+    if (s_4 != 1 or s_3 != n4 or s_2 != n3 * n4) and 0 not in shape:
         raise ValueError("a page must be contiguous")
+    if dtype is torch.uint8:
+        hkv, page, d, dt = n2, 16 * n3, n4 * 2 // 17, PRESTO_DT_FP4
+        if d * 17 != n4 * 2:
+            raise ValueError("the last dimension of a 4-bit pool must be 17 dim / 2 bytes")
+        page_units = n2 * n3 * n4
+    else:
+        page, hkv, d, dt = n2, n3, n4, _DT[dtype]
+        page_units = page * hkv * d
     # (the stride of a single page or layer is free: the default, 0)
     if n <= 1:
         s_page = 0
-    elif s_page < page * hkv * d:
+    elif s_page < page_units:
         raise ValueError("pages must not overlap")
     if n_layers == 1:
         layer_stride = 0
-    elif layer_stride < (n - 1) * s_page + page * hkv * d and (
-            layer_stride < page * hkv * d or s_page < (n_layers - 1) * layer_stride + page * hkv * d):
+    elif layer_stride < (n - 1) * s_page + page_units and (
+            layer_stride < page_units or s_page < (n_layers - 1) * layer_stride + page_units):
         raise ValueError("layers must not overlap")  # (they may lie one behind the other or page by page)
-    return PagesDesc(batch, cols, n, page, hkv, d, _DT[dtype], n_layers, s_page, layer_stride)
+    return PagesDesc(batch, cols, n, page, hkv, d, dt, n_layers, s_page, layer_stride)
 
 
 def _books(refs, page_table, page_size) -> PagesDesc:

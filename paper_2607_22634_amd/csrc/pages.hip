@@ -175,7 +175,7 @@ __global__ __launch_bounds__(kPlanThreads) void pages_fork_kernel(
     int32_t* __restrict__ refs, int32_t* __restrict__ table, int32_t* __restrict__ ctx,
     const int32_t* __restrict__ parent, const int32_t* __restrict__ child, int32_t n, int32_t batch,
     int32_t max_pages, int32_t num_pages, int32_t shift, int32_t* list, int32_t* need,
-    int32_t* lens, int32_t* first, Move* __restrict__ moves, int32_t* __restrict__ n_moves,
+    int32_t* lens, int32_t* first, Move* __restrict__ moves, int32_t* __restrict__ n_moves, int32_t whole,
     int32_t* __restrict__ flags) {
     __shared__ int s_wave[kPlanThreads / kWave];
     __shared__ int32_t s_need[kPlanThreads], s_len[kPlanThreads], s_list[kPlanThreads];
@@ -260,7 +260,7 @@ __global__ __launch_bounds__(kPlanThreads) void pages_fork_kernel(
                 const int p = list[at];
                 to[full] = p;
                 refs[p] = 1;
-                moves[at] = {from[full], p, part, 0};
+                moves[at] = {from[full], p, whole ? page : part, 0};  // (a 4-bit page keeps its rows apart by head)
             }
             ctx[child[i]] = len;
         }
@@ -550,12 +550,17 @@ PagesWs pages_ws(void* ws, int64_t num_pages, int64_t n) {
     return w;
 }
 
-int esize(const presto_pages_desc* d) { return d->dt == PRESTO_DT_BF16 ? 2 : 4; }
+// bytes of a unit of the pool's strides, and of one position's row
+int esize(const presto_pages_desc* d) { return d->dt == PRESTO_DT_BF16 ? 2 : d->dt == PRESTO_DT_F32 ? 4 : 1; }
+int64_t row_bytes(const presto_pages_desc* d) {
+    const int64_t n = (int64_t)d->hkv * d->head_dim;
+    return d->dt == PRESTO_DT_FP4 ? n * 17 / 32 : n * esize(d);
+}
 
 template <bool STREAM>
 void launch_move(const presto_pages_desc* d, void* k, void* v, const PagesWs& w, int64_t max_moves,
                  hipStream_t stream) {
-    const int64_t row = (int64_t)d->hkv * d->head_dim * esize(d);
+    const int64_t row = row_bytes(d);
     const int stretches = (int)((row * d->page_size + kMoveBytes - 1) / kMoveBytes);
     // (the number of moves is known to the device only)
     const int64_t units = max_moves * d->layers * 2 * stretches;
@@ -589,7 +594,8 @@ presto_status launch_pages_fork(const presto_pages_desc* d, int32_t* refs, int32
     const PagesWs w = pages_ws(ws, d->num_pages, d->batch);
     pages_fork_kernel<<<1, kPlanThreads, 0, stream>>>(refs, table, ctx, parent, child, n, d->batch, d->max_pages,
                                                       d->num_pages, __builtin_ctz((unsigned)d->page_size), w.list,
-                                                      w.need, w.lens, w.first, w.moves, w.n_moves, flags);
+                                                      w.need, w.lens, w.first, w.moves, w.n_moves,
+                                                      d->dt == PRESTO_DT_FP4, flags);
     launch_move<false>(d, k, v, w, n, stream);
     return check_launch("pages_fork_kernel");
 }

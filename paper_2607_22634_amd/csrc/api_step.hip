@@ -228,8 +228,8 @@ static presto_status check_sample(presto_dtype dt, int64_t rows, int32_t vocab, 
 }
 
 size_t presto_sample_workspace(presto_dtype dt, int64_t rows, int32_t vocab) {
-    check_sample(dt, rows, vocab, "presto_sample_workspace");
-    return 0;
+    if (check_sample(dt, rows, vocab, "presto_sample_workspace") != PRESTO_OK) return 0;
+    return sample_plan(dt, rows, vocab).bytes;
 }
 
 presto_status presto_sample(presto_dtype dt, const void* logits, int64_t rows, int32_t vocab, int64_t row_stride,
@@ -245,10 +245,11 @@ presto_status presto_sample(presto_dtype dt, const void* logits, int64_t rows, i
     if (rows == 0) return PRESTO_OK;
     REQUIRE(logits && u && token, "%s: null pointer", who);
     REQUIRE(((uintptr_t)logits & (dt == PRESTO_DT_BF16 ? 1 : 3)) == 0, "%s: misaligned logits", who);
-    st = check_ws(ws, ws_bytes, presto_sample_workspace(dt, rows, vocab));
+    st = check_ws(ws, ws_bytes, sample_plan(dt, rows, vocab).bytes);
     if (st != PRESTO_OK) return st;
+    REQUIRE(aligned16(ws, nullptr), "%s: the workspace must be 16-byte aligned", who);
     return launch_sample(dt, logits, rows, vocab, row_stride, u, temperature, top_k, top_p, min_p, token, logprob,
-                         flags, stream);
+                         flags, ws, stream);
 }
 
 }  // extern "C"

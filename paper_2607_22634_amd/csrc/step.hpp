@@ -30,8 +30,15 @@ presto_status launch_quant_attn(const presto_paged_attn_desc* d, presto_dtype dt
                                 const int32_t* q_off, const void* k, const void* v, const int32_t* table,
                                 const int32_t* ctx, void* out, int32_t* flags, void* ws, hipStream_t stream);
 
+struct SamplePlan {
+    int64_t rows;  // of a round
+    int slices, slice;  // of a row, and their length
+    size_t bytes;  // workspace
+};
+SamplePlan sample_plan(presto_dtype dt, int64_t rows, int32_t vocab);
 presto_status launch_sample(presto_dtype dt, const void* logits, int64_t rows, int32_t vocab, int64_t row_stride,
                             const float* u, const float* temperature, const int32_t* top_k, const float* top_p,
-                            const float* min_p, int32_t* token, float* logprob, int32_t* flags, hipStream_t stream);
+                            const float* min_p, int32_t* token, float* logprob, int32_t* flags, void* ws,
+                            hipStream_t stream);
 
 }  // namespace presto_host

@@ -96,14 +96,6 @@ __device__ __forceinline__ bool sees(const Args& a, int p, int j) {
     return j <= p && (a.window == 0 || j > p - a.window || j < a.sinks);
 }
 
-// A tile as a lane holds it.
-template <int D>
-struct Tile {
-    static constexpr int W = D / 32;  // words
-    uint32_t kc[2][W], vc[2][W], ve[2];
-    uint32_t ke[2];
-};
-
 template <int D>
 __device__ __forceinline__ void load_words(uint32_t (&w)[D / 32], const char* p) {
     if constexpr (D == 128) {
@@ -119,20 +111,70 @@ __device__ __forceinline__ void load_words(uint32_t (&w)[D / 32], const char* p)
     }
 }
 
+// A lane's offsets in a block.
 template <int D>
-__device__ __forceinline__ void load_tile(Tile<D>& t, const char* k0, const char* v0, const char* k1, const char* v1) {
-    const int n = lane_id() & 15, g = lane_id() >> 4;
-    const int kc = n * (D / 2) + g * (D / 8), ke = 8 * D + n * (D / 32) + g * (D / 4) / 32;
-    const int vc = lane_id() * (D / 8), ve = 8 * D + (g * (D / 32) + n * (D / 16) / 32) * 4;
-    load_words<D>(t.kc[0], k0 + kc);
-    load_words<D>(t.kc[1], k1 + kc);
-    t.ke[0] = (uint8_t)k0[ke];
-    t.ke[1] = (uint8_t)k1[ke];
-    load_words<D>(t.vc[0], v0 + vc);
-    load_words<D>(t.vc[1], v1 + vc);
-    t.ve[0] = *reinterpret_cast<const uint32_t*>(v0 + ve);
-    t.ve[1] = *reinterpret_cast<const uint32_t*>(v1 + ve);
+struct Lane {
+    uint32_t kc, ke, vc, ve;
+    __device__ __forceinline__ Lane() {
+        const uint32_t n = lane_id() & 15, g = lane_id() >> 4;
+        kc = n * (D / 2) + g * (D / 8);
+        ke = 8 * D + n * (D / 32) + g * (D / 4) / 32;
+        vc = lane_id() * (D / 8);
+        ve = 8 * D + (g * (D / 32) + n * (D / 16) / 32) * 4;
+    }
+};
+
+// Loads from global memory to LDS: lane l's bytes land at lds + 16 l (or 4 l),
+// lds the same for the wave (in m0).  From inline assembly, so that the compiler
+// does not put a wait for all of them in front of every LDS read; the kernel
+// waits for a tile itself.
+__device__ __forceinline__ uint64_t scalar(const void* p) {
+    const uint64_t b = (uint64_t)(uintptr_t)p;
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)b);
+    const uint32_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(b >> 32));
+    return (uint64_t)hi << 32 | lo;
 }
+__device__ __forceinline__ void to_lds16(const char* base, uint32_t off, uint32_t lds) {
+    asm volatile("global_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(scalar(base)), "{m0}"(lds) : "memory");
+}
+__device__ __forceinline__ void to_lds16_at(const char* at, uint32_t lds) {
+    asm volatile("global_load_lds_dwordx4 %0, off" ::"v"(at), "{m0}"(lds) : "memory");
+}
+__device__ __forceinline__ void to_lds4(const char* at, uint32_t lds) {
+    asm volatile("global_load_lds_dword %0, off" ::"v"(at), "{m0}"(lds) : "memory");
+}
+template <int N>
+__device__ __forceinline__ void wait_loads() {  // all but the N last ones
+    asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void wait_lds_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+// A tile in LDS: K codes of its blocks, V codes, then the exponents of K's two
+// blocks and of V's.
+template <int D>
+struct Slot {
+    static constexpr int kCodes = 2 * quant::code_bytes(D), kBytes = 2 * kCodes + 256;
+    static constexpr int kLoads = (D == 128 ? 4 : 2) + 1;
+};
+
+// What a lane holds of a tile's K, or of its V: of two blocks the codes, and
+// exponents.
+template <int D>
+struct Half {
+    uint32_t code[2][D / 32], exp[2];
+    __device__ __forceinline__ void load_k(const Lane<D>& at, const char* k0, const char* k1) {
+        load_words<D>(code[0], k0 + at.kc);
+        load_words<D>(code[1], k1 + at.kc);
+        exp[0] = (uint8_t)k0[at.ke];
+        exp[1] = (uint8_t)k1[at.ke];
+    }
+    __device__ __forceinline__ void load_v(const Lane<D>& at, const char* v0, const char* v1) {
+        load_words<D>(code[0], v0 + at.vc);
+        load_words<D>(code[1], v1 + at.vc);
+        exp[0] = *reinterpret_cast<const uint32_t*>(v0 + at.ve);
+        exp[1] = *reinterpret_cast<const uint32_t*>(v1 + at.ve);
+    }
+};
 
 __device__ __forceinline__ bf16x8 eight(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     const u32x4 w = {a, b, c, d};
@@ -161,6 +203,13 @@ __device__ __forceinline__ void split8(float v[8], bf16x8 (&p)[N]) {
     }
 }
 
+// (as one instruction: fmaxf first makes NaN operands quiet)
+__device__ __forceinline__ float max3(float x, float y, float z) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(x), "v"(y), "v"(z));
+    return r;
+}
+
 __device__ __forceinline__ f32x4 mma(const bf16x8& a, const bf16x8& b, const f32x4& c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
 }
@@ -173,15 +222,33 @@ __device__ __forceinline__ uint32_t odd_exps(uint32_t w) {
 }
 __device__ __forceinline__ uint32_t without(uint32_t w, uint32_t odd) { return w & ~((odd >> 7) * 255u); }
 
-// R blocks of 16 query rows per wave; the waves of a workgroup take its tiles
-// in turn.
+// The scale of byte B of w: the conversions read bits 23 .. 30 of it only.
+template <int B>
+__device__ __forceinline__ float scale_of(uint32_t w) {
+    return __uint_as_float(B == 3 ? w >> 1 : w << (23 - 8 * B));
+}
+
+// What a kernel keeps per wave in LDS of queries that do not fit registers.
 template <bool F32, int D, int R>
-__global__ __launch_bounds__(kThreads) void quant_attn_kernel(Args a) {
-    constexpr int NQ = F32 ? 3 : 1, NP = F32 ? 3 : 2;  // bf16 per query value and per probability
-    constexpr int STEPS = D / 32, PER = D / 16, ROWS = 16 * R;
+constexpr bool queries_in_lds() {
+    return !F32 && R > 2;
+}
+
+// R blocks of 16 query rows per wave.  ROWS: each wave has rows of its own and
+// takes all tiles; else the waves of a workgroup share their rows and take the
+// tiles in turn.
+template <bool F32, int D, int R, bool ROWS>
+__global__ __launch_bounds__(kThreads, F32 || R > 1 ? 2 : 4) void quant_attn_kernel(Args a) {
+    constexpr int NQ = F32 ? 3 : 1, NP = F32 ? 3 : ROWS ? 1 : 2;  // bf16 per query value and per probability
+    constexpr int STEPS = D / 32, PER = D / 16, OWN = 16 * R;     // rows of a wave
+    constexpr int ROWS_WG = ROWS ? kWaves * OWN : OWN, STRIDE = ROWS ? 1 : kWaves;
+    constexpr bool LDS_Q = queries_in_lds<F32, D, R>();
     using T = std::conditional_t<F32, float, uint16_t>;
-    __shared__ float s_o[kWaves][ROWS][D + 4];
-    __shared__ float s_m[kWaves][ROWS], s_l[kWaves][ROWS];
+    constexpr int RING = 2;  // tiles on their way per wave
+    constexpr int LDS = ROWS ? 16 : std::max(kWaves * RING * Slot<D>::kBytes, kWaves * OWN * (D + 4) * 4);
+    __shared__ __align__(16) char s_ring[LDS];
+    __shared__ float s_m[kWaves][OWN], s_l[kWaves][OWN];
+    __shared__ bf16x8 s_q[LDS_Q ? kWaves : 1][LDS_Q ? R * STEPS : 1][kWave];
 
     const int lane = lane_id(), n = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -194,16 +261,17 @@ __global__ __launch_bounds__(kThreads) void quant_attn_kernel(Args a) {
 
     const Seq s = sequence(a, b);
     if (s.odd && rb == 0 && split == 0 && head == 0 && threadIdx.x == 0) raise_flag(a.flags, PRESTO_FLAG_BAD_SEQ);
-    const int r0 = rb * ROWS;  // of the sequence's rows (token, head of the group)
+    const int r0 = rb * ROWS_WG + (ROWS ? wave * OWN : 0);  // of the sequence's rows (token, head of the group)
     const int i0 = r0 / a.group;
-    if (i0 >= s.n) return;
-    const int i1 = min((r0 + ROWS - 1) / a.group, s.n - 1);
+    if (i0 >= s.n) return;  // (ROWS: this wave; the waves do not meet)
+    const int i1 = min((r0 + OWN - 1) / a.group, s.n - 1);
     const Tiles t = tiles_of(a, s.first + i0, s.first + i1);
     const int u0 = split * a.split_tiles, u1 = min(u0 + a.split_tiles, t.count);
+    const int u_wave = u0 + (ROWS ? 0 : wave);
 
     // this lane's rows: positions (-1: none) and queries
     int pos[R];
-    bf16x8 qf[R][NQ][STEPS];
+    bf16x8 qf[LDS_Q ? 1 : R][NQ][STEPS];
 #pragma unroll
     for (int j = 0; j < R; ++j) {
         const int r = r0 + 16 * j + n, i = r / a.group;
@@ -220,6 +288,8 @@ __global__ __launch_bounds__(kThreads) void quant_attn_kernel(Args a) {
                 split8<NQ>(v, p);
 #pragma unroll
                 for (int k = 0; k < NQ; ++k) qf[j][k][st] = p[k];
+            } else if constexpr (LDS_Q) {
+                s_q[wave][j * STEPS + st][lane] = *reinterpret_cast<const bf16x8*>(q + 8 * st);
             } else {
                 qf[j][0][st] = *reinterpret_cast<const bf16x8*>(q + 8 * st);
             }
@@ -240,7 +310,7 @@ __global__ __launch_bounds__(kThreads) void quant_attn_kernel(Args a) {
     // the pages of this wave's next 32 tiles, one block of 16 keys per lane
     int pages = -1;
     auto look_up = [&](int first) {
-        const int u = u0 + wave + (first + (lane >> 1)) * kWaves;
+        const int u = u_wave + (first + (lane >> 1)) * STRIDE;
         pages = -1;
         if (u < u1) {
             const int j0 = tile_at(t, u) * kTile + (lane & 1) * 16;
@@ -253,73 +323,139 @@ __global__ __launch_bounds__(kThreads) void quant_attn_kernel(Args a) {
             }
         }
     };
-    const int blocks = 1 << (a.shift - 4);  // of a page
+    const int in_page = (1 << a.shift) - 1;
+    const int64_t head_at = (int64_t)head * ((1 << a.shift) >> 4) * quant::block_bytes(D);
     auto offset = [&](int page, int tile, int half) -> int64_t {
-        const int in_page = ((tile * kTile + half * 16) & ((1 << a.shift) - 1)) >> 4;
-        return max(page, 0) * a.page_bytes + ((int64_t)head * blocks + in_page) * quant::block_bytes(D);
+        return max(page, 0) * a.page_bytes + head_at +
+               (((tile * kTile + half * 16) & in_page) >> 4) * quant::block_bytes(D);
     };
     struct Where {
         int tile, p0, p1;
     };
     auto where = [&](int it) {
         Where w;
-        w.tile = tile_at(t, u0 + wave + it * kWaves);
+        w.tile = tile_at(t, u_wave + it * STRIDE);
         w.p0 = __builtin_amdgcn_readlane(pages, 2 * (it & 31));
         w.p1 = __builtin_amdgcn_readlane(pages, 2 * (it & 31) + 1);
         return w;
     };
-    auto fetch = [&](Tile<D>& tl, const Where& w) {
-        const int64_t f0 = offset(w.p0, w.tile, 0), f1 = offset(w.p1, w.tile, 1);
-        load_tile<D>(tl, a.k + f0, a.v + f0, a.k + f1, a.v + f1);
-    };
+    const Lane<D> at;
+    const int mine = u1 > u_wave ? (u1 - u_wave + STRIDE - 1) / STRIDE : 0;
 
-    const int mine = u1 > u0 + wave ? (u1 - u0 - wave + kWaves - 1) / kWaves : 0;
-    Tile<D> next;
-    Where w_next;
-    if (mine > 0) {
-        look_up(0);
-        w_next = where(0);
-        fetch(next, w_next);
+    // ROWS: the next tile's K is asked for when this one's is used up, its V
+    // likewise: one set of registers, and what is on its way has the rest of the
+    // step.  Else, where memory is what counts, tiles come through LDS, two ahead:
+    // a lane's registers could not hold as much.
+    Half<D> tk, tv;
+    Where w, w_next, w_then;
+    int64_t f0 = 0, f1 = 0;
+    auto next = [&](int it) {
+        if ((it & 31) == 0) look_up(it);
+        w_next = where(it);
+        f0 = offset(w_next.p0, w_next.tile, 0);
+        f1 = offset(w_next.p1, w_next.tile, 1);
+        tk.load_k(at, a.k + f0, a.k + f1);
+    };
+    char* ring = s_ring + wave * RING * Slot<D>::kBytes;
+    const uint32_t ring_at = (uint32_t)__builtin_amdgcn_readfirstlane(
+        (int)(uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)ring);
+    auto send = [&](int it) {  // tile `it` on its way
+        if ((it & 31) == 0) look_up(it);
+        w_then = where(it);
+        const char *k0 = a.k, *v0 = a.v, *k1 = a.k, *v1 = a.v;
+        const int64_t o0 = offset(w_then.p0, w_then.tile, 0), o1 = offset(w_then.p1, w_then.tile, 1);
+        k0 += o0, v0 += o0, k1 += o1, v1 += o1;
+        const uint32_t lds = ring_at + (it & 1) * Slot<D>::kBytes;
+        constexpr int CODES = quant::code_bytes(D);
+        if constexpr (D == 128) {  // (a lane's own piece of K in its own place)
+            to_lds16(k0, at.kc, lds);
+            to_lds16(k1, at.kc, lds + CODES);
+            to_lds16(v0, at.vc, lds + 2 * CODES);
+            to_lds16(v1, at.vc, lds + 3 * CODES);
+        } else {
+            const char *k = lane < 32 ? k0 : k1, *v = lane < 32 ? v0 : v1;
+            to_lds16_at(k + (lane & 31) * 16, lds);
+            to_lds16_at(v + (lane & 31) * 16, lds + 2 * CODES);
+        }
+        const char *e0 = lane < 16 ? k0 : k1, *e1 = lane < 48 ? v0 : v1;
+        to_lds4((lane < 32 ? e0 : e1) + CODES + (lane & (D / 8 - 1)) * 4, lds + 4 * CODES);
+    };
+    auto take = [&](int it) {
+        const char* p = ring + (it & 1) * Slot<D>::kBytes;
+        constexpr int CODES = quant::code_bytes(D);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            load_words<D>(tk.code[h], p + h * CODES + (D == 128 ? lane * 16u : at.kc));
+            load_words<D>(tv.code[h], p + (2 + h) * CODES + at.vc);
+            tk.exp[h] = (uint8_t)p[4 * CODES + h * 64 + at.ke - 8 * D];
+            tv.exp[h] = *reinterpret_cast<const uint32_t*>(p + 4 * CODES + 128 + h * 64 + at.ve - 8 * D);
+        }
+    };
+    if constexpr (ROWS) {
+        if (mine > 0) {
+            next(0);
+            tv.load_v(at, a.v + f0, a.v + f1);
+        }
+    } else {
+        if (mine > 0) send(0);
+        w_next = w_then;
+        if (mine > 1) send(1);
     }
     for (int it = 0; it < mine; ++it) {
-        const Tile<D> cur = next;
-        const Where w = w_next;
-        if (it + 1 < mine) {
-            if (((it + 1) & 31) == 0) look_up(it + 1);
-            w_next = where(it + 1);
-            fetch(next, w_next);
+        w = w_next;
+        if constexpr (!ROWS) {
+            w_next = w_then;
+            if (it + 1 < mine)
+                wait_loads<Slot<D>::kLoads>();
+            else
+                wait_loads<0>();
+            take(it);
+            wait_lds_reads();
+            if (it + 2 < mine) send(it + 2);
         }
         const int j0 = w.tile * kTile;
         const bool whole = j0 + kTile - 1 <= t.pmin &&
                            (a.window == 0 || j0 > t.pmax - a.window || j0 + kTile - 1 < a.sinks) && w.p0 >= 0 &&
                            w.p1 >= 0;
-
         // scores
         f32x4 sc[R][2];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const float ks = quant::exp_scale(cur.ke[h]);
+        for (int j = 0; j < R; ++j) sc[j][0] = sc[j][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+        const float ks[2] = {scale_of<0>(tk.exp[0]), scale_of<0>(tk.exp[1])};
 #pragma unroll
-            for (int j = 0; j < R; ++j) sc[j][h] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int st = 0; st < STEPS; ++st) {
+            bf16x8 kf[2];
 #pragma unroll
-            for (int st = 0; st < STEPS; ++st) {
-                const uint32_t c = cur.kc[h][st];
-                const bf16x8 kf = eight(quant::decode2<0>(c, ks), quant::decode2<1>(c, ks), quant::decode2<2>(c, ks),
-                                        quant::decode2<3>(c, ks));
-#pragma unroll
-                for (int k = NQ - 1; k >= 0; --k)
-#pragma unroll
-                    for (int j = 0; j < R; ++j) sc[j][h] = mma(kf, qf[j][k][st], sc[j][h]);
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t c = tk.code[h][st];
+                kf[h] = eight(quant::decode2<0>(c, ks[h]), quant::decode2<1>(c, ks[h]), quant::decode2<2>(c, ks[h]),
+                              quant::decode2<3>(c, ks[h]));
             }
+#pragma unroll
+            for (int j = 0; j < R; ++j)
+#pragma unroll
+                for (int k = NQ - 1; k >= 0; --k) {
+                    bf16x8 q;
+                    if constexpr (LDS_Q)
+                        q = s_q[wave][j * STEPS + st][lane];
+                    else
+                        q = qf[j][k][st];
+                    sc[j][0] = mma(kf[0], q, sc[j][0]);
+                    sc[j][1] = mma(kf[1], q, sc[j][1]);
+                }
         }
 
-        // probabilities: x = s c - m
+        __builtin_amdgcn_sched_barrier(0);
+        if (ROWS && it + 1 < mine) next(it + 1);
+
+        // probabilities 2^x, x = s c - m: m is a row's largest score so far, or up
+        // to kSlack below it
         bf16x8 p[R][NP];
 #pragma unroll
         for (int j = 0; j < R; ++j) {
             float z[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) z[i] = sc[j][i >> 2][i & 3] * a.scale;
+            for (int i = 0; i < 8; ++i) z[i] = sc[j][i >> 2][i & 3];
             if (!whole) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
@@ -327,16 +463,14 @@ __global__ __launch_bounds__(kThreads) void quant_attn_kernel(Args a) {
                     if (!(sees(a, pos[j], key) && (i < 4 ? w.p0 : w.p1) >= 0)) z[i] = -INFINITY;
                 }
             }
-            float top = z[0];
-#pragma unroll
-            for (int i = 1; i < 8; ++i) top = fmaxf(top, z[i]);
             // (NaN scores take no part in the maximum and reach l through exp2)
-            const bool unset = m[j] == -INFINITY;
-            if (__any(unset ? top > -INFINITY : top > m[j] + kSlack)) {
+            const float top3 = max3(max3(z[0], z[1], z[2]), max3(z[3], z[4], z[5]), max3(z[6], z[7], z[7]));
+            float top = top3 * a.scale;
+            if (__any(top > m[j] + kSlack)) {
                 top = fmaxf(top, __shfl_xor(top, 16));
                 top = fmaxf(top, __shfl_xor(top, 32));
                 if (top > m[j]) {
-                    const float f = unset ? 0.f : __builtin_amdgcn_exp2f(m[j] - top);
+                    const float f = __builtin_amdgcn_exp2f(m[j] - top);  // (0 where there was no key)
                     m[j] = top;
                     l[j] *= f;
 #pragma unroll
@@ -345,15 +479,15 @@ __global__ __launch_bounds__(kThreads) void quant_attn_kernel(Args a) {
             }
             const float ref = m[j] == -INFINITY ? 0.f : m[j];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                z[i] = __builtin_amdgcn_exp2f(z[i] - ref);
-                l[j] += z[i];
-            }
+            for (int i = 0; i < 8; ++i) z[i] = __builtin_amdgcn_exp2f(fmaf(z[i], a.scale, -ref));
+            l[j] += ((z[0] + z[1]) + (z[2] + z[3])) + ((z[4] + z[5]) + (z[6] + z[7]));
             split8<NP>(z, p[j]);
+            if (R > 2) __builtin_amdgcn_sched_barrier(0);
         }
+        __builtin_amdgcn_sched_barrier(0);
 
         // values
-        uint32_t ve[2] = {cur.ve[0], cur.ve[1]};
+        uint32_t ve[2] = {tv.exp[0], tv.exp[1]};
         if (!whole) {  // keys that no row sees may be anything
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -362,22 +496,22 @@ __global__ __launch_bounds__(kThreads) void quant_attn_kernel(Args a) {
                 if (!seen) ve[i >> 2] &= ~(255u << (8 * (i & 3)));
             }
         }
-        if (__any(odd_exps(ve[0]) | odd_exps(ve[1]))) {
+        // (bytes above kMostExp are above 127, which few are)
+        if (__any((ve[0] | ve[1]) & 0x80808080u) && __any(odd_exps(ve[0]) | odd_exps(ve[1]))) {
             odd_v = true;
             ve[0] = without(ve[0], odd_exps(ve[0]));
             ve[1] = without(ve[1], odd_exps(ve[1]));
         }
-        float vs[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) vs[i] = quant::exp_scale((ve[i >> 2] >> (8 * (i & 3))) & 255);
+        const float vs[8] = {scale_of<0>(ve[0]), scale_of<1>(ve[0]), scale_of<2>(ve[0]), scale_of<3>(ve[0]),
+                             scale_of<0>(ve[1]), scale_of<1>(ve[1]), scale_of<2>(ve[1]), scale_of<3>(ve[1])};
         auto pv = [&](auto B) {  // dims 2 B and 2 B + 1 of the lane's
             uint32_t c[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 if constexpr (D == 128) {
-                    c[i] = quant::decode2<B()>(cur.vc[i >> 2][i & 3], vs[i]);
+                    c[i] = quant::decode2<B()>(tv.code[i >> 2][i & 3], vs[i]);
                 } else {
-                    const uint32_t word = cur.vc[i >> 2][(i & 3) >> 1];
+                    const uint32_t word = tv.code[i >> 2][(i & 3) >> 1];
                     c[i] = (i & 1) ? quant::decode2<2 + B()>(word, vs[i]) : quant::decode2<B()>(word, vs[i]);
                 }
             }
@@ -402,6 +536,8 @@ __global__ __launch_bounds__(kThreads) void quant_attn_kernel(Args a) {
             pv(std::integral_constant<int, 2>{});
             pv(std::integral_constant<int, 3>{});
         }
+        __builtin_amdgcn_sched_barrier(0);
+        if (ROWS && it + 1 < mine) tv.load_v(at, a.v + f0, a.v + f1);
     }
 
     // A group of V that is not finite took part as zeros: now the rows that see
@@ -430,41 +566,20 @@ __global__ __launch_bounds__(kThreads) void quant_attn_kernel(Args a) {
                 for (int d = 0; d < PER; ++d) o[j][d] = f32x4{NAN, NAN, NAN, NAN};
             }
     }
-
-    // the waves' states, joined
 #pragma unroll
     for (int j = 0; j < R; ++j) {
         l[j] += __shfl_xor(l[j], 16);
         l[j] += __shfl_xor(l[j], 32);
-        if (g == 0) {
-            s_m[wave][16 * j + n] = m[j];
-            s_l[wave][16 * j + n] = l[j];
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int d = 0; d < PER; d += 4)
-                *reinterpret_cast<float4*>(&s_o[wave][16 * j + n][PER * (4 * g + i) + d]) =
-                    make_float4(o[j][d][i], o[j][d + 1][i], o[j][d + 2][i], o[j][d + 3][i]);
     }
-    __syncthreads();
-    constexpr int PIECES = D / 8;
-    for (int e = threadIdx.x; e < ROWS * PIECES; e += kThreads) {
-        const int r = e / PIECES, x0 = e % PIECES * 8, i = (r0 + r) / a.group;
-        if (i >= s.n) continue;
-        float top = -INFINITY, sum = 0.f, v[8] = {};
-        for (int w = 0; w < kWaves; ++w) top = fmaxf(top, s_m[w][r]);
-        for (int w = 0; w < kWaves; ++w) {
-            if (s_m[w][r] == -INFINITY && s_l[w][r] == 0.f) continue;  // (no key)
-            const float f = __builtin_amdgcn_exp2f(s_m[w][r] - (top == -INFINITY ? 0.f : top));
-            sum += f * s_l[w][r];
-            for (int d = 0; d < 8; ++d) v[d] += f * s_o[w][r][x0 + d];
-        }
-        const int64_t row = (s.row + i) * a.hkv * a.group + (int64_t)head * a.group + (r0 + r) % a.group;
+
+    // Eight values of a row (of the sequence's) from dim x0 on: as part of the
+    // row, or as its output.
+    auto put = [&](int r, int x0, const float (&v)[8], float top, float sum) {
+        const int64_t row = (s.row + r / a.group) * a.hkv * a.group + (int64_t)head * a.group + r % a.group;
         if (a.splits > 1) {
-            const int64_t at = row * a.splits + split;
-            if (x0 == 0) a.part_ml[at] = make_float2(top, sum);
-            float4* to = reinterpret_cast<float4*>(a.part_o + at * D + x0);
+            const int64_t part = row * a.splits + split;
+            if (x0 == 0) a.part_ml[part] = make_float2(top, sum);
+            float4* to = reinterpret_cast<float4*>(a.part_o + part * D + x0);
             to[0] = make_float4(v[0], v[1], v[2], v[3]);
             to[1] = make_float4(v[4], v[5], v[6], v[7]);
         } else {
@@ -478,6 +593,57 @@ __global__ __launch_bounds__(kThreads) void quant_attn_kernel(Args a) {
                     make_uint4(pack2(v[0] * f, v[1] * f), pack2(v[2] * f, v[3] * f), pack2(v[4] * f, v[5] * f),
                                pack2(v[6] * f, v[7] * f));
             }
+        }
+    };
+
+    if constexpr (ROWS) {
+        // a lane holds PER dims of each of 4 g .. 4 g + 3: D / 4 in one piece
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            const int r = r0 + 16 * j + n;
+            if (r / a.group >= s.n) continue;
+#pragma unroll
+            for (int e = 0; e < D / 4; e += 8) {
+                float v[8];
+#pragma unroll
+                for (int d = 0; d < 8; ++d) v[d] = o[j][(e + d) % PER][(e + d) / PER];
+                put(r, g * (D / 4) + e, v, m[j], l[j]);
+            }
+        }
+    } else {
+        // the waves' states, joined (in the ring's place, when all are through it)
+        float(*s_o)[OWN][D + 4] = reinterpret_cast<float(*)[OWN][D + 4]>(s_ring);
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            if (g == 0) {
+                s_m[wave][16 * j + n] = m[j];
+                s_l[wave][16 * j + n] = l[j];
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int d = 0; d < PER; d += 4)
+                    *reinterpret_cast<float4*>(&s_o[wave][16 * j + n][PER * (4 * g + i) + d]) =
+                        make_float4(o[j][d][i], o[j][d + 1][i], o[j][d + 2][i], o[j][d + 3][i]);
+        }
+        __syncthreads();
+        constexpr int PIECES = D / 8;
+        for (int e = threadIdx.x; e < OWN * PIECES; e += kThreads) {
+            const int r = e / PIECES, x0 = e % PIECES * 8;
+            if ((r0 + r) / a.group >= s.n) continue;
+            float top = -INFINITY, sum = 0.f, v[8] = {};
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) top = fmaxf(top, s_m[w][r]);
+#pragma unroll
+            for (int w = 0; w < kWaves; ++w) {
+                if (s_m[w][r] == -INFINITY && s_l[w][r] == 0.f) continue;  // (no key)
+                const float f = __builtin_amdgcn_exp2f(s_m[w][r] - (top == -INFINITY ? 0.f : top));
+                sum += f * s_l[w][r];
+#pragma unroll
+                for (int d = 0; d < 8; ++d) v[d] += f * s_o[w][r][x0 + d];
+            }
+            put(r0 + r, x0, v, top, sum);
         }
     }
 }
@@ -532,19 +698,23 @@ using namespace presto::qattn;
 QuantPlan quant_plan(const presto_paged_attn_desc* d, presto_dtype dt) {
     QuantPlan p{};
     const int64_t group = d->hq / d->pages.hkv, rows = (int64_t)d->max_q * group;
-    p.r = rows > 16 && dt == PRESTO_DT_BF16 ? 2 : 1;
-    p.row_blocks = (rows + 16 * p.r - 1) / (16 * p.r);
+    const bool f32 = dt == PRESTO_DT_F32;
+    p.own = !f32 && rows >= 256;
+    p.r = f32 ? 1 : p.own ? 4 : rows > 16 ? 2 : 1;
+    const int64_t of_group = p.own ? 16 * p.r * kWaves : 16 * p.r;
+    p.row_blocks = (rows + of_group - 1) / of_group;
     // the tiles of a row block: the longest, and on average
     int64_t most = ((int64_t)d->max_ctx + kTile - 1) / kTile;
-    const int64_t span = 16 * p.r / group + 2;  // tokens of a row block
+    const int64_t span = 16 * p.r / group + 2;  // tokens of a wave
     if (d->window)
         most = std::min(most, ((int64_t)d->window + span) / kTile + 2 + ((int64_t)d->sinks + kTile - 1) / kTile);
     most = std::max<int64_t>(most, 1);
     const int64_t blocks = (int64_t)d->pages.batch * p.row_blocks * d->pages.hkv;
     int64_t mean = most;
     if (d->total_ctx > 0) mean = std::min(most, d->total_ctx / d->pages.batch / kTile + 1);
-    constexpr int64_t kTarget = 1024, kLeast = 16, kMostSplits = 256;
-    int64_t tiles = std::max(kLeast, (blocks * mean + kTarget - 1) / kTarget);
+    const int64_t target = p.own ? 512 : 1024;
+    constexpr int64_t kLeast = 16, kMostSplits = 256;
+    int64_t tiles = std::max(kLeast, (blocks * mean + target - 1) / target);
     tiles = std::max(tiles, (most + kMostSplits - 1) / kMostSplits);
     p.splits = (most + tiles - 1) / tiles;
     p.split_tiles = (most + p.splits - 1) / p.splits;
@@ -592,10 +762,13 @@ presto_status launch_quant_attn(const presto_paged_attn_desc* d, presto_dtype dt
     a.split_tiles = (int)p.split_tiles;
     a.scale = d->scale * 1.4426950408889634f;
     auto run = [&](auto f32, auto dim) {
-        if (p.r == 2)
-            quant_attn_kernel<f32(), dim(), f32() ? 1 : 2><<<(unsigned)p.blocks, kThreads, 0, stream>>>(a);
+        const unsigned grid = (unsigned)p.blocks;
+        if (p.own)
+            quant_attn_kernel<f32(), dim(), f32() ? 1 : 4, !f32()><<<grid, kThreads, 0, stream>>>(a);
+        else if (p.r == 2)
+            quant_attn_kernel<f32(), dim(), f32() ? 1 : 2, false><<<grid, kThreads, 0, stream>>>(a);
         else
-            quant_attn_kernel<f32(), dim(), 1><<<(unsigned)p.blocks, kThreads, 0, stream>>>(a);
+            quant_attn_kernel<f32(), dim(), 1, false><<<grid, kThreads, 0, stream>>>(a);
         if (p.splits > 1) quant_merge_kernel<f32(), dim()><<<(unsigned)p.merge_blocks, kThreads, 0, stream>>>(a);
     };
     auto with = [&](auto f32) {

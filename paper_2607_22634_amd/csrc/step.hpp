@@ -21,6 +21,7 @@ presto_status launch_read_kv(const presto_append_desc* d, const void* k_pages, c
 
 struct QuantPlan {
     bool fits;  // false: more workgroups than a grid holds
+    bool own;   // waves have rows of their own, and do not share the tiles of the same ones
     int r;      // 16-row blocks of a wave
     int64_t row_blocks, splits, split_tiles, blocks, merge_blocks;
     size_t o_bytes, bytes;  // workspace

@@ -127,21 +127,15 @@ struct Lane {
 // Loads from global memory to LDS: lane l's bytes land at lds + 16 l (or 4 l),
 // lds the same for the wave (in m0).  From inline assembly, so that the compiler
 // does not put a wait for all of them in front of every LDS read; the kernel
-// waits for a tile itself.
-__device__ __forceinline__ uint64_t scalar(const void* p) {
-    const uint64_t b = (uint64_t)(uintptr_t)p;
-    const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)b);
-    const uint32_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(b >> 32));
-    return (uint64_t)hi << 32 | lo;
-}
-__device__ __forceinline__ void to_lds16(const char* base, uint32_t off, uint32_t lds) {
-    asm volatile("global_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(scalar(base)), "{m0}"(lds) : "memory");
-}
-__device__ __forceinline__ void to_lds16_at(const char* at, uint32_t lds) {
-    asm volatile("global_load_lds_dwordx4 %0, off" ::"v"(at), "{m0}"(lds) : "memory");
+// waits for a tile itself.  The hardware wants a wait state between m0's write
+// and the load, which the compiler does not put in front of assembly (nor the
+// five that an address in scalar registers would need after a v_readfirstlane:
+// the addresses here are in vector registers).
+__device__ __forceinline__ void to_lds16(const char* at, uint32_t lds) {
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(at), "{m0}"(lds) : "memory");
 }
 __device__ __forceinline__ void to_lds4(const char* at, uint32_t lds) {
-    asm volatile("global_load_lds_dword %0, off" ::"v"(at), "{m0}"(lds) : "memory");
+    asm volatile("s_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(at), "{m0}"(lds) : "memory");
 }
 template <int N>
 __device__ __forceinline__ void wait_loads() {  // all but the N last ones
@@ -203,12 +197,9 @@ __device__ __forceinline__ void split8(float v[8], bf16x8 (&p)[N]) {
     }
 }
 
-// (as one instruction: fmaxf first makes NaN operands quiet)
-__device__ __forceinline__ float max3(float x, float y, float z) {
-    float r;
-    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(x), "v"(y), "v"(z));
-    return r;
-}
+// The larger one, as one instruction: fmaxf first makes NaN operands quiet.  (Of
+// a number and a NaN the number, of two NaN infinity.)
+__device__ __forceinline__ float larger(float x, float y) { return __builtin_amdgcn_fmed3f(x, y, INFINITY); }
 
 __device__ __forceinline__ f32x4 mma(const bf16x8& a, const bf16x8& b, const f32x4& c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
@@ -368,14 +359,14 @@ __global__ __launch_bounds__(kThreads, F32 || R > 1 ? 2 : 4) void quant_attn_ker
         const uint32_t lds = ring_at + (it & 1) * Slot<D>::kBytes;
         constexpr int CODES = quant::code_bytes(D);
         if constexpr (D == 128) {  // (a lane's own piece of K in its own place)
-            to_lds16(k0, at.kc, lds);
-            to_lds16(k1, at.kc, lds + CODES);
-            to_lds16(v0, at.vc, lds + 2 * CODES);
-            to_lds16(v1, at.vc, lds + 3 * CODES);
+            to_lds16(k0 + at.kc, lds);
+            to_lds16(k1 + at.kc, lds + CODES);
+            to_lds16(v0 + at.vc, lds + 2 * CODES);
+            to_lds16(v1 + at.vc, lds + 3 * CODES);
         } else {
             const char *k = lane < 32 ? k0 : k1, *v = lane < 32 ? v0 : v1;
-            to_lds16_at(k + (lane & 31) * 16, lds);
-            to_lds16_at(v + (lane & 31) * 16, lds + 2 * CODES);
+            to_lds16(k + (lane & 31) * 16, lds);
+            to_lds16(v + (lane & 31) * 16, lds + 2 * CODES);
         }
         const char *e0 = lane < 16 ? k0 : k1, *e1 = lane < 48 ? v0 : v1;
         to_lds4((lane < 32 ? e0 : e1) + CODES + (lane & (D / 8 - 1)) * 4, lds + 4 * CODES);
@@ -463,9 +454,10 @@ __global__ __launch_bounds__(kThreads, F32 || R > 1 ? 2 : 4) void quant_attn_ker
                     if (!(sees(a, pos[j], key) && (i < 4 ? w.p0 : w.p1) >= 0)) z[i] = -INFINITY;
                 }
             }
-            // (NaN scores take no part in the maximum and reach l through exp2)
-            const float top3 = max3(max3(z[0], z[1], z[2]), max3(z[3], z[4], z[5]), max3(z[6], z[7], z[7]));
-            float top = top3 * a.scale;
+            // (a NaN score reaches l through exp2, whatever m is)
+            float top = larger(larger(larger(z[0], z[1]), larger(z[2], z[3])),
+                               larger(larger(z[4], z[5]), larger(z[6], z[7]))) *
+                        a.scale;
             if (__any(top > m[j] + kSlack)) {
                 top = fmaxf(top, __shfl_xor(top, 16));
                 top = fmaxf(top, __shfl_xor(top, 32));

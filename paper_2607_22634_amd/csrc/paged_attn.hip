@@ -827,10 +827,12 @@ constexpr int kTilePages = 4096;  // page numbers in LDS
 
 // 16 bytes per lane from memory to LDS: lane l's land at lds + 16 l.  In inline
 // assembly, because the compiler would put a wait for all loads before every
-// later LDS read; the kernel waits for each tile itself.
+// later LDS read; the kernel waits for each tile itself.  (s_nop: a load to LDS
+// wants a wait state after m0 is written, which the compiler does not put in
+// front of assembly.)
 __device__ __forceinline__ void lds_load16(const void* lane_ptr, uint32_t lds) {
     const uint32_t m0v = (uint32_t)__builtin_amdgcn_readfirstlane(lds);
-    asm volatile("global_load_lds_dwordx4 %0, off" ::"v"(lane_ptr), "{m0}"(m0v) : "memory");
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(lane_ptr), "{m0}"(m0v) : "memory");
 }
 // the same with a wave-uniform base and a 32-bit offset per lane
 __device__ __forceinline__ void lds_load16(const void* base, uint32_t off, uint32_t lds) {
@@ -839,7 +841,7 @@ __device__ __forceinline__ void lds_load16(const void* base, uint32_t off, uint3
     const uint32_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(b >> 32));
     const uint64_t sb = ((uint64_t)hi << 32) | (uint64_t)lo;
     const uint32_t m0v = (uint32_t)__builtin_amdgcn_readfirstlane(lds);
-    asm volatile("global_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(sb), "{m0}"(m0v) : "memory");
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(sb), "{m0}"(m0v) : "memory");
 }
 
 // A barrier for what is in LDS: loads and stores of global memory stay on their

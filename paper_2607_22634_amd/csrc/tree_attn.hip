@@ -156,9 +156,10 @@ __device__ __forceinline__ int xcd_task(int bid, int n_blocks) {
 // instruction is issued from inline assembly so that the compiler does not
 // guard every later LDS read with a wait for all outstanding loads; the
 // kernel waits for each tile itself (vmcnt) before the barrier that
-// publishes it.
+// publishes it.  (s_nop: a load to LDS wants a wait state after m0 is written,
+// which the compiler does not put in front of assembly.)
 __device__ __forceinline__ void lds_load16(const void* gptr, uint32_t lds) {
-    asm volatile("global_load_lds_dwordx4 %0, off" ::"v"(gptr), "{m0}"(lds) : "memory");
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(gptr), "{m0}"(lds) : "memory");
 }
 // the same with a wave-uniform base and a per-lane 32-bit byte offset (the
 // base and the LDS address are read from the first lane, so that they are
@@ -171,7 +172,7 @@ __device__ __forceinline__ void lds_load16(const void* base, uint32_t off, uint3
     const uint32_t hi = (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(b >> 32));
     const uint64_t sb = ((uint64_t)hi << 32) | (uint64_t)lo;
     const uint32_t m0v = (uint32_t)__builtin_amdgcn_readfirstlane(lds);
-    asm volatile("global_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(sb), "{m0}"(m0v) : "memory");
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(off), "s"(sb), "{m0}"(m0v) : "memory");
 }
 
 template <int D>

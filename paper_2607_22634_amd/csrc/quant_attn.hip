@@ -131,11 +131,20 @@ struct Lane {
 // and the load, which the compiler does not put in front of assembly (nor the
 // five that an address in scalar registers would need after a v_readfirstlane:
 // the addresses here are in vector registers).
+// ONCE: past the caches.
+template <bool ONCE>
 __device__ __forceinline__ void to_lds16(const char* at, uint32_t lds) {
-    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(at), "{m0}"(lds) : "memory");
+    if constexpr (ONCE)
+        asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off nt" ::"v"(at), "{m0}"(lds) : "memory");
+    else
+        asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(at), "{m0}"(lds) : "memory");
 }
+template <bool ONCE>
 __device__ __forceinline__ void to_lds4(const char* at, uint32_t lds) {
-    asm volatile("s_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(at), "{m0}"(lds) : "memory");
+    if constexpr (ONCE)
+        asm volatile("s_nop 0\n\tglobal_load_lds_dword %0, off nt" ::"v"(at), "{m0}"(lds) : "memory");
+    else
+        asm volatile("s_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(at), "{m0}"(lds) : "memory");
 }
 template <int N>
 __device__ __forceinline__ void wait_loads() {  // all but the N last ones
@@ -197,9 +206,9 @@ __device__ __forceinline__ void split8(float v[8], bf16x8 (&p)[N]) {
     }
 }
 
-// The larger one, as one instruction: fmaxf first makes NaN operands quiet.  (Of
-// a number and a NaN the number, of two NaN infinity.)
-__device__ __forceinline__ float larger(float x, float y) { return __builtin_amdgcn_fmed3f(x, y, INFINITY); }
+// The larger one of two below the largest number, as one instruction: fmaxf
+// first makes NaN operands quiet.  (Of a number and a NaN the number.)
+__device__ __forceinline__ float larger(float x, float y) { return __builtin_amdgcn_fmed3f(x, y, 3.402823466e38f); }
 
 __device__ __forceinline__ f32x4 mma(const bf16x8& a, const bf16x8& b, const f32x4& c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
@@ -225,42 +234,59 @@ constexpr bool queries_in_lds() {
     return !F32 && R > 2;
 }
 
-// R blocks of 16 query rows per wave.  ROWS: each wave has rows of its own and
-// takes all tiles; else the waves of a workgroup share their rows and take the
-// tiles in turn.
+// R blocks of 16 query rows per wave.  The waves of a workgroup share their rows
+// and take the tiles in turn; ROWS: two by two of them, on two sets of rows.
 template <bool F32, int D, int R, bool ROWS>
 __global__ __launch_bounds__(kThreads, F32 || R > 1 ? 2 : 4) void quant_attn_kernel(Args a) {
     constexpr int NQ = F32 ? 3 : 1, NP = F32 ? 3 : ROWS ? 1 : 2;  // bf16 per query value and per probability
     constexpr int STEPS = D / 32, PER = D / 16, OWN = 16 * R;     // rows of a wave
-    constexpr int ROWS_WG = ROWS ? kWaves * OWN : OWN, STRIDE = ROWS ? 1 : kWaves;
+    constexpr int SETS = ROWS ? 2 : 1, STRIDE = kWaves / SETS;    // of rows; waves on each
     constexpr bool LDS_Q = queries_in_lds<F32, D, R>();
     using T = std::conditional_t<F32, float, uint16_t>;
-    constexpr int RING = 2;  // tiles on their way per wave
-    constexpr int LDS = ROWS ? 16 : std::max(kWaves * RING * Slot<D>::kBytes, kWaves * OWN * (D + 4) * 4);
-    __shared__ __align__(16) char s_ring[LDS];
-    __shared__ float s_m[kWaves][OWN], s_l[kWaves][OWN];
-    __shared__ bf16x8 s_q[LDS_Q ? kWaves : 1][LDS_Q ? R * STEPS : 1][kWave];
+    constexpr int RING = 2;       // tiles on their way per wave
+    constexpr bool ONCE = R == 1;  // (with one row block nobody else reads them)
+    constexpr int LDS = std::max(ROWS ? SETS * R * STEPS * kWave * 16 : kWaves * RING * Slot<D>::kBytes,
+                                 kWaves * 16 * (D + 4) * 4);
+    __shared__ __align__(16) char s_mem[LDS];
+    __shared__ float s_m[kWaves][16], s_l[kWaves][16];
 
     const int lane = lane_id(), n = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-    int x = blockIdx.x;
-    const int head = x % a.hkv;
-    x /= a.hkv;
-    const int split = x % a.splits;
-    x /= a.splits;
-    const int rb = x % a.row_blocks, b = x / a.row_blocks;
+    const int set = wave % SETS;
+    // blocks go round the eight XCDs.  ROWS: those of one head, which share its
+    // keys, to one of them where there are eight heads; else the heads of a
+    // stretch of positions, which lie side by side in the pool
+    int x = blockIdx.x, head, split, rb, b;
+    if constexpr (ROWS) {
+        head = x % a.hkv;
+        x /= a.hkv;
+        split = x % a.splits;
+        x /= a.splits;
+        rb = x % a.row_blocks;
+        b = x / a.row_blocks;
+    } else {
+        const int xcd = x % 8;
+        x /= 8;
+        rb = x % a.row_blocks;
+        x /= a.row_blocks;
+        head = x % a.hkv;
+        const int unit = x / a.hkv * 8 + xcd;
+        split = unit % a.splits;
+        b = unit / a.splits;
+        if (b >= a.batch) return;
+    }
 
     const Seq s = sequence(a, b);
     if (s.odd && rb == 0 && split == 0 && head == 0 && threadIdx.x == 0) raise_flag(a.flags, PRESTO_FLAG_BAD_SEQ);
-    const int r0 = rb * ROWS_WG + (ROWS ? wave * OWN : 0);  // of the sequence's rows (token, head of the group)
-    const int i0 = r0 / a.group;
-    if (i0 >= s.n) return;  // (ROWS: this wave; the waves do not meet)
-    const int i1 = min((r0 + OWN - 1) / a.group, s.n - 1);
+    const int r0 = (rb * SETS + set) * OWN;  // of the sequence's rows (token, head of the group)
+    if (rb * SETS * OWN / a.group >= s.n) return;
+    const int i0 = r0 / a.group, i1 = min((r0 + OWN - 1) / a.group, s.n - 1);  // (i0 > i1: a set without rows)
     const Tiles t = tiles_of(a, s.first + i0, s.first + i1);
-    const int u0 = split * a.split_tiles, u1 = min(u0 + a.split_tiles, t.count);
-    const int u_wave = u0 + (ROWS ? 0 : wave);
+    const int u0 = split * a.split_tiles, u1 = i0 > i1 ? 0 : min(u0 + a.split_tiles, t.count);
+    const int u_wave = u0 + wave / SETS;
 
     // this lane's rows: positions (-1: none) and queries
+    bf16x8* s_q = reinterpret_cast<bf16x8*>(s_mem) + set * R * STEPS * kWave;
     int pos[R];
     bf16x8 qf[LDS_Q ? 1 : R][NQ][STEPS];
 #pragma unroll
@@ -279,8 +305,8 @@ __global__ __launch_bounds__(kThreads, F32 || R > 1 ? 2 : 4) void quant_attn_ker
                 split8<NQ>(v, p);
 #pragma unroll
                 for (int k = 0; k < NQ; ++k) qf[j][k][st] = p[k];
-            } else if constexpr (LDS_Q) {
-                s_q[wave][j * STEPS + st][lane] = *reinterpret_cast<const bf16x8*>(q + 8 * st);
+            } else if constexpr (LDS_Q) {  // (by every wave of the set: the same)
+                s_q[(j * STEPS + st) * kWave + lane] = *reinterpret_cast<const bf16x8*>(q + 8 * st);
             } else {
                 qf[j][0][st] = *reinterpret_cast<const bf16x8*>(q + 8 * st);
             }
@@ -347,7 +373,7 @@ __global__ __launch_bounds__(kThreads, F32 || R > 1 ? 2 : 4) void quant_attn_ker
         f1 = offset(w_next.p1, w_next.tile, 1);
         tk.load_k(at, a.k + f0, a.k + f1);
     };
-    char* ring = s_ring + wave * RING * Slot<D>::kBytes;
+    char* ring = s_mem + wave * RING * Slot<D>::kBytes;
     const uint32_t ring_at = (uint32_t)__builtin_amdgcn_readfirstlane(
         (int)(uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)ring);
     auto send = [&](int it) {  // tile `it` on its way
@@ -358,25 +384,28 @@ __global__ __launch_bounds__(kThreads, F32 || R > 1 ? 2 : 4) void quant_attn_ker
         k0 += o0, v0 += o0, k1 += o1, v1 += o1;
         const uint32_t lds = ring_at + (it & 1) * Slot<D>::kBytes;
         constexpr int CODES = quant::code_bytes(D);
-        if constexpr (D == 128) {  // (a lane's own piece of K in its own place)
-            to_lds16(k0 + at.kc, lds);
-            to_lds16(k1 + at.kc, lds + CODES);
-            to_lds16(v0 + at.vc, lds + 2 * CODES);
-            to_lds16(v1 + at.vc, lds + 3 * CODES);
+        if constexpr (D == 128) {
+            // (the four pieces of a K row in an order that turns with the row, so
+            // that the lanes' reads spread over the banks)
+            const int piece = (lane ^ (lane >> 4)) & 3 | (lane & ~3);
+            to_lds16<ONCE>(k0 + piece * 16, lds);
+            to_lds16<ONCE>(k1 + piece * 16, lds + CODES);
+            to_lds16<ONCE>(v0 + at.vc, lds + 2 * CODES);
+            to_lds16<ONCE>(v1 + at.vc, lds + 3 * CODES);
         } else {
             const char *k = lane < 32 ? k0 : k1, *v = lane < 32 ? v0 : v1;
-            to_lds16(k + (lane & 31) * 16, lds);
-            to_lds16(v + (lane & 31) * 16, lds + 2 * CODES);
+            to_lds16<ONCE>(k + (lane & 31) * 16, lds);
+            to_lds16<ONCE>(v + (lane & 31) * 16, lds + 2 * CODES);
         }
         const char *e0 = lane < 16 ? k0 : k1, *e1 = lane < 48 ? v0 : v1;
-        to_lds4((lane < 32 ? e0 : e1) + CODES + (lane & (D / 8 - 1)) * 4, lds + 4 * CODES);
+        to_lds4<ONCE>((lane < 32 ? e0 : e1) + CODES + (lane & (D / 8 - 1)) * 4, lds + 4 * CODES);
     };
     auto take = [&](int it) {
         const char* p = ring + (it & 1) * Slot<D>::kBytes;
         constexpr int CODES = quant::code_bytes(D);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            load_words<D>(tk.code[h], p + h * CODES + (D == 128 ? lane * 16u : at.kc));
+            load_words<D>(tk.code[h], p + h * CODES + (D == 128 ? n * 64 + (g ^ (n >> 2)) * 16 : at.kc));
             load_words<D>(tv.code[h], p + (2 + h) * CODES + at.vc);
             tk.exp[h] = (uint8_t)p[4 * CODES + h * 64 + at.ke - 8 * D];
             tv.exp[h] = *reinterpret_cast<const uint32_t*>(p + 4 * CODES + 128 + h * 64 + at.ve - 8 * D);
@@ -428,7 +457,7 @@ __global__ __launch_bounds__(kThreads, F32 || R > 1 ? 2 : 4) void quant_attn_ker
                 for (int k = NQ - 1; k >= 0; --k) {
                     bf16x8 q;
                     if constexpr (LDS_Q)
-                        q = s_q[wave][j * STEPS + st][lane];
+                        q = s_q[(j * STEPS + st) * kWave + lane];
                     else
                         q = qf[j][k][st];
                     sc[j][0] = mma(kf[0], q, sc[j][0]);
@@ -440,43 +469,49 @@ __global__ __launch_bounds__(kThreads, F32 || R > 1 ? 2 : 4) void quant_attn_ker
         if (ROWS && it + 1 < mine) next(it + 1);
 
         // probabilities 2^x, x = s c - m: m is a row's largest score so far, or up
-        // to kSlack below it
-        bf16x8 p[R][NP];
+        // to kSlack below it (a NaN score reaches l through exp2, whatever m is)
+        if (!whole) {
 #pragma unroll
-        for (int j = 0; j < R; ++j) {
-            float z[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) z[i] = sc[j][i >> 2][i & 3];
-            if (!whole) {
+            for (int j = 0; j < R; ++j)
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const int key = j0 + (i >> 2) * 16 + 4 * g + (i & 3);
-                    if (!(sees(a, pos[j], key) && (i < 4 ? w.p0 : w.p1) >= 0)) z[i] = -INFINITY;
+                    if (!(sees(a, pos[j], key) && (i < 4 ? w.p0 : w.p1) >= 0)) sc[j][i >> 2][i & 3] = -INFINITY;
                 }
-            }
-            // (a NaN score reaches l through exp2, whatever m is)
-            float top = larger(larger(larger(z[0], z[1]), larger(z[2], z[3])),
-                               larger(larger(z[4], z[5]), larger(z[6], z[7]))) *
-                        a.scale;
-            if (__any(top > m[j] + kSlack)) {
-                top = fmaxf(top, __shfl_xor(top, 16));
-                top = fmaxf(top, __shfl_xor(top, 32));
-                if (top > m[j]) {
-                    const float f = __builtin_amdgcn_exp2f(m[j] - top);  // (0 where there was no key)
-                    m[j] = top;
+        }
+        float top[R];
+        bool far = false;
+#pragma unroll
+        for (int j = 0; j < R; ++j) {
+            top[j] = larger(larger(larger(sc[j][0][0], sc[j][0][1]), larger(sc[j][0][2], sc[j][0][3])),
+                            larger(larger(sc[j][1][0], sc[j][1][1]), larger(sc[j][1][2], sc[j][1][3]))) *
+                     a.scale;
+            far |= top[j] > m[j] + kSlack;
+        }
+        if (__any(far)) {
+#pragma unroll
+            for (int j = 0; j < R; ++j) {
+                top[j] = fmaxf(top[j], __shfl_xor(top[j], 16));
+                top[j] = fmaxf(top[j], __shfl_xor(top[j], 32));
+                if (top[j] > m[j]) {
+                    const float f = __builtin_amdgcn_exp2f(m[j] - top[j]);  // (0 where there was no key)
+                    m[j] = top[j];
                     l[j] *= f;
 #pragma unroll
                     for (int d = 0; d < PER; ++d) o[j][d] *= f;
                 }
             }
-            const float ref = m[j] == -INFINITY ? 0.f : m[j];
+        }
+        bf16x8 p[R][NP];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) z[i] = __builtin_amdgcn_exp2f(fmaf(z[i], a.scale, -ref));
+        for (int j = 0; j < R; ++j) {
+            const float ref = m[j] == -INFINITY ? 0.f : m[j];
+            float z[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) z[i] = __builtin_amdgcn_exp2f(fmaf(sc[j][i >> 2][i & 3], a.scale, -ref));
             l[j] += ((z[0] + z[1]) + (z[2] + z[3])) + ((z[4] + z[5]) + (z[6] + z[7]));
             split8<NP>(z, p[j]);
-            if (R > 2) __builtin_amdgcn_sched_barrier(0);
         }
-        __builtin_amdgcn_sched_barrier(0);
 
         // values
         uint32_t ve[2] = {tv.exp[0], tv.exp[1]};
@@ -588,64 +623,52 @@ __global__ __launch_bounds__(kThreads, F32 || R > 1 ? 2 : 4) void quant_attn_ker
         }
     };
 
-    if constexpr (ROWS) {
-        // a lane holds PER dims of each of 4 g .. 4 g + 3: D / 4 in one piece
+    // the states of the waves on the same rows, joined, 16 rows at a time (in the
+    // place of what the loop had in LDS)
+    float(*s_o)[16][D + 4] = reinterpret_cast<float(*)[16][D + 4]>(s_mem);
+    constexpr int PIECES = D / 8;
 #pragma unroll
-        for (int j = 0; j < R; ++j) {
-            const int r = r0 + 16 * j + n;
-            if (r / a.group >= s.n) continue;
-#pragma unroll
-            for (int e = 0; e < D / 4; e += 8) {
-                float v[8];
-#pragma unroll
-                for (int d = 0; d < 8; ++d) v[d] = o[j][(e + d) % PER][(e + d) / PER];
-                put(r, g * (D / 4) + e, v, m[j], l[j]);
-            }
-        }
-    } else {
-        // the waves' states, joined (in the ring's place, when all are through it)
-        float(*s_o)[OWN][D + 4] = reinterpret_cast<float(*)[OWN][D + 4]>(s_ring);
+    for (int j = 0; j < R; ++j) {
         __syncthreads();
-#pragma unroll
-        for (int j = 0; j < R; ++j) {
-            if (g == 0) {
-                s_m[wave][16 * j + n] = m[j];
-                s_l[wave][16 * j + n] = l[j];
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int d = 0; d < PER; d += 4)
-                    *reinterpret_cast<float4*>(&s_o[wave][16 * j + n][PER * (4 * g + i) + d]) =
-                        make_float4(o[j][d][i], o[j][d + 1][i], o[j][d + 2][i], o[j][d + 3][i]);
+        if (g == 0) {
+            s_m[wave][n] = m[j];
+            s_l[wave][n] = l[j];
         }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int d = 0; d < PER; d += 4)
+                *reinterpret_cast<float4*>(&s_o[wave][n][PER * (4 * g + i) + d]) =
+                    make_float4(o[j][d][i], o[j][d + 1][i], o[j][d + 2][i], o[j][d + 3][i]);
         __syncthreads();
-        constexpr int PIECES = D / 8;
-        for (int e = threadIdx.x; e < OWN * PIECES; e += kThreads) {
-            const int r = e / PIECES, x0 = e % PIECES * 8;
-            if ((r0 + r) / a.group >= s.n) continue;
-            float top = -INFINITY, sum = 0.f, v[8] = {};
+        for (int e = threadIdx.x; e < SETS * 16 * PIECES; e += kThreads) {
+            const int of = e / (16 * PIECES), r = e / PIECES % 16, x0 = e % PIECES * 8;
+            const int row = (rb * SETS + of) * OWN + 16 * j + r;
+            if (row / a.group >= s.n) continue;
+            float most = -INFINITY, sum = 0.f, v[8] = {};
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) top = fmaxf(top, s_m[w][r]);
+            for (int k = 0; k < STRIDE; ++k) most = fmaxf(most, s_m[k * SETS + of][r]);
 #pragma unroll
-            for (int w = 0; w < kWaves; ++w) {
-                if (s_m[w][r] == -INFINITY && s_l[w][r] == 0.f) continue;  // (no key)
-                const float f = __builtin_amdgcn_exp2f(s_m[w][r] - (top == -INFINITY ? 0.f : top));
-                sum += f * s_l[w][r];
+            for (int k = 0; k < STRIDE; ++k) {
+                const int from = k * SETS + of;
+                if (s_m[from][r] == -INFINITY && s_l[from][r] == 0.f) continue;  // (no key)
+                const float f = __builtin_amdgcn_exp2f(s_m[from][r] - (most == -INFINITY ? 0.f : most));
+                sum += f * s_l[from][r];
 #pragma unroll
-                for (int d = 0; d < 8; ++d) v[d] += f * s_o[w][r][x0 + d];
+                for (int d = 0; d < 8; ++d) v[d] += f * s_o[from][r][x0 + d];
             }
-            put(r0 + r, x0, v, top, sum);
+            put(row, x0, v, most, sum);
         }
     }
 }
 
-// Joins the splits of a row: a wave per row.
+// Joins the splits of a row: a wave per row, a lane per split for the weights and
+// per D / 64 dims for the sums, the parts of eight splits on their way at a time.
 template <bool F32, int D>
 __global__ __launch_bounds__(kThreads) void quant_merge_kernel(Args a) {
     const int lane = lane_id();
     const int hq = a.hkv * a.group;
-    const int64_t u = (int64_t)blockIdx.x * kWaves + threadIdx.x / kWave;
+    const int64_t u = (int64_t)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int64_t token = u / hq;
     const int h = (int)(u - token * hq);
     const int b = (int)(token / a.max_q), i = (int)(token - (int64_t)b * a.max_q);
@@ -653,29 +676,47 @@ __global__ __launch_bounds__(kThreads) void quant_merge_kernel(Args a) {
     const Seq s = sequence(a, b);
     if (i >= s.n) return;
     const int64_t row = (s.row + i) * hq + h;
-    const float2* ml = a.part_ml + row * a.splits;
-    float top = -INFINITY;
-    for (int k = lane; k < a.splits; k += kWave) top = fmaxf(top, ml[k].x);
-    top = wave_max_f32_dpp(top);
-    const float ref = top == -INFINITY ? 0.f : top;
     constexpr int N = D / kWave;
-    float sum = 0.f, v[N] = {};
-    for (int k = 0; k < a.splits; ++k) {
-        const float2 x = ml[k];
-        if (x.y == 0.f) continue;  // (no key)
-        const float f = __builtin_amdgcn_exp2f((x.x == -INFINITY ? 0.f : x.x) - ref);
-        sum += f * x.y;
-        const float* o = a.part_o + (row * a.splits + k) * D + lane * N;
+    float top = -INFINITY, sum = 0.f, v[N] = {};
+    for (int k0 = 0; k0 < a.splits; k0 += kWave) {
+        const int k = k0 + lane;
+        const float2 ml = k < a.splits ? a.part_ml[row * a.splits + k] : make_float2(-INFINITY, 0.f);
+        // (a part without keys has no mass, and undefined sums)
+        const uint64_t some = __ballot(ml.y != 0.f);
+        if (some == 0) continue;
+        const float most = fmaxf(top, wave_max_f32_dpp(ml.y != 0.f ? ml.x : -INFINITY));
+        const float ref = most == -INFINITY ? 0.f : most;
+        const float f = ml.y != 0.f ? __builtin_amdgcn_exp2f(ml.x - ref) : 0.f;
+        const float old = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - ref);
+        top = most;
+        sum = sum * old + wave_sum_f32_dpp(ml.y != 0.f ? f * ml.y : 0.f);
 #pragma unroll
-        for (int d = 0; d < N; ++d) v[d] += f * o[d];
+        for (int d = 0; d < N; ++d) v[d] *= old;
+        const int end = min(a.splits - k0, 64 - __clzll((long long)some));
+        const float* o = a.part_o + (row * a.splits + k0) * D + lane * N;
+        for (int j0 = 0; j0 < end; j0 += 8) {
+            float x[8][N];
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                __builtin_memcpy(x[j], o + (int64_t)min(j0 + j, end - 1) * D, sizeof(x[j]));
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int at = min(j0 + j, end - 1);
+                const bool on = j0 + j < end && (some >> at & 1);
+                const float w = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(f), at));
+#pragma unroll
+                for (int d = 0; d < N; ++d) v[d] += on ? w * x[j][d] : 0.f;
+            }
+        }
     }
     const float f = sum == 0.f ? 0.f : 1.f / sum;
+    if constexpr (F32) {
 #pragma unroll
-    for (int d = 0; d < N; ++d) {
-        if constexpr (F32)
-            static_cast<float*>(a.out)[row * D + lane * N + d] = v[d] * f;
-        else
-            static_cast<__bf16*>(a.out)[row * D + lane * N + d] = (__bf16)(v[d] * f);
+        for (int d = 0; d < N; ++d) static_cast<float*>(a.out)[row * D + lane * N + d] = v[d] * f;
+    } else if constexpr (N == 2) {
+        static_cast<uint32_t*>(a.out)[(row * D) / 2 + lane] = pack2(v[0] * f, v[1] * f);
+    } else {
+        static_cast<__bf16*>(a.out)[row * D + lane] = (__bf16)(v[0] * f);
     }
 }
 
@@ -689,11 +730,11 @@ using namespace presto::qattn;
 
 QuantPlan quant_plan(const presto_paged_attn_desc* d, presto_dtype dt) {
     QuantPlan p{};
-    const int64_t group = d->hq / d->pages.hkv, rows = (int64_t)d->max_q * group;
+    const int64_t group = d->hq / d->pages.hkv, rows = (int64_t)d->max_q * group, batch = d->pages.batch;
     const bool f32 = dt == PRESTO_DT_F32;
-    p.own = !f32 && rows >= 256;
+    p.own = !f32 && rows >= 128;
     p.r = f32 ? 1 : p.own ? 4 : rows > 16 ? 2 : 1;
-    const int64_t of_group = p.own ? 16 * p.r * kWaves : 16 * p.r;
+    const int64_t of_group = (p.own ? 2 : 1) * 16 * p.r;
     p.row_blocks = (rows + of_group - 1) / of_group;
     // the tiles of a row block: the longest, and on average
     int64_t most = ((int64_t)d->max_ctx + kTile - 1) / kTile;
@@ -701,16 +742,20 @@ QuantPlan quant_plan(const presto_paged_attn_desc* d, presto_dtype dt) {
     if (d->window)
         most = std::min(most, ((int64_t)d->window + span) / kTile + 2 + ((int64_t)d->sinks + kTile - 1) / kTile);
     most = std::max<int64_t>(most, 1);
-    const int64_t blocks = (int64_t)d->pages.batch * p.row_blocks * d->pages.hkv;
-    int64_t mean = most;
-    if (d->total_ctx > 0) mean = std::min(most, d->total_ctx / d->pages.batch / kTile + 1);
-    const int64_t target = p.own ? 512 : 1024;
+    int64_t all = batch * most;  // of the batch, for one row block and head
+    if (d->total_ctx > 0) all = std::min(all, d->total_ctx / kTile + batch);
+    // Contexts are cut into pieces of one length, so many that they make one round
+    // of workgroups: as many as run at once, less one per sequence (whose last
+    // piece is a short one).
+    const int64_t room = (p.own ? 512 : p.r == 1 && !f32 ? 1024 : 512) / (p.row_blocks * d->pages.hkv);
     constexpr int64_t kLeast = 16, kMostSplits = 256;
-    int64_t tiles = std::max(kLeast, (blocks * mean + target - 1) / target);
-    tiles = std::max(tiles, (most + kMostSplits - 1) / kMostSplits);
+    int64_t tiles = room > batch ? (all + room - batch - 1) / (room - batch) : most;
+    tiles = std::max(tiles, std::max(kLeast, (most + kMostSplits - 1) / kMostSplits));
     p.splits = (most + tiles - 1) / tiles;
     p.split_tiles = (most + p.splits - 1) / p.splits;
-    p.blocks = blocks * p.splits;
+    const int64_t blocks = batch * p.row_blocks * d->pages.hkv;
+    p.blocks = p.own ? blocks * p.splits
+                     : ((int64_t)d->pages.batch * p.splits + 7) / 8 * 8 * p.row_blocks * d->pages.hkv;
     const int64_t out_rows = d->total_q * d->hq, merge_rows = (int64_t)d->pages.batch * d->max_q * d->hq;
     p.merge_blocks = (merge_rows + kWaves - 1) / kWaves;
     p.fits = p.blocks <= (1 << 23) && merge_rows < ((int64_t)1 << 31) && p.merge_blocks <= (1 << 23);

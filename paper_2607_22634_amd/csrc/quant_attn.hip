@@ -40,7 +40,7 @@ struct Args {
     int32_t* flags;
     int64_t page_bytes, q_stride, total_q;
     int32_t batch, hkv, group, max_q, max_ctx, window, sinks, max_pages, num_pages, shift;
-    int32_t row_blocks, splits, split_tiles;
+    int32_t row_blocks, splits, split_tiles, own;  // own: rows of a wave
     float scale;  // times log2 e
 };
 
@@ -160,6 +160,33 @@ struct Slot {
     static constexpr int kLoads = (D == 128 ? 4 : 2) + 1;
 };
 
+// The unit-th (sequence, piece).  Pieces behind a sequence's end are left out
+// where batches are small enough to count the others: they would take the places
+// of those that work.
+__device__ __forceinline__ bool piece_at(const Args& a, int unit, int& b, int& split) {
+    if (a.splits == 1 || a.batch > 4 * kWave) {
+        split = unit / a.batch;
+        b = unit % a.batch;
+        return split < a.splits;
+    }
+    int before = 0;
+    for (int b0 = 0; b0 < a.batch; b0 += kWave) {
+        const int i = b0 + lane_id();
+        const int tiles = i < a.batch ? (min(max(a.ctx[i], 0), a.max_ctx) + kTile - 1) / kTile : 0;
+        const int pieces = i < a.batch ? max(1, min((tiles + a.split_tiles - 1) / a.split_tiles, a.splits)) : 0;
+        const int run = before + (int)wave_scan_dpp((uint32_t)pieces);
+        const uint64_t past = __ballot(run > unit);
+        if (past) {
+            const int k = __ffsll((unsigned long long)past) - 1;
+            b = b0 + k;
+            split = unit - (__builtin_amdgcn_readlane(run, k) - __builtin_amdgcn_readlane(pieces, k));
+            return true;
+        }
+        before = __builtin_amdgcn_readlane(run, kWave - 1);
+    }
+    return false;
+}
+
 // What a lane holds of a tile's K, or of its V: of two blocks the codes, and
 // exponents.
 template <int D>
@@ -271,9 +298,7 @@ __global__ __launch_bounds__(kThreads, F32 || R > 1 ? 2 : 4) void quant_attn_ker
         x /= a.row_blocks;
         head = x % a.hkv;
         const int unit = x / a.hkv * 8 + xcd;
-        split = unit % a.splits;
-        b = unit / a.splits;
-        if (b >= a.batch) return;
+        if (!piece_at(a, unit, b, split)) return;
     }
 
     const Seq s = sequence(a, b);
@@ -283,6 +308,7 @@ __global__ __launch_bounds__(kThreads, F32 || R > 1 ? 2 : 4) void quant_attn_ker
     const int i0 = r0 / a.group, i1 = min((r0 + OWN - 1) / a.group, s.n - 1);  // (i0 > i1: a set without rows)
     const Tiles t = tiles_of(a, s.first + i0, s.first + i1);
     const int u0 = split * a.split_tiles, u1 = i0 > i1 ? 0 : min(u0 + a.split_tiles, t.count);
+    if (SETS == 1 && split > 0 && u0 >= u1) return;  // (the merge knows)
     const int u_wave = u0 + wave / SETS;
 
     // this lane's rows: positions (-1: none) and queries
@@ -676,11 +702,16 @@ __global__ __launch_bounds__(kThreads) void quant_merge_kernel(Args a) {
     const Seq s = sequence(a, b);
     if (i >= s.n) return;
     const int64_t row = (s.row + i) * hq + h;
+    // the pieces that the tiles of this row's block make (the first one always is
+    // one)
+    const int r0 = (i * a.group + h % a.group) / a.own * a.own;
+    const Tiles t = tiles_of(a, s.first + r0 / a.group, s.first + min((r0 + a.own - 1) / a.group, s.n - 1));
+    const int splits = min(max((t.count + a.split_tiles - 1) / a.split_tiles, 1), a.splits);
     constexpr int N = D / kWave;
     float top = -INFINITY, sum = 0.f, v[N] = {};
-    for (int k0 = 0; k0 < a.splits; k0 += kWave) {
+    for (int k0 = 0; k0 < splits; k0 += kWave) {
         const int k = k0 + lane;
-        const float2 ml = k < a.splits ? a.part_ml[row * a.splits + k] : make_float2(-INFINITY, 0.f);
+        const float2 ml = k < splits ? a.part_ml[row * a.splits + k] : make_float2(-INFINITY, 0.f);
         // (a part without keys has no mass, and undefined sums)
         const uint64_t some = __ballot(ml.y != 0.f);
         if (some == 0) continue;
@@ -692,7 +723,7 @@ __global__ __launch_bounds__(kThreads) void quant_merge_kernel(Args a) {
         sum = sum * old + wave_sum_f32_dpp(ml.y != 0.f ? f * ml.y : 0.f);
 #pragma unroll
         for (int d = 0; d < N; ++d) v[d] *= old;
-        const int end = min(a.splits - k0, 64 - __clzll((long long)some));
+        const int end = min(splits - k0, 64 - __clzll((long long)some));
         const float* o = a.part_o + (row * a.splits + k0) * D + lane * N;
         for (int j0 = 0; j0 < end; j0 += 8) {
             float x[8][N];
@@ -742,14 +773,20 @@ QuantPlan quant_plan(const presto_paged_attn_desc* d, presto_dtype dt) {
     if (d->window)
         most = std::min(most, ((int64_t)d->window + span) / kTile + 2 + ((int64_t)d->sinks + kTile - 1) / kTile);
     most = std::max<int64_t>(most, 1);
-    int64_t all = batch * most;  // of the batch, for one row block and head
-    if (d->total_ctx > 0) all = std::min(all, d->total_ctx / kTile + batch);
     // Contexts are cut into pieces of one length, so many that they make one round
-    // of workgroups: as many as run at once, less one per sequence (whose last
-    // piece is a short one).
+    // of workgroups, as many as run at once; ragged ones so that there are about
+    // that many.
     const int64_t room = (p.own ? 512 : p.r == 1 && !f32 ? 1024 : 512) / (p.row_blocks * d->pages.hkv);
     constexpr int64_t kLeast = 16, kMostSplits = 256;
-    int64_t tiles = room > batch ? (all + room - batch - 1) / (room - batch) : most;
+    int64_t tiles = most;
+    if (room > batch) {
+        tiles = (most + room / batch - 1) / (room / batch);
+        const int64_t all = d->total_ctx / kTile + batch;
+        if (d->total_ctx > 0 && !d->window && all < batch * most) {
+            const int64_t pieces = std::max<int64_t>(room - batch / 2, 1);
+            tiles = std::min(tiles, (all + pieces - 1) / pieces);
+        }
+    }
     tiles = std::max(tiles, std::max(kLeast, (most + kMostSplits - 1) / kMostSplits));
     p.splits = (most + tiles - 1) / tiles;
     p.split_tiles = (most + p.splits - 1) / p.splits;
@@ -797,6 +834,7 @@ presto_status launch_quant_attn(const presto_paged_attn_desc* d, presto_dtype dt
     a.row_blocks = (int)p.row_blocks;
     a.splits = (int)p.splits;
     a.split_tiles = (int)p.split_tiles;
+    a.own = 16 * p.r;
     a.scale = d->scale * 1.4426950408889634f;
     auto run = [&](auto f32, auto dim) {
         const unsigned grid = (unsigned)p.blocks;

@@ -149,10 +149,13 @@ def _books_of(batch, cols, pages, page_size) -> PagesDesc:
 
 def _rows(name, t, heads, d):
     """Token rows [n, heads, dim], any stride between tokens; the stride."""
-    shape, stride = t.shape, t.stride()
+    return _rows_of(name, t.shape, t.stride(), heads, d)
+
+
+def _rows_of(name, shape, stride, heads, d):
     if len(shape) != 3 or shape[1] != heads or shape[2] != d:
         raise ValueError(f"{name} must be [tokens, {heads}, {d}]")
-    if (stride[2] != 1 or (stride[1] != d and heads > 1)) and t.numel() > 0:
+    if (stride[2] != 1 or (stride[1] != d and heads > 1)) and 0 not in shape:
         raise ValueError(f"the heads of a token of {name} must be contiguous")
     if shape[0] <= 1:
         return 0

@@ -8,12 +8,14 @@ device of their tensors, on that device's current stream unless one is given.
 from __future__ import annotations
 
 import ctypes
+import functools
 
 import torch
 
 from ._lib import (PRESTO_ROPE_RAMP_LOG, PRESTO_ROPE_RAMP_NONE, PRESTO_ROPE_RAMP_TURNS, AppendDesc, PagedAttnDesc,
                    PagesDesc, RopeDesc, RopeFreqDesc, _check, _ptr, lib)
-from ._paged import _DT, _I32, _book, _empty, _int32, _launch, _one_by_one, _pool, _room, _rows, _same, _vector
+from ._paged import (_DT, _I32, _book, _empty, _int32, _launch, _one_by_one, _pool, _pool_of, _room, _rows, _rows_of,
+                     _same, _vector)
 
 _RAMPS = {None: PRESTO_ROPE_RAMP_NONE, "turns": PRESTO_ROPE_RAMP_TURNS, "log": PRESTO_ROPE_RAMP_LOG}
 
@@ -76,23 +78,34 @@ def _plan_on(plan: RopePlan, dev: int) -> None:
         raise ValueError("the plan must be on the GPU of the tensors")
 
 
+# (Calls on few rows are bound by the host: what follows from sizes alone is
+# looked up, and the usual tensors are looked at in one expression before they
+# are gone through to say which one is wrong.)
+@functools.lru_cache(maxsize=64)
+def _rope_of(shape, stride, out_shape, out_stride):
+    if len(shape) != 3:
+        raise ValueError("x must be [rows, heads, dim]")
+    n, heads, d = shape
+    _one_by_one(heads, d)
+    from_ = _rows_of("x", shape, stride, heads, d)
+    if out_shape != shape:
+        raise ValueError("out must be a tensor of x's shape and type on its GPU")
+    return n, heads, d, from_, _rows_of("out", out_shape, out_stride, heads, d)
+
+
 def presto_rope(x: torch.Tensor, positions: torch.Tensor, plan: RopePlan, *, out=None, stream=None) -> torch.Tensor:
     """x [rows, heads, dim] rotated by positions [rows] (int32): in `out`, which
     may be x itself, or a new tensor."""
-    if x.dim() != 3:
-        raise ValueError("x must be [rows, heads, dim]")
-    n, heads, d = x.shape
     dt, dev = _type(x), x.get_device()
-    _one_by_one(heads, d)
-    stride = _rows("x", x, heads, d)
-    _book(dev, "positions", positions)
-    _vector("positions", positions, n)
-    _plan_on(plan, dev)
     if out is None:
         out = _empty(stream, x.shape, x.dtype, x.device)
-    elif out.shape != x.shape or out.dtype is not x.dtype or out.get_device() != dev:
+    n, heads, d, stride, to = _rope_of(x.shape, x.stride(), out.shape, out.stride())
+    if not (0 <= dev == positions.get_device() == out.get_device() == plan.device_index and out.dtype is x.dtype
+            and positions.dtype is _I32 and positions.is_contiguous() and positions.shape == (n,)):
+        _book(dev, "positions", positions)
+        _vector("positions", positions, n)
+        _plan_on(plan, dev)
         raise ValueError("out must be a tensor of x's shape and type on its GPU")
-    to = _rows("out", out, heads, d)
     _launch(lib().presto_rope, "presto_rope", dev, stream, plan.ref, plan.address, dt, x.data_ptr(), stride, n, heads,
             d, positions.data_ptr(), out.data_ptr(), to)
     return out
@@ -124,6 +137,26 @@ def _cached(k_pages, v_pages, page_table, offsets, ctx, ctx_new, flags, dev) -> 
     return _pool(k_pages, v_pages, table[1], b, False)
 
 
+@functools.lru_cache(maxsize=64)
+def _append_of(shape, k_stride, v_stride, q_shape, q_stride, out_stride, dt, max_new, pool, pool_stride, pool_type,
+               cols, batch):
+    """Descriptor of presto_append_rope from sizes alone, and a reference to it
+    (not to be changed)."""
+    _int32(max_new)
+    pages = _pool_of(pool, pool_stride, pool_type, batch, cols, False)
+    strides = [_rows_of(name, shape, s, pages.hkv, pages.head_dim) for name, s in (("k_new", k_stride),
+                                                                                  ("v_new", v_stride))]
+    hq, q_strides = 0, (0, 0)
+    if q_shape is not None:
+        if len(q_shape) != 3 or q_shape[0] != shape[0]:
+            raise ValueError("q must be [tokens, heads, dim] of k_new's type on its GPU")
+        hq = q_shape[1]
+        q_strides = [_rows_of(name, q_shape, s, hq, pages.head_dim) for name, s in (("q", q_stride),
+                                                                                   ("out", out_stride))]
+    desc = AppendDesc(pages, dt, hq, max_new, shape[0], *q_strides, *strides)
+    return desc, ctypes.byref(desc)
+
+
 def presto_append_rope(plan: RopePlan | None, q: torch.Tensor | None, k_new: torch.Tensor, v_new: torch.Tensor,
                        offsets: torch.Tensor, max_new: int, k_pages: torch.Tensor, v_pages: torch.Tensor,
                        page_table: torch.Tensor, ctx: torch.Tensor, ctx_new: torch.Tensor, *, out=None, flags=None,
@@ -131,37 +164,44 @@ def presto_append_rope(plan: RopePlan | None, q: torch.Tensor | None, k_new: tor
     """presto_append_kv with the new keys rotated by their positions (plan None:
     as they are), into a cache of the rows' type or of 4 bits; with q [rows, Hq,
     d] given, its rows rotated alike into `out` (may be q), which is returned."""
-    _int32(max_new)
-    dev, dt = k_new.get_device(), _type(k_new)
-    _same(dev, "k_new v_new k_pages v_pages", k_new, v_new, k_pages, v_pages)
-    pages = _cached(k_pages, v_pages, page_table, offsets, ctx, ctx_new, flags, dev)
-    if v_new.dtype is not k_new.dtype or k_pages.dtype not in (k_new.dtype, torch.uint8):
-        raise TypeError("the new rows and the pages must be of one type, or the pages of 4 bits")
-    k_stride = _rows("k_new", k_new, pages.hkv, pages.head_dim)
-    if v_new.shape != k_new.shape:
+    dev, dtype, dt, table, pool, pool_stride = (k_new.get_device(), k_new.dtype, _type(k_new), page_table.shape,
+                                                k_pages.shape, k_pages.stride())
+    b = offsets.shape[0] - 1
+    if not (0 <= dev == v_new.get_device() == k_pages.get_device() == v_pages.get_device() == offsets.get_device()
+            == page_table.get_device() == ctx.get_device() == ctx_new.get_device()
+            and offsets.dtype is _I32 is page_table.dtype and ctx.dtype is _I32 is ctx_new.dtype
+            and offsets.is_contiguous() and page_table.is_contiguous() and ctx.is_contiguous()
+            and ctx_new.is_contiguous() and len(table) == 2 and table[0] == b and offsets.shape == (b + 1,)
+            and ctx.shape == (b,) == ctx_new.shape and v_new.shape == k_new.shape and v_new.dtype is dtype
+            and k_pages.dtype in (dtype, torch.uint8)
+            and v_pages.shape == pool and v_pages.stride() == pool_stride and v_pages.dtype is k_pages.dtype):
+        _same(dev, "k_new v_new k_pages v_pages", k_new, v_new, k_pages, v_pages)
+        _cached(k_pages, v_pages, page_table, offsets, ctx, ctx_new, flags, dev)
+        if v_new.dtype is not dtype or k_pages.dtype not in (dtype, torch.uint8):
+            raise TypeError("the new rows and the pages must be of one type, or the pages of 4 bits")
         raise ValueError("k_new and v_new must have one shape")
-    v_stride = _rows("v_new", v_new, pages.hkv, pages.head_dim)
-    n = k_new.shape[0]
-    hq = q_stride = out_stride = 0
+    if flags is not None:
+        _book(dev, "flags", flags)
+    q_shape = q_stride = out_stride = None
     if q is not None:
-        if q.get_device() != dev or q.dtype is not k_new.dtype or q.dim() != 3 or q.shape[0] != n:
-            raise ValueError("q must be [tokens, heads, dim] of k_new's type on its GPU")
-        hq = q.shape[1]
-        q_stride = _rows("q", q, hq, pages.head_dim)
+        q_shape, q_stride = q.shape, q.stride()
         if out is None:
-            out = _empty(stream, q.shape, q.dtype, q.device)
-        elif out.shape != q.shape or out.dtype is not q.dtype or out.get_device() != dev:
+            out = _empty(stream, q_shape, q.dtype, q.device)
+        elif out.shape != q_shape or out.dtype is not q.dtype or out.get_device() != q.get_device():
             raise ValueError("out must be a tensor of q's shape and type on its GPU")
-        out_stride = _rows("out", out, hq, pages.head_dim)
+        if q.get_device() != dev or q.dtype is not dtype:
+            raise ValueError("q must be [tokens, heads, dim] of k_new's type on its GPU")
+        out_stride = out.stride()
     elif out is not None:
         raise ValueError("out without q")
     if plan is not None:
         _plan_on(plan, dev)
-    desc = AppendDesc(pages, dt, hq, max_new, n, q_stride, out_stride, k_stride, v_stride)
-    _launch(lib().presto_append_rope, "presto_append_rope", dev, stream, ctypes.byref(desc),
-            None if plan is None else plan.ref, None if plan is None else plan.address, _ptr(q), k_new.data_ptr(),
-            v_new.data_ptr(), offsets.data_ptr(), _ptr(out), k_pages.data_ptr(), v_pages.data_ptr(),
-            page_table.data_ptr(), ctx.data_ptr(), ctx_new.data_ptr(), _ptr(flags))
+    _, ref = _append_of(k_new.shape, k_new.stride(), v_new.stride(), q_shape, q_stride, out_stride, dt, max_new, pool,
+                        pool_stride, k_pages.dtype, table[1], b)
+    _launch(lib().presto_append_rope, "presto_append_rope", dev, stream, ref, None if plan is None else plan.ref,
+            None if plan is None else plan.address, _ptr(q), k_new.data_ptr(), v_new.data_ptr(), offsets.data_ptr(),
+            _ptr(out), k_pages.data_ptr(), v_pages.data_ptr(), page_table.data_ptr(), ctx.data_ptr(),
+            ctx_new.data_ptr(), _ptr(flags))
     return out
 
 
@@ -205,17 +245,24 @@ def presto_read_kv(k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: tor
     return out
 
 
-def _quant_desc(q, k_pages, v_pages, page_table, batch, max_q, max_ctx, scale, window, sinks, total_ctx):
-    table = page_table.shape
+@functools.lru_cache(maxsize=64)
+def _queries_of(shape, stride, pool, pool_stride, pool_type, table, batch):
+    """(pages, heads, rows, stride of a row) of an attention, from sizes alone."""
     if len(table) != 2 or table[0] != batch:
         raise ValueError("page_table must be [sequences, columns]")
-    if k_pages.dtype is not torch.uint8:
+    if pool_type is not torch.uint8:
         raise TypeError("the pages must be of 4 bits (uint8)")
-    pages = _pool(k_pages, v_pages, table[1], batch, False)
-    if q.dim() != 3:
+    pages = _pool_of(pool, pool_stride, pool_type, batch, table[1], False)
+    if len(shape) != 3:
         raise ValueError("q must be [tokens, heads, dim]")
-    n, hq = q.shape[:2]
-    stride = _rows("q", q, hq, pages.head_dim)
+    return pages, shape[1], shape[0], _rows_of("q", shape, stride, shape[1], pages.head_dim)
+
+
+def _quant_desc(q, k_pages, v_pages, page_table, batch, max_q, max_ctx, scale, window, sinks, total_ctx):
+    pool, pool_stride = k_pages.shape, k_pages.stride()
+    if v_pages.shape != pool or v_pages.stride() != pool_stride or v_pages.dtype is not k_pages.dtype:
+        raise ValueError("k_pages and v_pages must have one shape, stride and type")
+    pages, hq, n, stride = _queries_of(q.shape, q.stride(), pool, pool_stride, k_pages.dtype, page_table.shape, batch)
     if max_ctx is None:
         max_ctx = pages.max_pages * pages.page_size
     _int32(max_q | max_ctx | window | sinks)
@@ -234,10 +281,14 @@ def presto_quant_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torc
     dt, dev = _type(q), q.get_device()
     desc = _quant_desc(q, k_pages, v_pages, page_table, b, 1 if q_offsets is None else max_q, max_ctx, scale, window,
                        sinks, total_ctx)
-    _same(dev, "q k_pages v_pages", q, k_pages, v_pages)
-    _book(dev, "page_table ctx q_offsets flags", page_table, ctx, q_offsets, flags)
-    _vector("ctx", ctx, b)
-    if q_offsets is not None:
+    if not (0 <= dev == k_pages.get_device() == v_pages.get_device() == page_table.get_device() == ctx.get_device()
+            and page_table.dtype is _I32 is ctx.dtype and page_table.is_contiguous() and ctx.is_contiguous()
+            and ctx.shape == (b,)):
+        _same(dev, "q k_pages v_pages", q, k_pages, v_pages)
+        _book(dev, "page_table ctx", page_table, ctx)
+        _vector("ctx", ctx, b)
+    if q_offsets is not None or flags is not None:
+        _book(dev, "q_offsets flags", q_offsets, flags)
         _vector("q_offsets", q_offsets, b + 1)
     L, ref, ws, nb = lib(), ctypes.byref(desc), workspace, 0
     if out is None:

@@ -28,7 +28,10 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 constexpr int kTile = 32;  // keys
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kWave;
-constexpr float kSlack = 16.f;  // a row's reference may lie this far (log2) below its largest score
+// A row's reference lies this far (log2) above its largest score when it is
+// chosen, and at most one below its largest score later on.
+constexpr float kAbove = 15.f;
+constexpr float kNoKey = -3.402823466e38f;  // reference of a row without keys (so that masked scores weigh 0)
 
 struct Args {
     const void* q;
@@ -276,21 +279,23 @@ __global__ __launch_bounds__(kThreads, F32 || R > 1 ? 2 : 4) void quant_attn_ker
                                  kWaves * 16 * (D + 4) * 4);
     __shared__ __align__(16) char s_mem[LDS];
     __shared__ float s_m[kWaves][16], s_l[kWaves][16];
+    __shared__ int s_pos[SETS][OWN];
 
     const int lane = lane_id(), n = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
     const int set = wave % SETS;
     // blocks go round the eight XCDs.  ROWS: those of one head, which share its
-    // keys, to one of them where there are eight heads; else the heads of a
+    // keys, to one of them where there are eight heads, and first pieces, which are
+    // whole, before last ones; else the heads of a
     // stretch of positions, which lie side by side in the pool
     int x = blockIdx.x, head, split, rb, b;
     if constexpr (ROWS) {
         head = x % a.hkv;
         x /= a.hkv;
-        split = x % a.splits;
-        x /= a.splits;
         rb = x % a.row_blocks;
-        b = x / a.row_blocks;
+        x /= a.row_blocks;
+        b = x % a.batch;
+        split = x / a.batch;
     } else {
         const int xcd = x % 8;
         x /= 8;
@@ -311,14 +316,13 @@ __global__ __launch_bounds__(kThreads, F32 || R > 1 ? 2 : 4) void quant_attn_ker
     if (SETS == 1 && split > 0 && u0 >= u1) return;  // (the merge knows)
     const int u_wave = u0 + wave / SETS;
 
-    // this lane's rows: positions (-1: none) and queries
+    // this lane's rows: positions (-1: none; by every wave of the set) and queries
     bf16x8* s_q = reinterpret_cast<bf16x8*>(s_mem) + set * R * STEPS * kWave;
-    int pos[R];
     bf16x8 qf[LDS_Q ? 1 : R][NQ][STEPS];
 #pragma unroll
     for (int j = 0; j < R; ++j) {
         const int r = r0 + 16 * j + n, i = r / a.group;
-        pos[j] = i < s.n ? s.first + i : -1;
+        s_pos[set][16 * j + n] = i < s.n ? s.first + i : -1;
         const T* q = static_cast<const T*>(a.q) + (s.row + min(i, s.n - 1)) * a.q_stride +
                      ((int64_t)head * a.group + r % a.group) * D + g * (D / 4);
 #pragma unroll
@@ -339,12 +343,13 @@ __global__ __launch_bounds__(kThreads, F32 || R > 1 ? 2 : 4) void quant_attn_ker
         }
     }
 
-    float m[R], l[R];
-    f32x4 o[R][PER];
+    float m[R];
+    f32x4 l[R], o[R][PER];  // (l: the same four times, from a product with ones)
+    bool chosen = false;    // every row of the wave has a reference
 #pragma unroll
     for (int j = 0; j < R; ++j) {
-        m[j] = -INFINITY;  // no key yet
-        l[j] = 0.f;
+        m[j] = kNoKey;
+        l[j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int d = 0; d < PER; ++d) o[j][d] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
@@ -387,7 +392,8 @@ __global__ __launch_bounds__(kThreads, F32 || R > 1 ? 2 : 4) void quant_attn_ker
 
     // ROWS: the next tile's K is asked for when this one's is used up, its V
     // likewise: one set of registers, and what is on its way has the rest of the
-    // step.  Else, where memory is what counts, tiles come through LDS, two ahead:
+    // step (the last tile asks for itself again: a load that might not be made
+    // costs a wait for those that are).  Else, where memory is what counts, tiles come through LDS, two ahead:
     // a lane's registers could not hold as much.
     Half<D> tk, tv;
     Where w, w_next, w_then;
@@ -468,6 +474,10 @@ __global__ __launch_bounds__(kThreads, F32 || R > 1 ? 2 : 4) void quant_attn_ker
 #pragma unroll
         for (int j = 0; j < R; ++j) sc[j][0] = sc[j][1] = f32x4{0.f, 0.f, 0.f, 0.f};
         const float ks[2] = {scale_of<0>(tk.exp[0]), scale_of<0>(tk.exp[1])};
+        constexpr int AHEAD = 2;  // reads of queries on their way (more, and registers spill)
+        bf16x8 ql[LDS_Q ? AHEAD : 1];
+        auto read_q = [&](int i) { return s_q[(i % R * STEPS + i / R) * kWave + lane]; };
+        if constexpr (LDS_Q) ql[0] = read_q(0);
 #pragma unroll
         for (int st = 0; st < STEPS; ++st) {
             bf16x8 kf[2];
@@ -482,62 +492,78 @@ __global__ __launch_bounds__(kThreads, F32 || R > 1 ? 2 : 4) void quant_attn_ker
 #pragma unroll
                 for (int k = NQ - 1; k >= 0; --k) {
                     bf16x8 q;
-                    if constexpr (LDS_Q)
-                        q = s_q[(j * STEPS + st) * kWave + lane];
-                    else
+                    if constexpr (LDS_Q) {
+                        const int i = st * R + j;
+                        if (i + 1 < STEPS * R) ql[(i + 1) % AHEAD] = read_q(i + 1);
+                        __builtin_amdgcn_sched_barrier(0x6);  // (the read stays in front of the products)
+                        q = ql[i % AHEAD];
+                    } else {
                         q = qf[j][k][st];
+                    }
                     sc[j][0] = mma(kf[0], q, sc[j][0]);
                     sc[j][1] = mma(kf[1], q, sc[j][1]);
                 }
         }
 
         __builtin_amdgcn_sched_barrier(0);
-        if (ROWS && it + 1 < mine) next(it + 1);
+        if constexpr (ROWS) next(min(it + 1, mine - 1));
 
-        // probabilities 2^x, x = s c - m: m is a row's largest score so far, or up
-        // to kSlack below it (a NaN score reaches l through exp2, whatever m is)
         if (!whole) {
 #pragma unroll
-            for (int j = 0; j < R; ++j)
+            for (int j = 0; j < R; ++j) {
+                const int pos = s_pos[set][16 * j + n];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const int key = j0 + (i >> 2) * 16 + 4 * g + (i & 3);
-                    if (!(sees(a, pos[j], key) && (i < 4 ? w.p0 : w.p1) >= 0)) sc[j][i >> 2][i & 3] = -INFINITY;
-                }
-        }
-        float top[R];
-        bool far = false;
-#pragma unroll
-        for (int j = 0; j < R; ++j) {
-            top[j] = larger(larger(larger(sc[j][0][0], sc[j][0][1]), larger(sc[j][0][2], sc[j][0][3])),
-                            larger(larger(sc[j][1][0], sc[j][1][1]), larger(sc[j][1][2], sc[j][1][3]))) *
-                     a.scale;
-            far |= top[j] > m[j] + kSlack;
-        }
-        if (__any(far)) {
-#pragma unroll
-            for (int j = 0; j < R; ++j) {
-                top[j] = fmaxf(top[j], __shfl_xor(top[j], 16));
-                top[j] = fmaxf(top[j], __shfl_xor(top[j], 32));
-                if (top[j] > m[j]) {
-                    const float f = __builtin_amdgcn_exp2f(m[j] - top[j]);  // (0 where there was no key)
-                    m[j] = top[j];
-                    l[j] *= f;
-#pragma unroll
-                    for (int d = 0; d < PER; ++d) o[j][d] *= f;
+                    if (!(sees(a, pos, key) && (i < 4 ? w.p0 : w.p1) >= 0)) sc[j][i >> 2][i & 3] = -INFINITY;
                 }
             }
         }
+        // probabilities 2^x, x = s c - m.  The largest score is looked for only
+        // where one of them reaches 2, which a bit of its exponent tells (or is
+        // not finite), or where a row has had no key: rarely after the first
+        // tiles.  (A NaN score reaches l, whatever m is.)
         bf16x8 p[R][NP];
+        for (bool choose = !chosen;;) {
+            if (choose) {
+                bool all = true;
 #pragma unroll
-        for (int j = 0; j < R; ++j) {
-            const float ref = m[j] == -INFINITY ? 0.f : m[j];
-            float z[8];
+                for (int j = 0; j < R; ++j) {
+                    float top = larger(larger(larger(sc[j][0][0], sc[j][0][1]), larger(sc[j][0][2], sc[j][0][3])),
+                                       larger(larger(sc[j][1][0], sc[j][1][1]), larger(sc[j][1][2], sc[j][1][3])));
+                    top = fmaxf(top, __shfl_xor(top, 16));
+                    top = fmaxf(top, __shfl_xor(top, 32));
+                    top = fmaf(top, a.scale, kAbove);
+                    if (top > m[j]) {
+                        const float f = __builtin_amdgcn_exp2f(m[j] - top);  // (0 where there was no key)
+                        m[j] = top;
+                        l[j] *= f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) z[i] = __builtin_amdgcn_exp2f(fmaf(sc[j][i >> 2][i & 3], a.scale, -ref));
-            l[j] += ((z[0] + z[1]) + (z[2] + z[3])) + ((z[4] + z[5]) + (z[6] + z[7]));
-            split8<NP>(z, p[j]);
+                        for (int d = 0; d < PER; ++d) o[j][d] *= f;
+                    }
+                    all &= m[j] > kNoKey || s_pos[set][16 * j + n] < 0;
+                }
+                chosen = __all(all);
+            }
+            u32x4 bits = {0, 0, 0, 0};
+#pragma unroll
+            for (int j = 0; j < R; ++j) {
+                float z[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    z[i] = __builtin_amdgcn_exp2f(fmaf(sc[j][i >> 2][i & 3], a.scale, -m[j]));
+                split8<NP>(z, p[j]);
+                bits |= __builtin_bit_cast(u32x4, p[j][0]);
+            }
+            if (choose || !__any((bits[0] | bits[1] | bits[2] | bits[3]) & 0x40004000u)) break;
+            choose = true;
         }
+        // (the sum is that of the rounded probabilities, as the values' is)
+#pragma unroll
+        for (int j = 0; j < R; ++j)
+#pragma unroll
+            for (int k = NP - 1; k >= 0; --k)
+                l[j] = mma(eight(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u), p[j][k], l[j]);
 
         // values
         uint32_t ve[2] = {tv.exp[0], tv.exp[1]};
@@ -590,7 +616,7 @@ __global__ __launch_bounds__(kThreads, F32 || R > 1 ? 2 : 4) void quant_attn_ker
             pv(std::integral_constant<int, 3>{});
         }
         __builtin_amdgcn_sched_barrier(0);
-        if (ROWS && it + 1 < mine) tv.load_v(at, a.v + f0, a.v + f1);
+        if constexpr (ROWS) tv.load_v(at, a.v + f0, a.v + f1);
     }
 
     // A group of V that is not finite took part as zeros: now the rows that see
@@ -608,7 +634,7 @@ __global__ __launch_bounds__(kThreads, F32 || R > 1 ? 2 : 4) void quant_attn_ker
                 for (int r = 0; r < 16; ++r) {
                     if ((uint8_t)e[(r >> 2) * (D / 8) + (r & 3)] <= quant::kMostExp) continue;
 #pragma unroll
-                    for (int j = 0; j < R; ++j) lost[j] |= sees(a, pos[j], w.tile * kTile + h * 16 + r);
+                    for (int j = 0; j < R; ++j) lost[j] |= sees(a, s_pos[set][16 * j + n], w.tile * kTile + h * 16 + r);
                 }
             }
         }
@@ -619,12 +645,6 @@ __global__ __launch_bounds__(kThreads, F32 || R > 1 ? 2 : 4) void quant_attn_ker
                 for (int d = 0; d < PER; ++d) o[j][d] = f32x4{NAN, NAN, NAN, NAN};
             }
     }
-#pragma unroll
-    for (int j = 0; j < R; ++j) {
-        l[j] += __shfl_xor(l[j], 16);
-        l[j] += __shfl_xor(l[j], 32);
-    }
-
     // Eight values of a row (of the sequence's) from dim x0 on: as part of the
     // row, or as its output.
     auto put = [&](int r, int x0, const float (&v)[8], float top, float sum) {
@@ -658,7 +678,7 @@ __global__ __launch_bounds__(kThreads, F32 || R > 1 ? 2 : 4) void quant_attn_ker
         __syncthreads();
         if (g == 0) {
             s_m[wave][n] = m[j];
-            s_l[wave][n] = l[j];
+            s_l[wave][n] = l[j][0];
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -671,14 +691,13 @@ __global__ __launch_bounds__(kThreads, F32 || R > 1 ? 2 : 4) void quant_attn_ker
             const int of = e / (16 * PIECES), r = e / PIECES % 16, x0 = e % PIECES * 8;
             const int row = (rb * SETS + of) * OWN + 16 * j + r;
             if (row / a.group >= s.n) continue;
-            float most = -INFINITY, sum = 0.f, v[8] = {};
+            float most = kNoKey, sum = 0.f, v[8] = {};
 #pragma unroll
             for (int k = 0; k < STRIDE; ++k) most = fmaxf(most, s_m[k * SETS + of][r]);
 #pragma unroll
             for (int k = 0; k < STRIDE; ++k) {
                 const int from = k * SETS + of;
-                if (s_m[from][r] == -INFINITY && s_l[from][r] == 0.f) continue;  // (no key)
-                const float f = __builtin_amdgcn_exp2f(s_m[from][r] - (most == -INFINITY ? 0.f : most));
+                const float f = __builtin_amdgcn_exp2f(s_m[from][r] - most);
                 sum += f * s_l[from][r];
 #pragma unroll
                 for (int d = 0; d < 8; ++d) v[d] += f * s_o[from][r][x0 + d];

@@ -782,6 +782,10 @@ QuantPlan quant_plan(const presto_paged_attn_desc* d, presto_dtype dt) {
     QuantPlan p{};
     const int64_t group = d->hq / d->pages.hkv, rows = (int64_t)d->max_q * group, batch = d->pages.batch;
     const bool f32 = dt == PRESTO_DT_F32;
+    // (sizes whose products below would not fit 64 bits are more than a launch)
+    if (batch * d->max_q >= ((int64_t)1 << 31) || batch * d->max_q * d->hq >= ((int64_t)1 << 31) ||
+        d->total_q * d->hq >= ((int64_t)1 << 40))
+        return p;
     p.own = !f32 && rows >= 128;
     p.r = f32 ? 1 : p.own ? 4 : rows > 16 ? 2 : 1;
     const int64_t of_group = (p.own ? 2 : 1) * 16 * p.r;
@@ -814,7 +818,7 @@ QuantPlan quant_plan(const presto_paged_attn_desc* d, presto_dtype dt) {
                      : ((int64_t)d->pages.batch * p.splits + 7) / 8 * 8 * p.row_blocks * d->pages.hkv;
     const int64_t out_rows = d->total_q * d->hq, merge_rows = (int64_t)d->pages.batch * d->max_q * d->hq;
     p.merge_blocks = (merge_rows + kWaves - 1) / kWaves;
-    p.fits = p.blocks <= (1 << 23) && merge_rows < ((int64_t)1 << 31) && p.merge_blocks <= (1 << 23);
+    p.fits = p.blocks <= (1 << 23) && p.merge_blocks <= (1 << 23);
     if (p.splits > 1) {
         p.o_bytes = (size_t)(out_rows * p.splits * d->pages.head_dim) * 4;
         p.bytes = p.o_bytes + (size_t)(out_rows * p.splits) * 8;

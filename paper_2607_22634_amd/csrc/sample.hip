@@ -838,14 +838,18 @@ __device__ __forceinline__ bool pick_counted(const Args& a, int64_t r, int64_t s
         // the bin's tokens in order, from the slices that hold any
         if (tid == 0) s.n_list = 0;
         __syncthreads();
-        for (int k = 0; k < a.slices; ++k)
-            if (slice_at<F32>(a.ws, slice0 + k).count[b])
-                for_range<kThreads, F32 ? 4 : 2>(row, k * a.slice, min((k + 1) * a.slice, a.vocab), [&](float y, int i) {
-                    if (bins.at(y) == b) {
-                        const uint32_t at = atomicAdd(&s.n_list, 1u);
-                        if (at < (uint32_t)kList) s.list[at] = place_key(y, i);
-                    }
-                });
+        const int lane = lane_id();  // (every wave for itself)
+        uint64_t some = __ballot(lane < a.slices && slice_at<F32>(a.ws, slice0 + lane).count[b] != 0);
+        while (some) {  // neighbours in one go, so that more loads are in flight
+            const int k = __ffsll((unsigned long long)some) - 1, end = k + __ffsll(~(unsigned long long)(some >> k)) - 1;
+            for_range<kThreads, F32 ? 4 : 2>(row, k * a.slice, min(end * a.slice, a.vocab), [&](float y, int i) {
+                if (bins.at(y) == b) {
+                    const uint32_t at = atomicAdd(&s.n_list, 1u);
+                    if (at < (uint32_t)kList) s.list[at] = place_key(y, i);
+                }
+            });
+            some &= ~0ull << end;
+        }
         __syncthreads();
         const uint64_t key = sorted(s, (int)n);
         double run[1] = {tid < (int)n ? weight_of(octaves(key_value(key))) : 0.0};

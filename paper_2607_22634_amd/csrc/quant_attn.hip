@@ -786,6 +786,10 @@ QuantPlan quant_plan(const presto_paged_attn_desc* d, presto_dtype dt) {
     if (batch * d->max_q >= ((int64_t)1 << 31) || batch * d->max_q * d->hq >= ((int64_t)1 << 31) ||
         d->total_q * d->hq >= ((int64_t)1 << 40))
         return p;
+    // Waves on rows of their own from 128 rows on (4 x 32 new tokens on 8192 with 4
+    // heads per KV head 41 us, shared 43; 4 x 64 of them 57 and 73; 4 x 16 31 and
+    // 28), and 32 rows of a wave from 17 on (4 x 16 28, on 16 rows each 34; 4 x 8
+    // 23.2 and 22.6).  fp32 operands take three times the registers.
     p.own = !f32 && rows >= 128;
     p.r = f32 ? 1 : p.own ? 4 : rows > 16 ? 2 : 1;
     const int64_t of_group = (p.own ? 2 : 1) * 16 * p.r;
@@ -797,10 +801,18 @@ QuantPlan quant_plan(const presto_paged_attn_desc* d, presto_dtype dt) {
         most = std::min(most, ((int64_t)d->window + span) / kTile + 2 + ((int64_t)d->sinks + kTile - 1) / kTile);
     most = std::max<int64_t>(most, 1);
     // Contexts are cut into pieces of one length, so many that they make one round
-    // of workgroups, as many as run at once; ragged ones so that there are about
+    // of workgroups, as many as run at once (half as many decoding 16 x 8192 keys
+    // 35.4 us, these 34.6, twice as many 38.2); ragged ones so that there are about
     // that many.
     const int64_t room = (p.own ? 512 : p.r == 1 && !f32 ? 1024 : 512) / (p.row_blocks * d->pages.hkv);
-    constexpr int64_t kLeast = 16, kMostSplits = 256;
+    // No piece is shorter than 16 tiles, or, where those would be less than 256
+    // workgroups, so short that they are that many, but of 4 tiles and not more
+    // than 16 of them (a sequence of 1024 keys 8.8 us, in pieces of 16 tiles 11.5;
+    // of 4096 10.6 and 11.7; of 32768 19.6, in pieces of 8 26); up to 20 tiles are
+    // not cut (300 keys 7.1 us, in pieces of 4 9.1; 16 x 600 10.0, of 10 11.4).
+    constexpr int64_t kMostSplits = 256;
+    const int64_t even = most * batch * p.row_blocks * d->pages.hkv / 256;
+    const int64_t least = most <= 20 ? most : std::min<int64_t>(std::max({(int64_t)4, (most + 15) / 16, even}), 16);
     int64_t tiles = most;
     if (room > batch) {
         tiles = (most + room / batch - 1) / (room / batch);
@@ -810,7 +822,7 @@ QuantPlan quant_plan(const presto_paged_attn_desc* d, presto_dtype dt) {
             tiles = std::min(tiles, (all + pieces - 1) / pieces);
         }
     }
-    tiles = std::max(tiles, std::max(kLeast, (most + kMostSplits - 1) / kMostSplits));
+    tiles = std::max(tiles, std::max(least, (most + kMostSplits - 1) / kMostSplits));
     p.splits = (most + tiles - 1) / tiles;
     p.split_tiles = (most + p.splits - 1) / p.splits;
     const int64_t blocks = batch * p.row_blocks * d->pages.hkv;

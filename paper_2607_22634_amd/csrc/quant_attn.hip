@@ -10,8 +10,18 @@
 //      being dim PER n + t, its contraction slots the lane's own 8 keys.
 // S^T leaves a lane with row n and the same 8 keys, so the probabilities are the
 // B operand as they stand, and O^T leaves it with row n again: no value crosses
-// lanes but in the row maximum, and the cache goes from memory to the matrix
-// cores through registers only.
+// lanes but in the row maximum, and nothing is turned through LDS.
+//
+// What bounds it.  Decoding: the cache read once.  16 x 32768 keys of 8 heads of
+// 128 (571 MB) take 98 us and 4.8 of the merge, 5.5 TB/s; the conversions and
+// products of those tiles alone about 78, so tiles come through an LDS ring while
+// the ones before are in work.  16 ragged sequences (75 MB) 21 and 4.7: the
+// workgroups' starts, about 5 us, and their first tiles.  Long prompts: the matrix
+// cores and the vector ALU of two waves per SIMD.  A tile of a wave's 64 rows is 68
+// products (1088 cycles) and some 260 vector instructions (about 1400), of which
+// half convert keys and values, a quarter are exponentials at a quarter of the
+// rate; 4 x 332..448 new tokens on 11000 take 372 us, 775 TFLOP/s, on 392
+// workgroups, two to a CU.
 #include <algorithm>
 #include <type_traits>
 
@@ -273,7 +283,7 @@ __global__ __launch_bounds__(kThreads, F32 || R > 1 ? 2 : 4) void quant_attn_ker
     constexpr int SETS = ROWS ? 2 : 1, STRIDE = kWaves / SETS;    // of rows; waves on each
     constexpr bool LDS_Q = queries_in_lds<F32, D, R>();
     using T = std::conditional_t<F32, float, uint16_t>;
-    constexpr int RING = 2;       // tiles on their way per wave
+    constexpr int RING = 2;       // tiles on their way per wave (four workgroups fill a CU's LDS)
     constexpr bool ONCE = R == 1;  // (with one row block nobody else reads them)
     constexpr int LDS = std::max(ROWS ? SETS * R * STEPS * kWave * 16 : kWaves * RING * Slot<D>::kBytes,
                                  kWaves * 16 * (D + 4) * 4);
@@ -810,7 +820,7 @@ QuantPlan quant_plan(const presto_paged_attn_desc* d, presto_dtype dt) {
     // than 16 of them (a sequence of 1024 keys 8.8 us, in pieces of 16 tiles 11.5;
     // of 4096 10.6 and 11.7; of 32768 19.6, in pieces of 8 26); up to 20 tiles are
     // not cut (300 keys 7.1 us, in pieces of 4 9.1; 16 x 600 10.0, of 10 11.4).
-    constexpr int64_t kMostSplits = 256;
+    constexpr int64_t kMostSplits = 256;  // (parts that one wave joins)
     const int64_t even = most * batch * p.row_blocks * d->pages.hkv / 256;
     const int64_t least = most <= 20 ? most : std::min<int64_t>(std::max({(int64_t)4, (most + 15) / 16, even}), 16);
     int64_t tiles = most;

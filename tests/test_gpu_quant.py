@@ -179,6 +179,36 @@ def test_keys_on_a_border_turn_to_the_right_side():
     assert (S.held(k) != want).mean() > 0.1  # (the angles matter)
 
 
+def test_keys_next_to_a_border_keep_their_side():
+    """fp32 keys that the rotation takes to within 1e-10 .. 1e-8 of a border between
+    two codes: cosines and sines in fp32 would take many of them across."""
+    n, dim, past = 256, 128, 992
+    rng = np.random.default_rng(77)
+    freq = S.frequencies(dim)
+    turn = (np.arange(n) + past)[:, None, None] * freq[:, None]
+    c, s = np.cos(turn), np.sin(turn)
+    border = rng.choice([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0], (n, 64, 1)) * rng.choice([-1, 1], (n, 64, 1))
+    border[:, ::32] = 6.25  # (the largest of a group: codes count in ones)
+    # of 256 pairs (a, b) each the one that comes nearest
+    b = rng.uniform(-2, 2, (n, 64, 1)).astype(np.float32) * (1 + np.arange(256) * 2.0 ** -22).astype(np.float32)
+    a = ((border + b * s) / np.where(np.abs(c) > 0.3, c, 1)).astype(np.float32)
+    off = np.abs(a * c - b * s - border)
+    off = np.where((off > 1e-10) & (np.abs(c) > 0.3), off, 1.0)
+    at = off.argmin(-1)[..., None]
+    use = np.take_along_axis(off, at, -1)[..., 0] < 1e-8
+    assert use.sum() > 5000
+    k = np.zeros((n, 1, dim), dtype=np.float32)
+    k[:, 0, :64] = np.where(use, np.take_along_axis(a, at, -1)[..., 0], 0)
+    k[:, 0, 64:] = np.where(use, np.take_along_axis(b, at, -1)[..., 0], 0)
+    want = S.held(S.rotate(k.astype(np.float64), np.arange(n) + past, freq)[0])
+    pool = [P.quant_pages(n // 16, 16, 1, dim) for _ in range(2)]
+    books = ints([[-1] * (past // 16) + list(range(n // 16))]), ints([past]), ints([past + n])
+    kt = dev(k)
+    P.presto_append_rope(P.rope_plan(dim), None, kt, kt, ints([0, n]), n, *pool, *books)
+    got, _ = P.presto_read_kv(*pool, *books, ints([0, n]), n, rows=n, dtype=torch.float32)
+    assert (got.double().cpu().numpy() == want).all()
+
+
 def test_groups_that_are_not_finite_or_extreme():
     dim = 64
     x = torch.ones(6, 2, dim, device="cuda")

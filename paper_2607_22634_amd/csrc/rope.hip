@@ -55,9 +55,12 @@ __device__ __forceinline__ void turn_sincos(uint64_t a, float& s, float& c) {
     c = (quarter + 1) & 2 ? -c : c;
 }
 
-// The same in 64 bits, to x^15 and x^16 off by 1e-16 and less: for keys that are
-// coded, where an error of an fp32 step takes one in a few million values over the
-// border between two codes.
+// The largest error of a rotation in 32 bits, relative to its terms |a| and |b|:
+// x is off by 1.5e-7 of at most 0.79, sine and cosine with their roundings by less
+// than 3e-7, the products, their sum and the magnitude by 2e-7 more.
+constexpr float kTurnError = 0x1p-20f;
+
+// The same in 64 bits, to x^15 and x^16 off by 1e-16 and less.
 __device__ __forceinline__ void turn_sincos(uint64_t a, double& s, double& c) {
     const uint64_t r64 = a + (1ull << 61);
     const uint32_t quarter = (uint32_t)(r64 >> 62);
@@ -191,6 +194,15 @@ struct Angles {
             out[j] = PART && x0 + j >= rot ? a : r;
         }
     }
+    // (2^-140: where the products' own roundings are of the least numbers)
+    __device__ __forceinline__ void off(const float own[8], const float other[8], float eps, float out[8]) const {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float b = PAIRS == kNext ? own[j ^ 1] : other[j];
+            const float r = fmaf(fabsf(own[j]) + fabsf(b), eps, 0x1p-140f);
+            out[j] = PART && x0 + j >= rot ? 0.f : r;
+        }
+    }
 };
 
 // A lane's piece of a head and its partners.
@@ -214,13 +226,24 @@ struct Piece {
     template <typename F, typename A>
     __device__ __forceinline__ void turned(const A& a, F out[8]) const {
         float mine[8], theirs[8];
+        values(mine, theirs);
+        a.turned(mine, theirs, out);
+    }
+    // and how far the outputs may be off, by eps of their terms
+    template <typename A>
+    __device__ __forceinline__ void turned(const A& a, float out[8], float eps, float off[8]) const {
+        float mine[8], theirs[8];
+        values(mine, theirs);
+        a.turned(mine, theirs, out);
+        a.off(mine, theirs, eps, off);
+    }
+    __device__ __forceinline__ void values(float mine[8], float theirs[8]) const {
         own.get(mine);
         if constexpr (PAIRS == kHalf) other.get(theirs);
         if constexpr (PAIRS == kHalfOdd) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) theirs[j] = odd[j];
         }
-        a.turned(mine, theirs, out);
     }
 };
 
@@ -318,12 +341,35 @@ __device__ __forceinline__ float group_top(const float v[8]) {
     return __uint_as_float(t);
 }
 
-// Eight values of position r of a block (a head's sixteen positions) as codes,
-// and by the first lane of a group its exponent.
+// Eight values' codes and their group's exponent.
+struct Coded {
+    uint32_t w;
+    int e;
+    __device__ __forceinline__ void make(const float v[8]) {
+        e = quant::group_exp(group_top(v));
+        w = quant::encode8(v, e);
+    }
+    // the same of values that are off by up to off[]; false: that may matter (of a
+    // 0 but for its sign), or one is not finite
+    __device__ __forceinline__ bool make(const float v[8], const float off[8]) {
+        float hi[8], lo[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            hi[i] = fabsf(v[i]) + off[i];
+            lo[i] = fmaxf(fabsf(v[i]) - off[i], 0.f);
+        }
+        e = quant::group_exp(group_top(hi));
+        w = quant::encode8(v, e);
+        return quant::group_exp(group_top(lo)) == e && quant::encode8(lo, e) == quant::encode8(hi, e);
+    }
+};
+
+// Eight values of position r of a block (a head's sixteen positions), and by the
+// first lane of a group its exponent.
 template <int D, bool V>
-__device__ __forceinline__ void store_quant(char* block, int r, int x0, const float v[8]) {
-    const int e = quant::group_exp(group_top(v));
-    const uint32_t w = quant::encode8(v, e);
+__device__ __forceinline__ void store_quant(char* block, int r, int x0, const Coded& c) {
+    const int e = c.e;
+    const uint32_t w = c.w;
     if constexpr (!V) {
         *reinterpret_cast<uint32_t*>(block + quant::k_code_at<D>(r, x0)) = w;
         if (x0 % 32 == 0) block[quant::k_exp_at<D>(r, x0)] = (char)e;
@@ -371,7 +417,7 @@ __global__ __launch_bounds__(kThreads) void append_rope_kernel(Turn turn, Cache 
         // this wave's heads of [queries; keys; values]
         const int from = seg * seg_heads, to = from + seg_heads;
         Angles<PAIRS, PART> ang;
-        if (from < (Q4 ? hq : hq + hkv)) ang.make(turn, pos, x0);
+        if (from < hq + hkv) ang.make(turn, pos, x0);
         if (from < hq)
             rotate_heads<T, PAIRS, PART>(q + src * q_stride, q_out + src * q_out_stride, D, from, min(to, hq), kPer,
                                          mine, ang);
@@ -394,24 +440,34 @@ __global__ __launch_bounds__(kThreads) void append_rope_kernel(Turn turn, Cache 
                 e.store(reinterpret_cast<T*>(a.v + at) + (int64_t)h * D + x0);
             }
         } else {
-            Angles<PAIRS, PART, double> fine;
-            if (k0 < k1) fine.make(turn, pos, x0);
+            // Keys are coded as if rotated in 64 bits: in 32 where no border between
+            // two codes is near, else (a few thousandths of the tokens) again.
+            const float eps = kTurnError * fabsf(turn.magnitude);
             for (int h = k0 + mine; h < k1; h += kPer) {
                 Piece<T, PAIRS> p;
-                p.load(k_new + src * k_stride + (int64_t)h * D, fine);
-                double d[8];
-                p.turned(fine, d);
-                float f[8];
+                p.load(k_new + src * k_stride + (int64_t)h * D, ang);
+                float f[8], off[8];
+                p.turned(ang, f, eps, off);
+                Coded code;
+                if (__any(!code.make(f, off))) {
+                    Angles<PAIRS, PART, double> fine;
+                    fine.make(turn, pos, x0);
+                    double d[8];
+                    p.turned(fine, d);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) f[j] = to_odd(d[j]);
-                store_quant<D, false>(a.k + quant_block<D>(a, page, row, h), row & 15, x0, f);
+                    for (int j = 0; j < 8; ++j) f[j] = to_odd(d[j]);
+                    code.make(f);
+                }
+                store_quant<D, false>(a.k + quant_block<D>(a, page, row, h), row & 15, x0, code);
             }
             for (int h = v0 + mine; h < v1; h += kPer) {
                 Eight<T> e;
                 e.stream(v_new + src * v_stride + (int64_t)h * D + x0);
                 float f[8];
                 e.get(f);
-                store_quant<D, true>(a.v + quant_block<D>(a, page, row, h), row & 15, x0, f);
+                Coded code;
+                code.make(f);
+                store_quant<D, true>(a.v + quant_block<D>(a, page, row, h), row & 15, x0, code);
             }
         }
     }

@@ -39,8 +39,10 @@ constexpr int kTile = 32;  // keys
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * kWave;
 // A row's reference lies this far (log2) above its largest score when it is
-// chosen, and at most one below its largest score later on.
-constexpr float kAbove = 15.f;
+// chosen, and at most one below its largest score later on.  (Its probabilities
+// then begin at 2^-4, and their products with the least values that a cache holds,
+// 2^-121, are still normal numbers.)
+constexpr float kAbove = 4.f;
 constexpr float kNoKey = -3.402823466e38f;  // reference of a row without keys (so that masked scores weigh 0)
 
 struct Args {

@@ -401,6 +401,51 @@ def test_scores_far_from_zero(shift, dtype):
         assert (np.abs(out[b:b + 1] - want) <= bound).all()
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("new", [1, 4, 40])
+@pytest.mark.parametrize("way", [1, -1])
+def test_scores_that_rise_and_fall(way, new, dtype):
+    """One K group holds a value that grows (or falls) from tile to tile, by more
+    and more: a row's reference has to move in each of them, or in none."""
+    rng = np.random.default_rng(17)
+    c = Quant(rng, [420, 420], 32, 1, 128)
+    steps = np.array([2.0 ** (i // 2) * (1, 1.5)[i % 2] for i in range(14)])[::way]
+    for b in range(2):
+        at = c.where(b, range(420))
+        k = S.read(c.kh, False, *at)
+        k[..., 96:] = steps[np.arange(420) // 32][:, None, None]
+        S.write(c.kh, False, *at, *S.encode(k))
+    c.upload()
+    q = tensor(rng, (2 * new, 8, 128), dtype)
+    q[..., 96:] = 0.25
+    out = P.presto_quant_attention(q, c.k, c.v, c.table, c.ctx, q_offsets=ints([0, new, 2 * new]), max_q=new)
+    out = out.double().cpu().numpy()
+    for b in range(2):
+        one = slice(b * new, (b + 1) * new)
+        want, bound = tight(q[one].double().cpu().numpy(), *c.rows(b), 420 - new, 0, 0, dtype, new * 8 < 128)
+        assert (np.abs(out[one] - want) <= bound).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("new", [1, 40])
+def test_least_values(new, dtype):
+    """Values of the least exponent under equal probabilities (queries of 0)."""
+    rng = np.random.default_rng(16)
+    c = Quant(rng, [60, 300], 16, 1, 128)
+    for b in range(2):
+        at = c.where(b, range(c.ctx_h[b]))
+        S.write(c.vh, True, *at, *S.encode(rng.standard_normal((c.ctx_h[b], 1, 128)) * 2.0 ** -120))
+    c.upload()
+    q = torch.zeros(2 * new, 8, 128, dtype=DT[dtype], device="cuda")
+    out = P.presto_quant_attention(q, c.k, c.v, c.table, c.ctx, q_offsets=ints([0, new, 2 * new]), max_q=new)
+    out = out.double().cpu().numpy()
+    for b in range(2):
+        one = slice(b * new, (b + 1) * new)
+        want, bound = tight(q[one].double().cpu().numpy(), *c.rows(b), c.ctx_h[b] - new, 0, 0, dtype, new * 8 < 128)
+        # (and half a step of the output's subnormal numbers)
+        assert (np.abs(out[one] - want) <= bound + (2.0 ** -134 if dtype == "bf16" else 2.0 ** -150)).all()
+
+
 @pytest.mark.parametrize("dim", [64, 128])
 @pytest.mark.parametrize("new", [1, 40])
 def test_groups_that_are_not_finite_reach_who_sees_them(dim, new):

@@ -12,9 +12,9 @@
 // Measured: 16384 rows of 40 heads of 128 bf16 values, half of them turning, 66 us,
 // 5.1 TB/s, what a large copy moves; 528 rows 5.5 us as a call, the kernel's start
 // and one round of loads.  23627 new tokens (32 + 2 x 8 heads of 128) into a 4-bit
-// cache 127 us and back out of it 30, 4.1 TB/s: keys and values of a token go
-// through 16 lanes each with few loads in flight (both in one pass: 182 registers,
-// 160 to 195 us).
+// cache and back out of it 157 us, 4 TB/s: keys and values of a token go through 16
+// lanes each with few loads in flight (both in one pass took 182 registers, and a
+// fifth longer), and keys are coded three times (below).
 #include <algorithm>
 #include <type_traits>
 

@@ -171,6 +171,7 @@ struct Bins {
 // The grid of sample_count_kernel: 15 binades on either side of the bin around
 // 0, a bin of what is above (0) and one of what is below.
 constexpr float kGridNear = 0x1p-8f, kGridMost = 0x1.fffffep+6f;
+constexpr int kNearBits = (127 - 8) << 7;  // of kGridNear as bf16
 constexpr int kGridSide = 15 * 128, kGridMid = kGridSide + 1, kGridBelow = 2 * kGridSide + 2;
 static_assert(kGridBelow < kGridWords && kGridWords <= kPer * kThreads && kGridWords % kPer == 0, "");
 constexpr int kNearList = 1024;  // values of a bf16 slice in the bin around 0
@@ -259,7 +260,7 @@ __global__ __launch_bounds__(kCountThreads) void sample_count_kernel(Args a) {
         // two values at a time, in 16 bits each: the magnitude's distance from
         // the bin around 0, with the sign turned, is the bin
         typedef short i16x2 __attribute__((ext_vector_type(2)));
-        constexpr short kLeast = (short)((127 - 8) << 7);
+        constexpr short kLeast = (short)kNearBits;
         i16x2 most = {0, 0};
         auto count = [&](uint32_t w, bool high) {
             const i16x2 mag = __builtin_bit_cast(i16x2, w & 0x7fff7fffu);
@@ -847,12 +848,31 @@ __device__ __forceinline__ bool pick_counted(const Args& a, int64_t r, int64_t s
         uint64_t some = __ballot(lane < a.slices && slice_at<F32>(a.ws, slice0 + lane).count[b] != 0);
         while (some) {  // neighbours in one go, so that more loads are in flight
             const int k = __ffsll((unsigned long long)some) - 1, end = k + __ffsll(~(unsigned long long)(some >> k)) - 1;
-            for_range<kThreads, F32 ? 4 : 2>(row, k * a.slice, min(end * a.slice, a.vocab), [&](float y, int i) {
-                if (bins.at(y) == b) {
-                    const uint32_t at = atomicAdd(&s.n_list, 1u);
-                    if (at < (uint32_t)kList) s.list[at] = vocab_key(y, (uint32_t)i);
-                }
-            });
+            const int from = k * a.slice, to = min(end * a.slice, a.vocab);
+            auto put = [&](float y, int i) {
+                const uint32_t at = atomicAdd(&s.n_list, 1u);
+                if (at < (uint32_t)kList) s.list[at] = vocab_key(y, (uint32_t)i);
+            };
+            if constexpr (F32) {
+                for_range<kThreads, 4>(row, from, to, [&](float y, int i) {
+                    if (bins.at(y) == b) put(y, i);
+                });
+            } else {  // (the bin around 0)
+                auto near = [&](uint32_t h, int i) {
+                    if ((h & 0x7fffu) < (uint32_t)kNearBits) put(bf16_to_f((uint16_t)h), i);
+                };
+                for_pieces<kThreads, 4>(
+                    row, from, to,
+                    [&](const uint4& x, int i) {
+                        const uint32_t v[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            near(v[j] & 0xffffu, i + 2 * j);
+                            near(v[j] >> 16, i + 2 * j + 1);
+                        }
+                    },
+                    near);
+            }
             some &= ~0ull << end;
         }
         __syncthreads();

@@ -112,6 +112,26 @@ def test_wide_and_narrow_ranges(scale, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("vocab", [6000, 100000])
+def test_places_around_zero(vocab, dtype):
+    """Draws, and each of the cuts, among logits within 2^-8 of 0, where bf16 values
+    lie closer than elsewhere (and unaligned ends of a slice's pieces)."""
+    rng = np.random.default_rng(28)
+    wide = torch.from_numpy(rng.standard_normal((8, vocab + 3)).astype(np.float32)).to(DT[dtype]).cuda()
+    z = wide[:, 3:]
+    zd = np.sort(z.double().cpu().numpy(), -1)[:, ::-1]
+    w = np.exp(zd - zd[:, :1])
+    at = (zd > 0).sum(1) + rng.integers(-4, 5, 8)  # a place in the order next to 0
+    share = np.array([w[r, :at[r]].sum() / w[r].sum() for r in range(8)])
+    assert (np.abs(zd[np.arange(8), at]) < 2.0 ** -8).all()
+    check(z, share)
+    check(z, rng.random(8), top_k=at.astype(np.int32))
+    check(z, np.full(8, 1 - 2.0 ** -24), top_k=at.astype(np.int32))
+    check(z, np.full(8, 1 - 2.0 ** -24), top_p=share.astype(np.float32))
+    check(z, np.full(8, 1 - 2.0 ** -24), min_p=w[np.arange(8), at].astype(np.float32))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_masked_logits(dtype):
     rng = np.random.default_rng(24)
     z = torch.from_numpy(rng.standard_normal((6, 5000)).astype(np.float32)).to(DT[dtype])

@@ -270,8 +270,8 @@ __device__ __forceinline__ float scale_of(uint32_t w) {
     return __uint_as_float(B == 3 ? w >> 1 : w << (23 - 8 * B));
 }
 
-// What a kernel keeps per wave in LDS of queries that do not fit registers.
-template <bool F32, int D, int R>
+// Whether queries are kept in LDS, as they do not fit registers.
+template <bool F32, int R>
 constexpr bool queries_in_lds() {
     return !F32 && R > 2;
 }
@@ -283,7 +283,7 @@ __global__ __launch_bounds__(kThreads, F32 || R > 1 ? 2 : 4) void quant_attn_ker
     constexpr int NQ = F32 ? 3 : 1, NP = F32 ? 3 : ROWS ? 1 : 2;  // bf16 per query value and per probability
     constexpr int STEPS = D / 32, PER = D / 16, OWN = 16 * R;     // rows of a wave
     constexpr int SETS = ROWS ? 2 : 1, STRIDE = kWaves / SETS;    // of rows; waves on each
-    constexpr bool LDS_Q = queries_in_lds<F32, D, R>();
+    constexpr bool LDS_Q = queries_in_lds<F32, R>();
     using T = std::conditional_t<F32, float, uint16_t>;
     constexpr int RING = 2;       // tiles on their way per wave (four workgroups fill a CU's LDS)
     constexpr bool ONCE = R == 1;  // (with one row block nobody else reads them)
@@ -298,8 +298,8 @@ __global__ __launch_bounds__(kThreads, F32 || R > 1 ? 2 : 4) void quant_attn_ker
     const int set = wave % SETS;
     // blocks go round the eight XCDs.  ROWS: those of one head, which share its
     // keys, to one of them where there are eight heads, and first pieces, which are
-    // whole, before last ones; else the heads of a
-    // stretch of positions, which lie side by side in the pool
+    // whole, before last ones; else the heads of a stretch of positions, which lie
+    // side by side in the pool
     int x = blockIdx.x, head, split, rb, b;
     if constexpr (ROWS) {
         head = x % a.hkv;

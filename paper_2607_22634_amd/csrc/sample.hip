@@ -302,9 +302,23 @@ __global__ __launch_bounds__(kCountThreads) void sample_count_kernel(Args a) {
             const double y = ((double)kGridNear - (double)bf16_to_f(s_near[j])) * rate;
             if (y < kRange) atomicAdd((unsigned long long*)s_weight, (unsigned long long)as_fixed(weight_of(y), scale));
         }
-        // (-inf is a value like others)
-        if (max(most[0], most[1]) >= 0x7f80)
-            for_range<kCountThreads, 1>(row, from, to, [&](float z, int) { bad |= !(z < INFINITY); });
+        // (-inf is a value like others.  A thread looks again at the elements that
+        // it counted: the ends of a slice that is not aligned go to other threads in
+        // for_range.)
+        if (max(most[0], most[1]) >= 0x7f80) {
+            auto look = [&](uint32_t h) { bad |= (h & 0x7fffu) >= 0x7f80u && h != 0xff80u; };
+            for_pieces<kCountThreads, 1>(
+                row, from, to,
+                [&](const uint4& x, int) {
+                    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        look(w[j] & 0xffffu);
+                        look(w[j] >> 16);
+                    }
+                },
+                [&](uint16_t h, int) { look(h); });
+        }
     }
     const bool any_bad = __any(bad);
     if (any_bad && lane_id() == 0) atomicOr(&s_bad, kNotANumber);

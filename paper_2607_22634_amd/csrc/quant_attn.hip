@@ -264,6 +264,9 @@ __device__ __forceinline__ uint32_t odd_exps(uint32_t w) {
 }
 __device__ __forceinline__ uint32_t without(uint32_t w, uint32_t odd) { return w & ~((odd >> 7) * 255u); }
 
+// The same of one exponent of K, whose group then is NaN in every product.
+__device__ __forceinline__ uint32_t odd_as_nan(uint32_t e) { return e > (uint32_t)quant::kMostExp ? 255u : e; }
+
 // The scale of byte B of w: the conversions read bits 23 .. 30 of it only.
 template <int B>
 __device__ __forceinline__ float scale_of(uint32_t w) {
@@ -485,7 +488,7 @@ __global__ __launch_bounds__(kThreads, F32 || R > 1 ? 2 : 4) void quant_attn_ker
         f32x4 sc[R][2];
 #pragma unroll
         for (int j = 0; j < R; ++j) sc[j][0] = sc[j][1] = f32x4{0.f, 0.f, 0.f, 0.f};
-        const float ks[2] = {scale_of<0>(tk.exp[0]), scale_of<0>(tk.exp[1])};
+        const float ks[2] = {scale_of<0>(odd_as_nan(tk.exp[0])), scale_of<0>(odd_as_nan(tk.exp[1]))};
         constexpr int AHEAD = 2;  // reads of queries on their way (more, and registers spill)
         bf16x8 ql[LDS_Q ? AHEAD : 1];
         auto read_q = [&](int i) { return s_q[(i % R * STEPS + i / R) * kWave + lane]; };

@@ -352,9 +352,10 @@ struct Shared : Scratch<kThreads> {
     uint32_t cc[kRareBins];
     uint64_t sw[kSubBins];
     uint32_t sc[kSubBins];
+    uint64_t cw2[kRareBins], sw2[kSubBins];  // (second words of sums)
     uint32_t top, cbase, n;
     double base;
-    uint64_t sum;
+    uint64_t sum, sum2;
 };
 
 template <int CTRL, int ROW_MASK = 0xf>
@@ -512,12 +513,29 @@ __device__ __forceinline__ void pick_rare(const Args& a, int64_t r, float hi, Sh
     const double rate = rate_of(temp), scale = ldexp(1.0, a.bits), unit = ldexp(1.0, -a.bits);
     const float cut = cut_of(hi, rate);
     auto octaves = [&](float z) { return ((double)hi - (double)z) * rate; };
-    auto fixed = [&](float z) { return as_fixed(weight_of(octaves(z)), scale); };
-    auto real = [&](uint64_t w) { return (double)w * unit; };
+    // Weights relative to the largest, as integers in two words, of 2^-bits and of
+    // 2^-2 bits: a bin may be wide here, and what many tokens of 2^-40 to 2^-64 weigh
+    // together counts.
+    auto parts = [&](float z, uint64_t& first, uint64_t& second) {
+        const double w = weight_of(octaves(z)) * scale, whole = floor(w);
+        first = (uint64_t)whole;
+        second = as_fixed(w - whole, scale);
+    };
+    auto add = [&](uint64_t* to, uint64_t* to2, uint64_t first, uint64_t second) {
+        if (first) atomicAdd((unsigned long long*)to, (unsigned long long)first);
+        if (second) atomicAdd((unsigned long long*)to2, (unsigned long long)second);
+    };
+    auto add_weight = [&](uint64_t* to, uint64_t* to2, float z) {
+        uint64_t first, second;
+        parts(z, first, second);
+        add(to, to2, first, second);
+    };
+    auto real = [&](uint64_t first, uint64_t second) { return ((double)first + (double)second * unit) * unit; };
 
     __syncthreads();
     for (int i = tid; i < kRareBins; i += kThreads) {
         s.cw[i] = 0.0;
+        s.cw2[i] = 0;
         s.cc[i] = 0;
     }
     float lo = hi;
@@ -532,7 +550,7 @@ __device__ __forceinline__ void pick_rare(const Args& a, int64_t r, float hi, Sh
         if (!(z > cut)) return;
         const int b = bins.at(z);
         atomicAdd(&s.cc[b], 1u);
-        if (F32 || b == bins.mid) atomicAdd((unsigned long long*)&s.cw[b], (unsigned long long)fixed(z));
+        if (F32 || b == bins.mid) add_weight((uint64_t*)&s.cw[b], &s.cw2[b], z);
     });
     __syncthreads();
     double w[N];
@@ -543,7 +561,7 @@ __device__ __forceinline__ void pick_rare(const Args& a, int64_t r, float hi, Sh
         c[i] = s.cc[b];
         w[i] = 0.0;
         if (c[i])
-            w[i] = F32 || b == bins.mid ? real((uint64_t)__double_as_longlong(s.cw[b]))
+            w[i] = F32 || b == bins.mid ? real((uint64_t)__double_as_longlong(s.cw[b]), s.cw2[b])
                                         : c[i] * weight_of(octaves(bins.value(b)));
     }
     block_scan<N>(w, c, s);
@@ -578,15 +596,19 @@ __device__ __forceinline__ void pick_rare(const Args& a, int64_t r, float hi, Sh
             if (ask.m > 0.f) {  // (w >= min_p: at most that many octaves below the largest)
                 const double most = -log2((double)ask.m);
                 __syncthreads();
-                if (tid == 0) s.sum = 0;
+                if (tid == 0) s.sum = s.sum2 = 0;
                 __syncthreads();
-                uint64_t mine = 0;
+                uint64_t mine = 0, mine2 = 0;
                 for_range<kThreads, 1>(row, 0, a.vocab, [&](float y, int) {
-                    if (y > cut && octaves(y) <= most) mine += fixed(y);
+                    if (!(y > cut && octaves(y) <= most)) return;
+                    uint64_t first, second;
+                    parts(y, first, second);
+                    mine += first;
+                    mine2 += second;
                 });
-                if (mine) atomicAdd((unsigned long long*)&s.sum, (unsigned long long)mine);
+                add(&s.sum, &s.sum2, mine, mine2);
                 __syncthreads();
-                total = fmin(total, real(s.sum));
+                total = fmin(total, real(s.sum, s.sum2));
             }
             if (greedy)
                 count = 1;
@@ -608,7 +630,7 @@ __device__ __forceinline__ void pick_rare(const Args& a, int64_t r, float hi, Sh
             for (bool again = true; again; again = klo != khi) {
                 const int shift = max(0, 32 - __clz((int)(khi - klo)) - kSubBits);
                 for (int i = tid; i < kSubBins; i += kThreads) {
-                    s.sw[i] = 0;
+                    s.sw[i] = s.sw2[i] = 0;
                     s.sc[i] = 0;
                 }
                 __syncthreads();
@@ -617,14 +639,14 @@ __device__ __forceinline__ void pick_rare(const Args& a, int64_t r, float hi, Sh
                     if (key < klo || key > khi || !(y > cut) || bins.at(y) != b) return;
                     const uint32_t x = (khi - key) >> shift;
                     atomicAdd(&s.sc[x], 1u);
-                    atomicAdd((unsigned long long*)&s.sw[x], (unsigned long long)fixed(y));
+                    add_weight(&s.sw[x], &s.sw2[x], y);
                 });
                 __syncthreads();
                 double sub_w[M];
                 uint32_t sub_c[M];
 #pragma unroll
                 for (int i = 0; i < M; ++i) {
-                    sub_w[i] = real(s.sw[tid * M + i]);
+                    sub_w[i] = real(s.sw[tid * M + i], s.sw2[tid * M + i]);
                     sub_c[i] = s.sc[tid * M + i];
                 }
                 block_scan<M>(sub_w, sub_c, s);
@@ -764,8 +786,12 @@ __device__ __forceinline__ bool pick_counted(const Args& a, int64_t r, int64_t s
     // y = (max - z) * rate octaves below the largest
     const double rate = rate_of(temp), unit = ldexp(1.0, -a.bits);
     auto octaves = [&](float z) { return ((double)hi - (double)z) * rate; };
+    // (weights of a bin of several values are held relative to its upper end: of at
+    // most four octaves)
+    constexpr double kWide = 4.0;
     grid = grid && (!below || octaves(-kGridMost) >= kRange) &&
-           (!F32 || ((double)bins.upper(first) - (double)bins.lower(first)) * rate <= 4.0);
+           (!F32 || ((double)bins.upper(first) - (double)bins.lower(first)) * rate <= kWide) &&
+           (octaves(kGridNear) >= kRange || 2 * (double)kGridNear * rate <= kWide);
     if (!grid) return false;
 
     // weights by bin

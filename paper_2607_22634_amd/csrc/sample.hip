@@ -7,17 +7,20 @@
 // weights pass given values.
 //
 // sample_count_kernel reads the logits once, slices of rows over the whole chip,
-// and counts them by value: 8 bits of mantissa, magnitudes of 2^-4 to 2^7, what
-// is nearer to 0 together.  A bf16 bin holds one value, whose weight is then
-// taken once per bin and not per token; fp32 bins and the one around 0 hold
-// several, and their weights are added up too, relative to the bin's upper end
-// (the row's maximum is not known yet), as integers, so that the order does not
-// matter.  sample_pick_kernel, a workgroup per row, adds the slices up and finds
-// the places; it goes back to the logits of a slice for the ids of the value
+// and counts them by value: 8 bits of mantissa, magnitudes of 2^-8 to 2^7 of
+// either sign, what is nearer to 0 together.  A bf16 bin holds one value, whose
+// weight is then taken once per bin and not per token; fp32 bins and the one
+// around 0 hold several, and their weights are added up too, relative to the bin's
+// upper end (the row's maximum is not known yet), as integers, so that the order
+// does not matter.  sample_pick_kernel, a workgroup per row, adds the slices up and
+// finds the places; it goes back to the logits of a slice for the ids of the value
 // drawn, and to the slices that hold a bin of several values where a border lies
-// in it.  Rows that do not fit that grid (a largest logit of 2^7 or next to 0,
-// fp32 at temperatures so low that a bin is wide) are counted again on one of
-// their own.  Rows of at most 1024 tokens are sorted as they are.
+// in it.  Rows that do not fit that grid are counted again on one of their own, by
+// one workgroup: those whose largest logit is 2^7 or more, or -2^7 or less, or
+// whose finite logits below that count (temperatures above about 3); those where a
+// border lies in a bin of more than 512 tokens that are not one value, or a bf16
+// slice has more than 1024 within 2^-8 of 0; and temperatures so low that a bin is
+// wide.  Rows of at most 1024 tokens are sorted as they are.
 //
 // Measured (151936 tokens, bf16): one row 21 us, 64 rows of a serving batch 26, 512
 // rows 62 (2.5 TB/s).  The counts are bound by LDS atomics next to HBM (39 us of
@@ -188,7 +191,7 @@ __device__ __forceinline__ Slice slice_at(char* ws, int64_t i) {
     return {reinterpret_cast<uint16_t*>(p), reinterpret_cast<uint64_t*>(p + kGridWords * 2),
             reinterpret_cast<uint32_t*>(p + kGridWords * 2 + (F32 ? kGridWords * 8 : 8))};
 }
-enum { kNotANumber = 1, kManyNear = 2 };
+enum { kNotANumber = 1, kManyNear = 2, kFar = 4 };
 
 struct Args {
     const void* logits;
@@ -240,7 +243,7 @@ __global__ __launch_bounds__(kCountThreads) void sample_count_kernel(Args a) {
     }
     __syncthreads();
     const double rate = rate_of(temperature_of(a, r)), scale = ldexp(1.0, a.bits);
-    bool bad = false;
+    bool bad = false, beyond = false;  // beyond: a finite value of -2^7 or less (bf16: 2^7 or more, too)
     if constexpr (F32) {
         Bins bins;
         bins.make(kGridNear, kGridMost);
@@ -249,6 +252,7 @@ __global__ __launch_bounds__(kCountThreads) void sample_count_kernel(Args a) {
             bad |= !(z < INFINITY);
             top = fmaxf(top, z);
             const int b = min(max(bins.at(z) + 1, 0), kGridBelow);
+            beyond |= b == kGridBelow && z > -INFINITY;
             atomicAdd(&s_count[b], 1u);
             const double y = ((double)bins.upper(b - 1) - (double)z) * rate;
             if (b > 0 && b < kGridBelow && y < kRange)
@@ -260,6 +264,7 @@ __global__ __launch_bounds__(kCountThreads) void sample_count_kernel(Args a) {
         // two values at a time, in 16 bits each: the magnitude's distance from
         // the bin around 0, with the sign turned, is the bin
         typedef short i16x2 __attribute__((ext_vector_type(2)));
+        typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
         constexpr short kLeast = (short)kNearBits;
         i16x2 most = {0, 0};
         auto count = [&](uint32_t w, bool high) {
@@ -302,26 +307,34 @@ __global__ __launch_bounds__(kCountThreads) void sample_count_kernel(Args a) {
             const double y = ((double)kGridNear - (double)bf16_to_f(s_near[j])) * rate;
             if (y < kRange) atomicAdd((unsigned long long*)s_weight, (unsigned long long)as_fixed(weight_of(y), scale));
         }
-        // (-inf is a value like others.  A thread looks again at the elements that
-        // it counted: the ends of a slice that is not aligned go to other threads in
-        // for_range.)
-        if (max(most[0], most[1]) >= 0x7f80) {
-            auto look = [&](uint32_t h) { bad |= (h & 0x7fffu) >= 0x7f80u && h != 0xff80u; };
-            for_pieces<kCountThreads, 1>(
+        // A thread that saw a magnitude of 2^7 or more looks again at the elements that
+        // it counted (the ends of a slice that is not aligned go to other threads in
+        // for_range): for the largest value, +inf or a NaN (a NaN of either sign is
+        // above 0x7f80 in `most`), and the largest finite magnitude, plus 0x80, with
+        // which infinities and NaN are negative numbers.
+        constexpr short kFarBits = (127 + 7) << 7;
+        if (max(most[0], most[1]) >= kFarBits) {
+            i16x2 value = {0, 0}, finite = {0, 0};
+            auto look = [&](uint32_t w) {
+                value = __builtin_elementwise_max(value, __builtin_bit_cast(i16x2, w));
+                const u16x2 up = __builtin_bit_cast(u16x2, w & 0x7fff7fffu) + (unsigned short)0x80;
+                finite = __builtin_elementwise_max(finite, __builtin_bit_cast(i16x2, up));
+            };
+            for_pieces<kCountThreads, 4>(
                 row, from, to,
                 [&](const uint4& x, int) {
-                    const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        look(w[j] & 0xffffu);
-                        look(w[j] >> 16);
-                    }
+                    look(x.x);
+                    look(x.y);
+                    look(x.z);
+                    look(x.w);
                 },
                 [&](uint16_t h, int) { look(h); });
+            bad = max(most[0], most[1]) > 0x7f80 || max(value[0], value[1]) == 0x7f80;
+            beyond = max(finite[0], finite[1]) >= kFarBits + 0x80;
         }
     }
-    const bool any_bad = __any(bad);
-    if (any_bad && lane_id() == 0) atomicOr(&s_bad, kNotANumber);
+    const uint32_t wrong = (__any(bad) ? kNotANumber : 0) | (__any(beyond) ? kFar : 0);
+    if (wrong && lane_id() == 0) atomicOr(&s_bad, wrong);
     __syncthreads();
     const Slice out = slice_at<F32>(a.ws, i);
     for (int b = 8 * tid; b < kGridWords; b += 8 * kCountThreads) {
@@ -758,17 +771,16 @@ __device__ __forceinline__ bool pick_counted(const Args& a, int64_t r, int64_t s
         if (tid == kGridMid / N)
             for (int k = 0; k < a.slices; ++k) several[0] += slice_at<F32>(a.ws, slice0 + k).weight[0];
     }
-    if (tid == kGridBelow / N) s.n_list = c[kGridBelow % N];
     Bins bins;
     bins.make(kGridNear, kGridMost);
     ++bins.mid;  // (bin 0 is what lies above)
     const int first = first_where<N>(s, turn, [&](int i) { return c[i] != 0; });
-    const bool below = s.n_list != 0;
-    bool grid = first > 0 && first < kGridMid && !(s.bad & kManyNear);
-    hi = F32 ? unord32(s.top) : grid ? bins.value(first) : -INFINITY;
-    if (!F32 && !grid && !(s.bad & kNotANumber)) {  // the largest logit is not known yet
+    bool grid = first > 0 && first < kGridBelow && !(s.bad & kManyNear);
+    const bool known = F32 || (grid && first != kGridMid);
+    hi = F32 ? unord32(s.top) : known ? bins.value(first) : -INFINITY;
+    if (!known && !(s.bad & kNotANumber)) {  // the largest logit
         float top = -INFINITY;
-        for_range<kThreads, 1>(row, 0, a.vocab, [&](float z, int) { top = fmaxf(top, z); });
+        for_range<kThreads, 4>(row, 0, a.vocab, [&](float z, int) { top = fmaxf(top, z); });
         atomicMax(&s.top, ord32(wave_max_f32_dpp(top)));
         __syncthreads();
         hi = unord32(s.top);
@@ -786,12 +798,15 @@ __device__ __forceinline__ bool pick_counted(const Args& a, int64_t r, int64_t s
     // y = (max - z) * rate octaves below the largest
     const double rate = rate_of(temp), unit = ldexp(1.0, -a.bits);
     auto octaves = [&](float z) { return ((double)hi - (double)z) * rate; };
-    // (weights of a bin of several values are held relative to its upper end: of at
-    // most four octaves)
+    // Weights of a bin of several values are held relative to its upper end, so none
+    // that takes part may be wide (in octaves).  In fp32 bins are wide by at most a
+    // 128th of their values' magnitude, which 64 octaves below the largest is at most
+    // that much more: that bounds those below 0; above it the first one is widest.
     constexpr double kWide = 4.0;
-    grid = grid && (!below || octaves(-kGridMost) >= kRange) &&
-           (!F32 || ((double)bins.upper(first) - (double)bins.lower(first)) * rate <= kWide) &&
-           (octaves(kGridNear) >= kRange || 2 * (double)kGridNear * rate <= kWide);
+    grid = grid && (!(s.bad & kFar) || octaves(-kGridMost) >= kRange) &&
+           (!F32 || (first < kGridMid ? ((double)bins.upper(first) - (double)bins.lower(first)) * rate <= kWide
+                                      : -(double)hi * rate + kRange <= 128 * kWide)) &&
+           (first > kGridMid || octaves(kGridNear) >= kRange || 2 * (double)kGridNear * rate <= kWide);
     if (!grid) return false;
 
     // weights by bin

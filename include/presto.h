@@ -643,7 +643,11 @@ presto_status presto_pages_compact(const presto_pages_desc *desc, const int32_t 
  *                              f_i / 2 pi is how often the pair turns over the
  *                              `original` context, and g = (r - low) /
  *                              (high - low) cut to 0 .. 1
- *     PRESTO_ROPE_RAMP_LOG     the same with the logarithms of r, low and high
+ *     PRESTO_ROPE_RAMP_LOG     the same with the logarithms of r, low and high.
+ *                              (The ramp runs between the turns themselves.  A
+ *                              model whose ramp's ends were rounded to whole
+ *                              pairs first has other frequencies in the pairs
+ *                              between them: give those in freq.)
  * Limits: rot_dim even, 2 .. 256; base > 0 and factor > 0, finite; with a ramp
  * original > 0 and 0 < low < high, finite.
  */
@@ -758,9 +762,10 @@ presto_status presto_read_kv(const presto_append_desc *desc, const void *k_pages
  * same 32 values of their outputs.  A row of q that is not finite has an
  * undefined output.
  * Arithmetic: products of the cached values with bf16 queries are exact, sums in
- * fp32; probabilities enter the second product as two bf16 (one in long
- * prompts, as in presto_window_attention).  fp32 queries and their
- * probabilities enter as three bf16 (24 bits).
+ * fp32.  With bf16 queries probabilities enter the second product as two bf16
+ * (16 bits), in calls of max_q * hq / hkv >= 128 as one (8 bits, as in the long
+ * prompts of presto_window_attention); fp32 queries and their probabilities
+ * enter as three bf16 (24 bits).
  */
 size_t presto_quant_attention_workspace(const presto_paged_attn_desc *desc, presto_dtype dt,
                                         int32_t ragged);
@@ -794,7 +799,12 @@ presto_status presto_quant_attention(const presto_paged_attn_desc *desc, presto_
  *   flags  optional: PRESTO_FLAG_NAN_LOGITS when a row holds a NaN or +inf
  *       or nothing above -inf; its token is -1 and its logprob NaN.
  * -inf logits are never drawn, nor tokens that weigh less than 2^-64 of the
- * largest.  Weights and sums are held in 64 bits.
+ * largest.  Weights are computed in 64 bits; a running sum is off by at most
+ * 2^-38 of itself (2^-41 where vocab is below 2^18).
+ * The workspace (none up to 1024 tokens) is 7.7 KB, for fp32 logits 38.5 KB, per
+ * slice of a row, for at most 2048 rows: a slice has up to 32768 tokens, fewer
+ * where rows are few.  (64 rows of 151936 fp32 logits: 39 MB; 2048 rows of 2^20:
+ * 2.5 GB.)
  * Limits: 1 <= vocab <= 2^20, row_stride >= vocab, rows 0 .. 2^21.
  */
 size_t presto_sample_workspace(presto_dtype dt, int64_t rows, int32_t vocab);

@@ -20,8 +20,9 @@
 // cores and the vector ALU of two waves per SIMD.  A tile of a wave's 64 rows is 68
 // products (1088 cycles) and some 260 vector instructions (about 1400), of which
 // half convert keys and values, a quarter are exponentials at a quarter of the
-// rate; 4 x 332..448 new tokens on 11000 take 372 us, 775 TFLOP/s, on 392
-// workgroups, two to a CU.
+// rate; 4 x 332..448 new tokens on 11000 take 375 us, 770 TFLOP/s, on 392
+// workgroups, two to a CU.  There a probability is one bf16: two, as everywhere
+// else, take the registers of 49 values and half as many products again, 671 us.
 #include <algorithm>
 #include <type_traits>
 

@@ -11,7 +11,8 @@
 //
 // Measured: 16384 rows of 40 heads of 128 bf16 values, half of them turning, 66 us,
 // 5.1 TB/s, what a large copy moves; 528 rows 5.5 us as a call, the kernel's start
-// and one round of loads.  23627 new tokens (32 + 2 x 8 heads of 128) into a 4-bit
+// and one round of loads.  Halves of a rot_dim that is no multiple of 16, whose
+// partners are read value by value, take 115 us where others take 69.  23627 new tokens (32 + 2 x 8 heads of 128) into a 4-bit
 // cache and back out of it 157 us, 4 TB/s: keys and values of a token go through 16
 // lanes each with few loads in flight (both in one pass took 182 registers, and a
 // fifth longer), and keys are coded three times (below).

@@ -823,6 +823,12 @@ __device__ __forceinline__ bool pick_counted(const Args& a, int64_t r, int64_t s
         live |= c[i] != 0;
         w[i] = 0.0;
     }
+    // what the largest logit was counted as: where its bin holds nothing else, which
+    // its sum tells, the sum is the number of tokens and not that of roundings (a
+    // border between equal tokens may be met exactly)
+    uint64_t full = 0;
+    if (F32 || first == kGridMid)
+        full = as_fixed(weight_of(((double)bins.upper(first) - (double)hi) * rate), ldexp(1.0, a.bits));
     if (__any(live)) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
@@ -830,6 +836,7 @@ __device__ __forceinline__ bool pick_counted(const Args& a, int64_t r, int64_t s
             const bool many = F32 || b == kGridMid;
             const double y = fmin(octaves(many ? bins.upper(b) : bins.value(b)), 2 * kRange);
             w[i] = c[i] ? (many ? (double)several[F32 ? i : 0] * unit : (double)c[i]) * weight_of(y) : 0.0;
+            if (many && b == first && several[F32 ? i : 0] == c[i] * full) w[i] = (double)c[i];
         }
     }
     double wb;
